@@ -246,6 +246,46 @@ fdkv_status fdkv_compress(const fdkv_dims* dims, int32_t seq_len, const void* co
                           const uint64_t* seg_offsets, const float* token_scores, const uint8_t* k_select,
                           void* cache, void* stream);
 
+/* Sparse decode (fdkv_key_bounds, fdkv_block_select, fdkv_decode_parts) reads a cache in blocks of this many tokens. */
+#define FDKV_BLOCK_TOKENS 64
+
+/*
+ * fdkv_key_bounds - device.  Per channel the least and the largest key of every
+ * block of 64 tokens of a prompt (the last block may be shorter), what
+ * fdkv_block_select chooses by.
+ *   k_layers    host array of L device pointers, layer l holds K_l [Hkv][T][d] (the keys that fdkv_compress takes)
+ *   bounds_out  host array of L device pointers, out: [Hkv][blocks_cap][2][d] in the element type of the
+ *               dims, row 0 the least and row 1 the largest; blocks past ceil(T / 64) are not written
+ *   blocks_cap  >= ceil(T / 64)
+ */
+fdkv_status fdkv_key_bounds(const fdkv_dims* dims, int32_t seq_len, const void* const* k_layers,
+                            void* const* bounds_out, int32_t blocks_cap, void* stream);
+
+/* Device workspace bytes for fdkv_block_select: batch x Hq x ceil(max_seq_len / 64) x 8. */
+fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_seq_len, size_t* bytes);
+
+/*
+ * fdkv_block_select - device.  The blocks of 64 tokens that one layer's decode
+ * step reads, per (sequence, KV head).  With U_gj = sum_c max(q_gc lo_jc, q_gc hi_jc),
+ * the largest q . K_t that block j's bounds allow query head g, a block's rank is
+ *   max over the group's heads g of (U_gj - max_j' U_gj'),
+ * in fp64.  Selected are the n_first first and the n_last last blocks of the
+ * sequence and the best others, ties to the lower block, n_sel in all; a
+ * sequence of at most n_sel blocks selects them all.
+ *   seq_lens    device int32 [batch], 0 <= T_i <= max_seq_len
+ *   bounds      device [batch][Hkv][ceil(max_seq_len / 64)][2][d] (fdkv_key_bounds with that blocks_cap)
+ *   q           device [batch][Hq][d]
+ *   n_first, n_last  >= 0, n_first + n_last <= n_sel
+ *   n_sel       >= 1
+ *   blocks_out  device int32 [batch][Hkv][n_sel], out: block numbers, ascending, then -1
+ *   counts_out  device int32 [batch][Hkv], out: min(n_sel, ceil(T_i / 64))
+ *   ws          device workspace of fdkv_block_select_workspace() bytes, 8-byte aligned
+ * batch x Hkv <= 65535 (FDKV_E_UNSUPPORTED otherwise).
+ */
+fdkv_status fdkv_block_select(const fdkv_dims* dims, int32_t batch, const int32_t* seq_lens, int32_t max_seq_len,
+                              const void* bounds, const void* q, int32_t n_first, int32_t n_last, int32_t n_sel,
+                              int32_t* blocks_out, int32_t* counts_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Device workspace bytes for fdkv_decode_attn on this batch shape. */
 fdkv_status fdkv_decode_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_seq_len, size_t* bytes);
 
@@ -372,6 +412,53 @@ typedef struct {
 fdkv_status fdkv_append(const fdkv_dims* dims, int32_t batch, const int32_t* pos, int32_t cap,
                         const void* k_new, const void* v_new, void* tail_k, void* tail_v, void* stream);
 
+/*
+ * Rotary positions: channel pair i < rot_dim / 2 of a query or key row turns by
+ * the angle pos[axis[i]] * inv_freq[i].  One axis is the usual form; images and
+ * video give every token a position on each of several axes (time, height,
+ * width) and every pair the axis it follows.
+ */
+typedef struct {
+  int32_t rot_dim;         /* channels that turn, the first of a row: a multiple of 16, 0..d (0: none) */
+  int32_t interleaved;     /* 0: pair i is channels (i, i + rot_dim / 2); 1: channels (2i, 2i + 1) */
+  int32_t n_axes;          /* 1..4 */
+  const double* inv_freq;  /* device [rot_dim / 2], radians a position (any scaling of them included) */
+  const int32_t* pos;      /* device [n_axes][n_tokens] */
+  uint8_t axis[64];        /* axis of each pair, below n_axes */
+} fdkv_rope;
+
+/*
+ * fdkv_rope_append - device.  One layer's new rows on their way into attention
+ * and the exact cache: query and key heads normed (root mean square over a
+ * head's d channels, y = x / sqrt(mean(x^2) + eps) * weight), query and key rows
+ * rotated, query rows written to q_out, key and value rows to the cache.  With a
+ * cache of one sequence and rows 0, 1, ... it lays a prompt's keys and values
+ * out as fdkv_probe and fdkv_compress take them.
+ *   n_tokens       tokens of the call, >= 0
+ *   q              device [n_tokens][Hq][d], q_stride elements from token to token
+ *   k, v           device [n_tokens][Hkv][d], k_stride / v_stride elements from token to token
+ *                  (a fused projection's output is all three, with one stride; a
+ *                  stride is >= 0 and a multiple of 16 bytes)
+ *   q_norm, k_norm device [d], or NULL: those rows are not normed
+ *   eps            finite, >= 0 (unused without a norm)
+ *   q_out          device [n_tokens][Hq][d]; q itself where q_stride is Hq * d (in
+ *                  place), otherwise apart from every input
+ *   batch, cap     the cache: sequences, and rows per (sequence, KV head)
+ *   seqs           device int32 [n_tokens], the sequence of each token; NULL: token i is of sequence i
+ *   rows           device int32 [n_tokens], the row that its key and value take.  A token whose
+ *                  sequence is outside [0, batch) or whose row is outside [0, cap) writes no key and
+ *                  no value.  Two tokens with the same sequence and row leave a mixture of both.
+ *   k_out, v_out   device [batch][Hkv][cap][d] (a layer's tail, or a prompt's K and V); only the rows named
+ *                  are written
+ * All of it in the element type of the dims.  Angles are taken in fp64, the rest
+ * in fp32, each output rounded once; value rows are copied.
+ */
+fdkv_status fdkv_rope_append(const fdkv_dims* dims, int32_t n_tokens, const fdkv_rope* rope, const void* q,
+                             int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             const void* q_norm, const void* k_norm, float eps, void* q_out, int32_t batch,
+                             const int32_t* seqs, const int32_t* rows, int32_t cap, void* k_out, void* v_out,
+                             void* stream);
+
 /* Device workspace bytes for fdkv_decode_spans: max_seq_lens host [n_spans],
  * tail_cap the tail's cap, or -1 for no tail.  At most 16 parts (spans + tail). */
 fdkv_status fdkv_decode_spans_workspace(const fdkv_dims* dims, int32_t batch, int32_t n_spans,
@@ -393,6 +480,50 @@ fdkv_status fdkv_decode_spans_workspace(const fdkv_dims* dims, int32_t batch, in
 fdkv_status fdkv_decode_spans(const fdkv_dims* dims, int32_t batch, int32_t n_spans, const fdkv_span* spans,
                               const fdkv_tail* tail, int32_t layer, const void* q, void* out, float sm_scale,
                               void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Decode over parts.  A step's attention reads, in one softmax, any mix of
+ *   FDKV_PART_OWN     a compressed span of each sequence, every token (as fdkv_decode_spans)
+ *   FDKV_PART_BLOCKS  the selected blocks of 64 tokens of a compressed span of each sequence
+ *   FDKV_PART_SHARED  a compressed span that all sequences of the batch share (a system prompt, a
+ *                     document): a cache of one sequence, read and rebuilt once for the whole batch
+ * and the exact tail of each sequence.
+ */
+typedef enum { FDKV_PART_OWN = 0, FDKV_PART_BLOCKS = 1, FDKV_PART_SHARED = 2 } fdkv_part_kind;
+
+typedef struct {
+  int32_t kind;                 /* fdkv_part_kind */
+  int32_t max_seq_len;          /* host: the largest entry of seq_lens */
+  int32_t n_sel;                /* BLOCKS: entries of a (sequence, KV head) in blocks, >= 1 */
+  const int32_t* seq_lens;      /* device [batch] (SHARED: [1]), 0 <= T_i <= max_seq_len */
+  const uint8_t* modes;         /* device [batch][n_blocks][Hkv] (SHARED: [1][n_blocks][Hkv]), 4-byte aligned, padded to 4 bytes */
+  const uint64_t* seg_offsets;  /* device, as modes */
+  const void* cache;            /* device, 256-byte aligned */
+  const int32_t* blocks;        /* BLOCKS: device [batch][Hkv][n_sel], block numbers in any order (fdkv_block_select);
+                                   a number outside [0, ceil(T_i / 64)) is passed over, one listed twice counts twice */
+  const int32_t* counts;        /* BLOCKS: device [batch][Hkv], entries of blocks that count, 0..n_sel */
+} fdkv_part;
+
+/* Device workspace bytes for fdkv_decode_parts over these parts (their kind, max_seq_len and n_sel
+ * count; the pointers are not read) and a tail of tail_cap rows, or -1 for no tail. */
+fdkv_status fdkv_decode_parts_workspace(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts,
+                                        int32_t tail_cap, size_t* bytes);
+
+/*
+ * fdkv_decode_parts - device.  One decode step of one layer:
+ * o = softmax(q K~^T * sm_scale) V~ over the tokens of every part and the
+ * tail's rows (NULL: no tail).  At most 16 parts, the tail included; a sequence
+ * with no token in any gets o = 0.  The limits, the treatment of corrupt units
+ * (of a shared part: in every sequence) and the layouts of q, out and the tail
+ * are those of fdkv_decode_spans.  Rows of the tail at or past its length, and
+ * what lies behind a span's tokens, are not used, whatever they hold.
+ *   ws   device workspace of fdkv_decode_parts_workspace() bytes (FDKV_E_WORKSPACE if smaller)
+ * Probabilities are rounded to the element type for their product with V, their
+ * sum is not; the order of fp32 sums depends on the batch and on the bounds.
+ */
+fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts,
+                              const fdkv_tail* tail, int32_t layer, const void* q, void* out, float sm_scale, void* ws,
+                              size_t ws_bytes, void* stream);
 
 /*
  * fdkv_check_conversions - diagnostic, synchronous on `stream`.  Runs the

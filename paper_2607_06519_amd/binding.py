@@ -27,9 +27,13 @@ SYMBOLS = ("fdkv_status_string", "fdkv_last_error", "fdkv_blocks", "fdkv_layout"
            "fdkv_probe_workspace", "fdkv_probe", "fdkv_compress", "fdkv_decode_workspace", "fdkv_decode_attn",
            "fdkv_append", "fdkv_decode_spans_workspace", "fdkv_decode_spans", "fdkv_decode_static_scratch_bytes",
            "fdkv_decode_attn_static", "fdkv_decode_partial", "fdkv_decode_combine", "fdkv_selection_bytes",
-           "fdkv_check_conversions")
+           "fdkv_check_conversions", "fdkv_rope_append",
+           "fdkv_key_bounds", "fdkv_block_select_workspace", "fdkv_block_select", "fdkv_decode_parts_workspace",
+           "fdkv_decode_parts")
 PAIRS, MIXED, QUADS = 0, 1, 2    # block schedules (fdkv_schedule)
 RES_CHANNELS, RES_TOKENS = 0, 1  # residual kinds (fdkv_residual)
+PART_OWN, PART_BLOCKS, PART_SHARED = 0, 1, 2  # parts of a decode step (fdkv_part_kind)
+BLOCK_TOKENS = 64                # tokens of a block of sparse decode (FDKV_BLOCK_TOKENS)
 
 
 class FdkvError(RuntimeError):
@@ -63,6 +67,17 @@ class Tail(ctypes.Structure):
     _fields_ = [("lens", ctypes.c_void_p), ("cap", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
 
 
+class Part(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("n_sel", ctypes.c_int32),
+                ("seq_lens", ctypes.c_void_p), ("modes", ctypes.c_void_p), ("seg_offsets", ctypes.c_void_p),
+                ("cache", ctypes.c_void_p), ("blocks", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("axis", ctypes.c_uint8 * 64)]
+
+
 def dims(n_layers, n_kv_heads, n_q_heads, head_dim, topk, dtype, schedule=PAIRS, residual=RES_CHANNELS,
          res_ppm=0, res_rates=()) -> Dims:
     """``res_rates``: routed candidate fractions (ppm) of token-level sets, at most 8."""
@@ -79,7 +94,7 @@ def load():
     if not os.path.exists(_LIB_PATH):
         raise RuntimeError(f"{_LIB_PATH} is not built; run __graft_entry__.build() first")
     lib = ctypes.CDLL(_LIB_PATH)
-    P, I32, U64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+    P, I32, I64, U64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
     DP = ctypes.POINTER(Dims)
     lib.fdkv_status_string.restype = ctypes.c_char_p
     lib.fdkv_status_string.argtypes = [I32]
@@ -119,6 +134,18 @@ def load():
     lib.fdkv_decode_spans_workspace.argtypes = [DP, I32, I32, P, I32, P]
     lib.fdkv_decode_spans.restype = I32
     lib.fdkv_decode_spans.argtypes = [DP, I32, I32, P, P, I32, P, P, ctypes.c_float, P, SZ, P]
+    lib.fdkv_rope_append.restype = I32
+    lib.fdkv_rope_append.argtypes = [DP, I32, P, P, I64, P, I64, P, I64, P, P, ctypes.c_float, P, I32, P, P, I32, P, P, P]
+    lib.fdkv_key_bounds.restype = I32
+    lib.fdkv_key_bounds.argtypes = [DP, I32, P, P, I32, P]
+    lib.fdkv_block_select_workspace.restype = I32
+    lib.fdkv_block_select_workspace.argtypes = [DP, I32, I32, P]
+    lib.fdkv_block_select.restype = I32
+    lib.fdkv_block_select.argtypes = [DP, I32, P, I32, P, P, I32, I32, I32, P, P, P, SZ, P]
+    lib.fdkv_decode_parts_workspace.restype = I32
+    lib.fdkv_decode_parts_workspace.argtypes = [DP, I32, I32, P, I32, P]
+    lib.fdkv_decode_parts.restype = I32
+    lib.fdkv_decode_parts.argtypes = [DP, I32, I32, P, P, I32, P, P, ctypes.c_float, P, SZ, P]
     _lib = lib
     return lib
 
@@ -311,3 +338,100 @@ def decode_spans(d: Dims, batch: int, spans: Sequence[Span], tail, layer: int, q
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),
                                     ctypes.c_float(sm_scale), _dev(ws), int(ws.numel() * ws.element_size()),
                                     _stream(stream)), "fdkv_decode_spans")
+
+
+# ----------------------------------------------------------------- a step's rows: norm, rotation, cache
+def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: bool = False) -> Rope:
+    """Rotary positions: ``inv_freq`` device float64 ``[rot_dim / 2]``, ``pos`` device int32 ``[n_tokens]``
+    or ``[n_axes][n_tokens]``, ``axis`` the axis that each pair follows (default: axis 0).  The descriptor
+    keeps both tensors."""
+    import torch
+    n_axes = 1 if pos.dim() == 1 else int(pos.shape[0])
+    if inv_freq.dtype != torch.float64 or pos.dtype != torch.int32 or pos.dim() > 2:
+        raise ValueError("rope: inv_freq is float64, pos int32 [n_tokens] or [n_axes][n_tokens]")
+    if inv_freq.numel() < rot_dim // 2 or not inv_freq.is_contiguous() or not pos.is_contiguous():
+        raise ValueError("rope: inv_freq holds rot_dim / 2 values; both tensors are contiguous")
+    if len(axis) not in (0, rot_dim // 2) or rot_dim > 128:
+        raise ValueError("rope: one axis for each of the rot_dim / 2 pairs")
+    r = Rope(int(rot_dim), int(interleaved), n_axes, _dev(inv_freq), _dev(pos), (ctypes.c_uint8 * 64)(*axis))
+    r.tensors = (inv_freq, pos)
+    return r
+
+
+def _token_rows(t, heads: int, d: int, what: str) -> int:
+    """The token stride of ``t [n_tokens][heads][d]`` whose heads are contiguous."""
+    if tuple(t.shape[1:]) != (heads, d) or (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"rope_append: {what} is [n_tokens][{heads}][{d}], contiguous but for its token stride")
+    return int(t.stride(0))
+
+
+def rope_append(d: Dims, rope: Rope, q, k, v, q_out, seqs, rows, k_out, v_out, q_norm=None, k_norm=None,
+                eps: float = 1e-6, stream=None):
+    """Queue fdkv_rope_append: ``q [n][Hq][d]``, ``k`` / ``v [n][Hkv][d]`` (views of one fused projection, say),
+    ``k_out`` / ``v_out [batch][Hkv][cap][d]``; ``seqs`` None: token i is of sequence i."""
+    n, hd = int(q.shape[0]), d.head_dim
+    qs = _token_rows(q, d.n_q_heads, hd, "q")
+    ks, vs = _token_rows(k, d.n_kv_heads, hd, "k"), _token_rows(v, d.n_kv_heads, hd, "v")
+    if k.shape[0] != n or v.shape[0] != n or rows.numel() != n or (seqs is not None and seqs.numel() != n) or \
+            (rope.rot_dim and rope.tensors[1].shape[-1] != n):
+        raise ValueError("rope_append: q, k, v, rows, seqs and the positions hold the same tokens")
+    if q_out.numel() != n * d.n_q_heads * hd or not q_out.is_contiguous() or not k_out.is_contiguous() or \
+            not v_out.is_contiguous() or k_out.shape != v_out.shape or tuple(k_out.shape[1::2]) != (d.n_kv_heads, hd):
+        raise ValueError("rope_append: q_out is [n][Hq][d], k_out and v_out [batch][Hkv][cap][d], all contiguous")
+    _check(load().fdkv_rope_append(ctypes.byref(d), n, ctypes.byref(rope), _dev(q), qs, _dev(k), ks, _dev(v), vs,
+                                   _dev(q_norm), _dev(k_norm), ctypes.c_float(eps), _dev(q_out), int(k_out.shape[0]),
+                                   _dev(seqs), _dev(rows), int(k_out.shape[2]), _dev(k_out), _dev(v_out),
+                                   _stream(stream)), "fdkv_rope_append")
+
+
+# ----------------------------------------------------------------- sparse decode: the index and the selection
+def key_bounds(d: Dims, seq_len: int, k_layers: Sequence, bounds_layers: Sequence, blocks_cap: int, stream=None):
+    """Queue fdkv_key_bounds: per layer ``k [Hkv][T][d]`` -> ``bounds [Hkv][blocks_cap][2][d]``."""
+    if len(k_layers) != d.n_layers or len(bounds_layers) != d.n_layers:
+        raise ValueError("key_bounds: one tensor of keys and one of bounds for every layer")
+    _check(load().fdkv_key_bounds(ctypes.byref(d), int(seq_len), _ptr_array(k_layers), _ptr_array(bounds_layers),
+                                  int(blocks_cap), _stream(stream)), "fdkv_key_bounds")
+
+
+def block_select_workspace(d: Dims, batch: int, max_seq_len: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdkv_block_select_workspace(ctypes.byref(d), int(batch), int(max_seq_len), ctypes.byref(n)),
+           "fdkv_block_select_workspace")
+    return int(n.value)
+
+
+def block_select(d: Dims, batch: int, seq_lens, max_seq_len: int, bounds, q, n_first: int, n_last: int, n_sel: int,
+                 blocks_out, counts_out, ws, stream=None):
+    """Queue fdkv_block_select for one layer: ``blocks_out [batch][Hkv][n_sel]``, ``counts_out [batch][Hkv]`` int32."""
+    _check(load().fdkv_block_select(ctypes.byref(d), int(batch), _dev(seq_lens), int(max_seq_len), _dev(bounds),
+                                    _dev(q), int(n_first), int(n_last), int(n_sel), _dev(blocks_out),
+                                    _dev(counts_out), _dev(ws), int(ws.numel() * ws.element_size()),
+                                    _stream(stream)), "fdkv_block_select")
+
+
+# ----------------------------------------------------------------- decode over parts
+def part(kind: int, seq_lens, max_seq_len: int, modes, seg_offsets, cache, blocks=None, counts=None,
+         n_sel: int = 0) -> Part:
+    """A part of a decode step (PART_OWN, PART_BLOCKS or PART_SHARED); the descriptor keeps its tensors."""
+    p = Part(int(kind), int(max_seq_len), int(n_sel), _dev(seq_lens), _dev(modes), _dev(seg_offsets), _dev(cache),
+             _dev(blocks), _dev(counts))
+    p.tensors = (seq_lens, modes, seg_offsets, cache, blocks, counts)
+    return p
+
+
+def decode_parts_workspace(d: Dims, batch: int, parts: Sequence[Part], tail_cap: int) -> int:
+    n = ctypes.c_size_t(0)
+    arr = _array_type(Part, max(len(parts), 1))(*parts)
+    _check(load().fdkv_decode_parts_workspace(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
+                                              int(tail_cap), ctypes.byref(n)), "fdkv_decode_parts_workspace")
+    return int(n.value)
+
+
+def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q, out, sm_scale: float, ws,
+                 stream=None):
+    """Queue fdkv_decode_parts for one layer; ``parts`` are ``Part`` descriptors, ``tail`` a ``Tail`` or None."""
+    arr = _array_type(Part, max(len(parts), 1))(*parts)
+    _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
+                                    None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),
+                                    ctypes.c_float(sm_scale), _dev(ws), int(ws.numel() * ws.element_size()),
+                                    _stream(stream)), "fdkv_decode_parts")

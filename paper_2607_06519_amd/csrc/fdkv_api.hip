@@ -170,6 +170,10 @@ ProbeWs probe_ws_layout(const fdkv_dims* d, int T) {
 // Bytes of a chunk's split-K record: (acc, m, l) of each query head of the KV head's group.
 uint64_t record_bytes(const fdkv_dims* d) { return (uint64_t)(d->n_q_heads / d->n_kv_heads) * (d->head_dim + 4) * 4; }
 
+// blocks of sparse decode in T tokens
+int block_count(int T) { return (int)(((int64_t)T + kBlockTokens - 1) / kBlockTokens); }
+static_assert(kBlockTokens == FDKV_BLOCK_TOKENS, "the header's block");
+
 uint64_t decode_chunks(int max_T) { return (uint64_t)(max_T + kDecodeWgTokens - 1) / kDecodeWgTokens; }
 
 // The split-K records of fdkv_decode_attn_static live in this file-scope
@@ -590,6 +594,128 @@ fdkv_status fdkv_append(const fdkv_dims* dims, int32_t batch, const int32_t* pos
   return FDKV_OK;
 }
 
+fdkv_status fdkv_rope_append(const fdkv_dims* dims, int32_t n_tokens, const fdkv_rope* rope, const void* q,
+                             int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             const void* q_norm, const void* k_norm, float eps, void* q_out, int32_t batch,
+                             const int32_t* seqs, const int32_t* rows, int32_t cap, void* k_out, void* v_out,
+                             void* stream) {
+  fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (n_tokens < 0 || !rope || batch < 1 || cap < 1) return FDKV_E_INVALID_ARG;
+  const int rot = rope->rot_dim;
+  if (rot < 0 || rot > dims->head_dim || rot % 16 || rope->n_axes < 1 || rope->n_axes > 4) return FDKV_E_INVALID_ARG;
+  if (rope->interleaved != 0 && rope->interleaved != 1) return FDKV_E_INVALID_ARG;
+  for (int i = 0; i < rot / 2; ++i)
+    if (rope->axis[i] >= rope->n_axes) return FDKV_E_INVALID_ARG;
+  if ((q_norm || k_norm) && !(isfinite(eps) && eps >= 0.f)) return FDKV_E_INVALID_ARG;
+  const int64_t e = elem_bytes(dims);
+  for (int64_t stride : {q_stride, k_stride, v_stride})
+    if (stride < 0 || stride > (INT64_MAX >> 34) || stride * e % 16) return FDKV_E_INVALID_ARG;
+  if (n_tokens == 0) return FDKV_OK;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) ||
+      !aligned(v_out, 16) || !aligned(rows, 4) || (seqs && !aligned(seqs, 4)) || (q_norm && !aligned(q_norm, 16)) ||
+      (k_norm && !aligned(k_norm, 16)) || (rot > 0 && (!aligned(rope->inv_freq, 8) || !aligned(rope->pos, 4))))
+    return FDKV_E_INVALID_ARG;
+  if (q_out == q && q_stride != (int64_t)dims->n_q_heads * dims->head_dim && n_tokens > 1) return FDKV_E_INVALID_ARG;
+  RopeParams rp{};
+  rp.q = q;
+  rp.k = k;
+  rp.v = v;
+  rp.q_stride = q_stride * e;
+  rp.k_stride = k_stride * e;
+  rp.v_stride = v_stride * e;
+  rp.q_norm = q_norm;
+  rp.k_norm = k_norm;
+  rp.inv_freq = rope->inv_freq;
+  rp.pos = rope->pos;
+  rp.seqs = seqs;
+  rp.rows = rows;
+  rp.q_out = q_out;
+  rp.k_out = k_out;
+  rp.v_out = v_out;
+  rp.eps = eps;
+  rp.n_tokens = n_tokens;
+  rp.hq = dims->n_q_heads;
+  rp.hkv = dims->n_kv_heads;
+  rp.d = dims->head_dim;
+  rp.rot = rot;
+  rp.batch = batch;
+  rp.cap = cap;
+  rp.interleaved = rope->interleaved != 0;
+  rp.bf16 = dims->dtype != FDKV_F32;
+  std::copy(rope->axis, rope->axis + 64, rp.axis);
+  const hipError_t he = launch_rope_append(rp, static_cast<hipStream_t>(stream));
+  if (he != hipSuccess) return hip_fail(he, "rope_append");
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_key_bounds(const fdkv_dims* dims, int32_t seq_len, const void* const* k_layers,
+                            void* const* bounds_out, int32_t blocks_cap, void* stream) {
+  fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (seq_len < 0 || !k_layers || !bounds_out || blocks_cap < block_count(seq_len)) return FDKV_E_INVALID_ARG;
+  if (seq_len == 0) return FDKV_OK;
+  for (int l = 0; l < dims->n_layers; ++l)
+    if (!aligned(k_layers[l], 16) || !aligned(bounds_out[l], 16)) return FDKV_E_INVALID_ARG;
+  if (dims->n_kv_heads > 65535) return FDKV_E_UNSUPPORTED;
+  BoundsParams bp{};
+  for (int l = 0; l < dims->n_layers; ++l) {
+    bp.k[l] = k_layers[l];
+    bp.out[l] = bounds_out[l];
+  }
+  bp.n_layers = dims->n_layers;
+  bp.hkv = dims->n_kv_heads;
+  bp.seq_len = seq_len;
+  bp.cap = blocks_cap;
+  bp.d = dims->head_dim;
+  bp.bf16 = dims->dtype != FDKV_F32;
+  const hipError_t e = launch_key_bounds(bp, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "key_bounds");
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_seq_len, size_t* bytes) {
+  fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (batch < 1 || max_seq_len < 0 || !bytes) return FDKV_E_INVALID_ARG;
+  *bytes = (size_t)((uint64_t)batch * dims->n_q_heads * std::max(block_count(max_seq_len), 1) * 8);
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_block_select(const fdkv_dims* dims, int32_t batch, const int32_t* seq_lens, int32_t max_seq_len,
+                              const void* bounds, const void* q, int32_t n_first, int32_t n_last, int32_t n_sel,
+                              int32_t* blocks_out, int32_t* counts_out, void* ws, size_t ws_bytes, void* stream) {
+  size_t need = 0;
+  fdkv_status st = fdkv_block_select_workspace(dims, batch, max_seq_len, &need);
+  if (st != FDKV_OK) return st;
+  if (n_sel < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_sel) return FDKV_E_INVALID_ARG;
+  if (!aligned(seq_lens, 4) || !aligned(bounds, 16) || !aligned(q, 16) || !aligned(blocks_out, 4) ||
+      !aligned(counts_out, 4) || !aligned(ws, 8))
+    return FDKV_E_INVALID_ARG;
+  if (ws_bytes < need) return FDKV_E_WORKSPACE;
+  if ((int64_t)batch * dims->n_kv_heads > 65535) return FDKV_E_UNSUPPORTED;
+  SelectParams sp{};
+  sp.seq_lens = seq_lens;
+  sp.bounds = bounds;
+  sp.q = q;
+  sp.ws = static_cast<double*>(ws);
+  sp.blocks = blocks_out;
+  sp.counts = counts_out;
+  sp.batch = batch;
+  sp.hkv = dims->n_kv_heads;
+  sp.hq = dims->n_q_heads;
+  sp.d = dims->head_dim;
+  sp.max_seq_len = max_seq_len;
+  sp.cap = block_count(max_seq_len);
+  sp.n_first = n_first;
+  sp.n_last = n_last;
+  sp.n_sel = n_sel;
+  sp.bf16 = dims->dtype != FDKV_F32;
+  const hipError_t e = launch_block_select(sp, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "block_select");
+  return FDKV_OK;
+}
+
 fdkv_status fdkv_check_conversions(uint64_t* mismatches, void* stream) {
   if (!mismatches) return FDKV_E_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -792,6 +918,225 @@ fdkv_status fdkv_decode_attn_static(const fdkv_dims* dims, int32_t batch, const 
   if (st != FDKV_OK) return st;
   return fdkv_decode_attn(dims, batch, seq_lens, max_seq_len, modes, seg_offsets, cache, layer, q, out, sm_scale, ws,
                           kStaticScratchBytes, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// How a decode over parts splits its tokens over workgroups.  The parts of
+// single sequences come first in the record slots, then the shared ones.
+struct PartsPlan {
+  int n_own, n_shared;          // parts (the tail among the own ones)
+  int own[kMaxParts], shared[kMaxParts];  // their indices in the call; -1: the tail
+  int own_tiles_per_wg, shared_tiles_per_wg, nq, rows, row_groups;
+  int64_t slots[kMaxParts];     // record slots of each part, own ones first
+  int64_t own_slots, total_slots;
+};
+
+// Workgroups that fill the card: two of up to 32 query rows to a CU, or one of 64.
+constexpr int64_t kPartsWorkgroups = 512;
+
+fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
+                       PartsPlan* out) {
+  if (batch < 1 || n_parts < 0 || n_parts + (tail_cap >= 0 ? 1 : 0) > kMaxParts || (n_parts > 0 && !parts))
+    return FDKV_E_INVALID_ARG;
+  const int tok = dims->dtype == FDKV_F32 ? 16 : 32;  // tokens of a tile
+  const int64_t G = dims->n_q_heads / dims->n_kv_heads, hkv = dims->n_kv_heads;
+  if (batch * G * hkv >= (1ll << 30)) return FDKV_E_UNSUPPORTED;
+  PartsPlan p{};
+  int64_t tiles[kMaxParts], own_tiles = 0, shared_tiles = 0;
+  for (int i = 0; i < n_parts; ++i) {
+    const fdkv_part& pt = parts[i];
+    if (pt.max_seq_len < 0 || pt.kind < FDKV_PART_OWN || pt.kind > FDKV_PART_SHARED) return FDKV_E_INVALID_ARG;
+    if (pt.kind == FDKV_PART_BLOCKS && pt.n_sel < 1) return FDKV_E_INVALID_ARG;
+    if (pt.kind == FDKV_PART_SHARED) {
+      p.shared[p.n_shared++] = i;
+      shared_tiles += ((int64_t)pt.max_seq_len + tok - 1) / tok;
+      continue;
+    }
+    int64_t n = ((int64_t)pt.max_seq_len + tok - 1) / tok;
+    // (a list may name blocks more than once, so its length counts, not the span's)
+    if (pt.kind == FDKV_PART_BLOCKS) n = pt.max_seq_len ? (int64_t)pt.n_sel * (kBlockTokens / tok) : 0;
+    tiles[p.n_own] = n;
+    own_tiles += n;
+    p.own[p.n_own++] = i;
+  }
+  if (tail_cap >= 0) {
+    tiles[p.n_own] = ((int64_t)tail_cap + tok - 1) / tok;
+    own_tiles += tiles[p.n_own];
+    p.own[p.n_own++] = -1;
+  }
+  auto per_wg = [](int64_t tiles, int64_t groups, int64_t most) {
+    const int64_t n = (tiles + std::max<int64_t>(groups, 1) - 1) / std::max<int64_t>(groups, 1);
+    return (int)std::min<int64_t>(most, std::max<int64_t>(4, (n + 3) / 4 * 4));
+  };
+  // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
+  p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 256);
+  p.rows = (int)(batch * G);
+  p.nq = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
+  p.row_groups = (p.rows + 16 * p.nq - 1) / (16 * p.nq);
+  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (p.nq == 4 ? 2 : 1) / (hkv * p.row_groups), 1 << 28);
+  for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
+  p.total_slots = p.own_slots;
+  for (int i = 0; i < p.n_shared; ++i) {
+    const int64_t n = ((int64_t)parts[p.shared[i]].max_seq_len + tok - 1) / tok;
+    p.total_slots += p.slots[p.n_own + i] = (n + p.shared_tiles_per_wg - 1) / p.shared_tiles_per_wg;
+  }
+  // workgroups and record slots are counted in 31 bits
+  if (batch * hkv * std::max<int64_t>(p.total_slots, 1) >= (1ll << 31) ||
+      (hkv * p.total_slots + 8) * p.row_groups >= (1ll << 31))
+    return FDKV_E_UNSUPPORTED;
+  *out = p;
+  return FDKV_OK;
+}
+
+uint64_t parts_bytes(const fdkv_dims* dims, int32_t batch, const PartsPlan& p) {
+  return (uint64_t)batch * dims->n_kv_heads * std::max<int64_t>(p.total_slots, 1) * record_bytes(dims);
+}
+
+hipError_t launch_parts(const PartsParams& p, hipStream_t s) {
+  if (p.coef8) return p.d == 128 ? launch_parts_c8_d128(p, s) : launch_parts_c8_d64(p, s);
+  if (p.bf16) return p.d == 128 ? launch_parts_bf16_d128(p, s) : launch_parts_bf16_d64(p, s);
+  return p.d == 128 ? launch_parts_f32_d128(p, s) : launch_parts_f32_d64(p, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+fdkv_status fdkv_decode_parts_workspace(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts,
+                                        int32_t tail_cap, size_t* bytes) {
+  fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  PartsPlan plan;
+  st = plan_parts(dims, batch, n_parts, parts, tail_cap, &plan);
+  if (st != FDKV_OK) return st;
+  if (!bytes) return FDKV_E_INVALID_ARG;
+  *bytes = (size_t)parts_bytes(dims, batch, plan);
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts,
+                              const fdkv_tail* tail, int32_t layer, const void* q, void* out, float sm_scale, void* ws,
+                              size_t ws_bytes, void* stream) {
+  fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (layer < 0 || layer >= dims->n_layers || (tail && tail->cap < 0)) return FDKV_E_INVALID_ARG;
+  PartsPlan plan;
+  st = plan_parts(dims, batch, n_parts, parts, tail ? tail->cap : -1, &plan);
+  if (st != FDKV_OK) return st;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || !isfinite(sm_scale)) return FDKV_E_INVALID_ARG;
+  const uint64_t row = (uint64_t)dims->head_dim * elem_bytes(dims);
+  for (int i = 0; i < n_parts; ++i) {
+    const fdkv_part& pt = parts[i];
+    if (!aligned(pt.seq_lens, 4) || !aligned(pt.modes, 4) || !aligned(pt.seg_offsets, 8) || !aligned(pt.cache, 256))
+      return FDKV_E_INVALID_ARG;
+    if (pt.kind == FDKV_PART_BLOCKS && (!aligned(pt.blocks, 4) || !aligned(pt.counts, 4))) return FDKV_E_INVALID_ARG;
+    if ((uint64_t)pt.max_seq_len * row >= (1ull << 31)) return FDKV_E_UNSUPPORTED;
+    if (tokens_mode(dims) && residual_token_count((uint64_t)pt.max_seq_len, max_ppm(dims)) * 3 * row >= (1ull << 31))
+      return FDKV_E_UNSUPPORTED;
+  }
+  if (tail) {
+    if (!aligned(tail->lens, 4) || !aligned(tail->k, 16) || !aligned(tail->v, 16)) return FDKV_E_INVALID_ARG;
+    if ((uint64_t)tail->cap * row >= (1ull << 31)) return FDKV_E_UNSUPPORTED;
+  }
+  if (ws_bytes < parts_bytes(dims, batch, plan)) return FDKV_E_WORKSPACE;
+
+  PartsParams p{};
+  p.q = q;
+  p.ws = static_cast<float*>(ws);
+  p.hkv = dims->n_kv_heads;
+  p.hq = dims->n_q_heads;
+  p.G = p.hq / p.hkv;
+  while ((1 << p.g_shift) < p.G) ++p.g_shift;
+  p.batch = batch;
+  p.d = dims->head_dim;
+  p.topk = dims->topk;
+  const Sched sch = sched_of(dims);
+  int blk = 0;
+  while (!(layer < sch.first[blk] + sch.size[blk])) ++blk;
+  p.n_blocks = sch.n;
+  p.block = blk;
+  p.pos = layer - sch.first[blk];
+  p.bsize = sch.size[blk];
+  layer_weights(p.bsize, p.pos, p.wres);
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.bf16 = dims->dtype != FDKV_F32;
+  p.coef8 = dims->dtype == FDKV_BF16_E4M3;
+  p.tokres = tokens_mode(dims);
+  p.res_ppm = dims->res_ppm;
+  p.n_rates = dims->n_rates;
+  for (int j = 0; j < dims->n_rates; ++j) p.rates_ppm[j] = dims->rates_ppm[j];
+  p.by_hkv.set((uint32_t)p.hkv);
+  p.by_topk.set((uint32_t)std::max(p.topk, 1));
+  p.n_slots_total = (int)plan.total_slots;
+  int base = 0;
+  for (int i = 0; i < plan.n_own + plan.n_shared; ++i) {
+    const int at = i < plan.n_own ? plan.own[i] : plan.shared[i - plan.n_own];
+    PartsPart& o = p.part[i];
+    p.part_base[i] = base;
+    base += (int)plan.slots[i];
+    if (at < 0) {
+      o.lens = tail->lens;
+      o.max_len = tail->cap;
+      p.tail_k = tail->k;
+      p.tail_v = tail->v;
+      p.tail_cap = tail->cap;
+      continue;
+    }
+    const fdkv_part& pt = parts[at];
+    o.lens = pt.seq_lens;
+    o.max_len = pt.max_seq_len;
+    o.cache = static_cast<const uint8_t*>(pt.cache);
+    o.modes = pt.modes;
+    o.seg_off = pt.seg_offsets;
+    if (pt.kind == FDKV_PART_BLOCKS) {
+      o.blocks = pt.blocks;
+      o.counts = pt.counts;
+      o.n_sel = pt.n_sel;
+    }
+  }
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (plan.own_slots > 0) {
+    p.shared = false;
+    p.nq = 1;
+    p.tiles_per_wg = plan.own_tiles_per_wg;
+    p.slot0 = 0;
+    p.n_slots = (int)plan.own_slots;
+    p.part0 = 0;
+    p.part_end = plan.n_own;
+    p.by_slots.set((uint32_t)p.n_slots);
+    const hipError_t e = launch_parts(p, s);
+    if (e != hipSuccess) return hip_fail(e, "decode_parts");
+  }
+  if (plan.total_slots > plan.own_slots) {
+    p.shared = true;
+    p.nq = plan.nq;
+    p.rows = plan.rows;
+    p.row_groups = plan.row_groups;
+    p.by_groups.set((uint32_t)p.row_groups);
+    p.tiles_per_wg = plan.shared_tiles_per_wg;
+    p.slot0 = (int)plan.own_slots;
+    p.n_slots = (int)(plan.total_slots - plan.own_slots);
+    p.part0 = plan.n_own;
+    p.part_end = plan.n_own + plan.n_shared;
+    const hipError_t e = launch_parts(p, s);
+    if (e != hipSuccess) return hip_fail(e, "decode_parts");
+  }
+  DecodeParams mp{};
+  mp.out = out;
+  mp.ws = p.ws;
+  mp.hkv = p.hkv;
+  mp.hq = p.hq;
+  mp.d = p.d;
+  mp.batch = batch;
+  mp.bf16 = p.bf16;
+  mp.n_chunks_total = p.n_slots_total;
+  mp.n_sub = 1;
+  const hipError_t e = launch_decode_merge(mp, s);
+  if (e != hipSuccess) return hip_fail(e, "decode_merge");
+  return FDKV_OK;
 }
 
 }  // extern "C"

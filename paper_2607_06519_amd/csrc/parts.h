@@ -1,0 +1,814 @@
+// Decode attention over parts (fdkv_decode_parts): whole spans, the selected
+// blocks of a span, the exact tail, and spans that all sequences of the batch
+// share.  One softmax over all of them: every workgroup writes an (acc, m, l)
+// record per query row of its chunk, and the records merge as those of the other
+// decode calls do.
+//
+// The columns of a wave's matrix products are query rows: the G heads of a
+// sequence's group, or, over a shared span, the rows of the whole batch, 16 NQ of
+// them, so that a shared token is read and rebuilt once for all.  A wave walks
+// tiles of TOK = 32 tokens (16 in fp32) by itself, with no barrier before the
+// final merge of the workgroup's four waves:
+//   S^T = K~ Q^T   A: 16 tokens x 32 channels straight from memory in the
+//                  operand's layout, B: the queries, kept in registers;
+//   softmax        a column lives on the four lanes l, l + 16, l + 32, l + 48, its
+//                  logits in their registers; running max (moved only by more
+//                  than 2^8) and sum in fp32;
+//   O^T += V~^T P^T  the probabilities are the B operand where they lie (the
+//                  tokens of a lane's S^T registers are the tokens of its B
+//                  slots), A: transposed reads of the V tile, which goes through
+//                  LDS for that, its 16-byte pieces permuted by the row so that
+//                  the 16 rows of an operand lie in distinct banks.
+// K~ = M + R and V~ = M + R: M as stored (bf16 or E4M3 widened to bf16, exact),
+// R a tile of LDS that is zero but for the residual entries (or the rows of a
+// token-level set) of the tile, each in its place: +-D of a pair is a bf16 value;
+// the sum of a block of four's weighted coefficients goes in as its bf16 rounding
+// and, for K (whose error an exponential would amplify), once more as the rest,
+// so a rebuilt key carries 2^-16 of its residual.  R multiplies the same operands
+// as M; no rebuilt value is rounded and no entry is gathered per query row.
+// Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
+//
+// What bounds it: HBM as long as 16 NQ columns are busy with less than the time
+// a tile takes to arrive (a CU gets some 13 bytes a cycle; a tile of 16 KB on one
+// SIMD of it takes 5000 cycles, its products at 64 columns 1100).
+#pragma once
+
+#include <type_traits>
+
+#include "decode_shape.h"
+#include "fdkv_common.h"
+#include "fdkv_kernels.h"
+
+namespace fdkv {
+
+namespace parts {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef short i16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+
+constexpr uint32_t kOob = 0x80000000u;  // buffer offset past every plane (planes are < 2^31 bytes): loads read 0
+constexpr float kSlack = 8.f;           // log2 headroom of the running reference max
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* base, uint64_t bytes) {
+  const uint32_t n = bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : (uint32_t)bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, n, 0x00020000);
+}
+template <int CACHE>
+__device__ __forceinline__ uint4 ld128(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  const auto v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, CACHE);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ uint2 ld64(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+  return make_uint2(v[0], v[1]);
+}
+
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3x2_bf16(uint32_t w) {  // exact: every E4M3 value is a bf16 value
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+}
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
+  return make_uint4(e4m3x2_bf16<false>(a), e4m3x2_bf16<true>(a), e4m3x2_bf16<false>(b), e4m3x2_bf16<true>(b));
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Max / sum over the four lanes of a column (l, l + 16, l + 32, l + 48).
+__device__ __forceinline__ float col_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float col_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Orders the compiler's LDS accesses; the hardware runs a wave's in order.
+__device__ __forceinline__ void lds_fence() { asm volatile("" ::: "memory"); }
+
+enum : int { kTyF32 = 0, kTyBf16 = 1, kTyC8 = 2 };
+
+template <int D, int TY>
+struct TileOf {
+  static constexpr bool F32 = TY == kTyF32;
+  static constexpr int E = F32 ? 4 : 2;            // bytes of an element
+  static constexpr int TOK = F32 ? 16 : 32;        // tokens of a tile
+  static constexpr int RB = D * E;                 // bytes of a row
+  static constexpr int NP = RB / 16;               // 16-byte pieces of a row
+  static constexpr int RPL = 64 / NP;              // rows of a load
+  static constexpr int NL = D / 16;                // loads of a tile's K (V): TOK * RB / 1024
+  static constexpr int KK = F32 ? D / 16 : D / 32; // pieces of the channels in an operand row
+  static constexpr int TI = F32 ? 1 : 2;           // 16-token operands of a tile
+  static constexpr int TILE_BYTES = TOK * RB;
+  static constexpr int CT = D / 16;                // 16-channel tiles of the output
+  static constexpr int TPB = kBlockTokens / TOK;   // tiles of a selected block
+};
+
+// First of the four tokens of lane group g's rows of the i-th 16-token operand.
+// (An E4M3 slot holds rows r and r + 512 / D of a 1 KB block, which go to the two
+// operands of one lane; the other types take the same order.)
+template <int D, int TY>
+__device__ __forceinline__ int quad_row(int g, int i) {
+  if constexpr (TY == kTyF32) return 4 * g;
+  return D == 128 ? 8 * g + 4 * i : 16 * (g >> 1) + 4 * (g & 1) + 8 * i;
+}
+
+// Byte of a 16-byte piece of a row in an LDS tile: pieces permuted so that the
+// rows of an operand (one piece, 16 rows) and of a transposed read lie in
+// distinct banks.
+template <int D, int TY>
+__device__ __forceinline__ uint32_t piece_at(int row, int piece) {
+  int f;
+  if constexpr (TY == kTyF32)
+    f = row & 15;
+  else if constexpr (D == 128)
+    f = (row & 3) | (((row >> 3) & 3) << 2);
+  else
+    f = ((row >> 1) & 1) | (((row >> 2) & 1) << 1) | (((row >> 4) & 1) << 2);
+  return (uint32_t)(row * TileOf<D, TY>::RB + ((piece ^ f) << 4));
+}
+
+// Eight consecutive residual entries of a tile as loaded, and (blocks of four)
+// the code before them and the two entries after.
+struct Entries {
+  uint4 ix;
+  uint4 v0, v1;
+  uint32_t prev, nix, nv0, nv1;
+};
+
+}  // namespace parts
+
+template <int D, int NQ, int TY>
+__global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams P) {
+  using namespace parts;
+  using S = TileOf<D, TY>;
+  constexpr bool F32 = S::F32;
+  constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
+  constexpr int RS = D + 4;
+  constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
+  constexpr int kWaveLds = 2 * S::TILE_BYTES;
+  static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kWaveLds];
+  __shared__ float ml_lds[4][16][2];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, lane = threadIdx.x & 63;
+  const int lc = lane & 15, lg = lane >> 4;  // column (or operand row) and lane group
+  const int G = P.G, hkv = P.hkv;
+
+  // ---- which chunk
+  int seq, head, slot, row0;
+  if (P.shared) {
+    // the row groups of one chunk follow each other on one XCD (workgroups go to the XCDs in turn)
+    const uint32_t x = blockIdx.x & 7u, y = blockIdx.x >> 3;
+    const uint32_t ym = P.by_groups.div(y);
+    const uint32_t w = ym * 8 + x;
+    if (w >= (uint32_t)(hkv * P.n_slots)) return;
+    slot = (int)P.by_hkv.div(w);
+    head = (int)w - slot * hkv;
+    row0 = (int)(y - ym * P.row_groups) * 16 * NQ;
+    seq = 0;
+  } else {
+    const uint32_t sl = P.by_hkv.div(blockIdx.x);
+    head = (int)(blockIdx.x - sl * hkv);
+    seq = (int)P.by_slots.div(sl);
+    slot = (int)sl - seq * P.n_slots;
+    row0 = 0;
+  }
+  slot += P.slot0;
+  int part = P.part0;
+#pragma unroll 1
+  while (part + 1 < P.part_end && slot >= P.part_base[part + 1]) ++part;
+  const PartsPart pt = P.part[part];
+  const bool tail = pt.cache == nullptr;
+  const int useq = P.shared ? 0 : seq;
+  const int T = min(max(as_const(pt.lens)[useq], 0), pt.max_len);
+  const int chunk0 = (slot - P.part_base[part]) * P.tiles_per_wg;  // first tile
+
+  // ---- the unit
+  uint32_t mbyte = (uint32_t)kExact;
+  uint64_t seg_off = 0;
+  if (!tail) {
+    const uint64_t u = ((uint64_t)useq * P.n_blocks + P.block) * hkv + head;
+    mbyte = (as_const(reinterpret_cast<const uint32_t*>(pt.modes))[u >> 2] >> (8 * (u & 3))) & 0xFFu;
+    seg_off = as_const(pt.seg_off)[u];
+  }
+  const bool bad_unit = !unit_byte_ok(mbyte, P.tokres ? P.n_rates : 0) || (seg_off & (kPlaneAlign - 1));
+  const int mode = mode_of(mbyte);
+  int n_tiles;  // of the part
+  const int32_t* list = nullptr;
+  if (pt.blocks) {
+    const int64_t at = (int64_t)seq * hkv + head;
+    list = pt.blocks + at * pt.n_sel;
+    n_tiles = min(max(as_const(pt.counts)[at], 0), pt.n_sel) * S::TPB;
+  } else {
+    n_tiles = (T + TOK - 1) / TOK;
+  }
+  const int end = min(chunk0 + P.tiles_per_wg, n_tiles);
+  int n = chunk0 + wave < end ? (end - chunk0 - wave + 3) / 4 : 0;  // the wave's tiles: chunk0 + wave + 4 i
+  if (bad_unit) n = 0;
+
+  // ---- queries
+  const uint8_t* q_all = static_cast<const uint8_t*>(P.q);
+  const int rows = P.shared ? P.rows : G;
+  auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // of the call: (sequence, head of the group)
+    const int r = row0 + col;
+    s = P.shared ? r >> P.g_shift : seq;
+    g = P.shared ? r & (G - 1) : r;
+    return r < rows;
+  };
+  uint4 qf[NQ][KK];
+  {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      int s, g;
+      const bool ok = row_of(16 * q + lc, s, g);
+      const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) qf[q][kk] = ok ? src[4 * kk + lg] : make_uint4(0, 0, 0, 0);
+    }
+  }
+
+  float m[NQ], l[NQ];
+  f32x4_t acc[NQ][CT];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[q][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  uint8_t* vt = lds + wave * kWaveLds;                 // the V tile
+  uint8_t* rt = vt + S::TILE_BYTES;                    // R
+  const uint8_t* seg = pt.cache + seg_off;
+
+  // RES: 0 none, 1 per-token entries, 2 a token-level set
+  auto walk = [&](auto c8_tag, auto res_tag) __attribute__((always_inline)) {
+    constexpr bool C8 = decltype(c8_tag)::value;       // shared planes and residual values in E4M3
+    constexpr int RES = decltype(res_tag)::value;
+    constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
+    constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
+    const int nb = P.bsize, k = P.topk;
+    const bool q4 = nb == 4;
+    const float w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2];
+
+    // ---- planes
+    const uint32_t dense = C8 ? ((uint32_t)T * D + kC8Block - 1) / kC8Block * kC8Block : (uint32_t)T * RB;
+    const uint32_t plane = (dense + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign;
+    const uint8_t* kb = seg + (uint64_t)(mode == kExact ? P.pos : 0) * plane;
+    const uint8_t* vb = kb + (uint64_t)(mode == kExact ? nb : 1) * plane;
+    if (tail) {
+      const uint64_t off = ((uint64_t)seq * hkv + head) * (uint64_t)P.tail_cap * RB;
+      kb = static_cast<const uint8_t*>(P.tail_k) + off;
+      vb = static_cast<const uint8_t*>(P.tail_v) + off;
+    }
+    const auto kr = rsrc(kb, dense), vr = rsrc(vb, dense);
+    // residual entries
+    const uint32_t ib = RES == 1 ? (uint32_t)T * k * (q4 ? 2 : 1) : 0, xb = RES == 1 ? (uint32_t)T * k * C : 0;
+    const uint32_t ip = (ib + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign, xp = (xb + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign;
+    const uint8_t* ent = seg + 2 * (uint64_t)plane;
+    // (whole 16-byte pieces: a load whose last word lies half behind the bytes would read 0 for all of it.  The
+    // plane's padding may hold anything; entries of tokens behind the last are not used.)
+    const uint32_t ibr = (ib + 15) & ~15u, xbr = (xb + 15) & ~15u;
+    const auto ikr = rsrc(ent, ibr), xkr = rsrc(ent + ip, xbr);
+    const auto ivr = rsrc(ent + ip + xp, ibr), xvr = rsrc(ent + 2 * (uint64_t)ip + xp, xbr);
+    // token-level set
+    TokLayout L{};
+    uint64_t set_bytes = 0;
+    if constexpr (RES == 2) {
+      const int ppm = unit_ppm(P.res_ppm, P.n_rates, P.rates_ppm, mbyte);
+      L = tok_layout(mode, (uint64_t)T, D, ppm, S::E, C, nb);
+      set_bytes = residual_token_count((uint64_t)T, ppm) * (uint64_t)(nb - 1) * D * C;
+    }
+    const auto hkr = rsrc(seg + L.hk, set_bytes), hvr = rsrc(seg + L.hv, set_bytes);
+    const auto* mask_words = as_const(reinterpret_cast<const uint32_t*>(seg + L.mask));
+    const auto* counts = as_const(reinterpret_cast<const uint32_t*>(seg + L.count));
+
+    // ---- the wave's tiles
+    int my_block = 0;  // lane i: the block of the wave's tile i
+    if (list) {
+      const int u = chunk0 + wave + 4 * lane;
+      my_block = lane < n ? list[u / S::TPB] : 0;
+      const int total = (T + kBlockTokens - 1) / kBlockTokens;
+      if (my_block < 0 || my_block >= total) my_block = -1;
+    }
+    // first token of the wave's tile i; T where it has none (every load reads zeros, every token is masked)
+    auto tile_token = [&](int i) __attribute__((always_inline)) -> int {
+      const int u = chunk0 + wave + 4 * i;
+      int t = u * TOK;
+      if (list) {
+        const int b = __builtin_amdgcn_readlane(my_block, i & 63);
+        t = b < 0 ? T : b * kBlockTokens + (u % S::TPB) * TOK;
+      }
+      return i < n ? t : T;
+    };
+
+    // ---- loads
+    uint4 kv[NLD], vv[NLD];
+    auto load_tile = [&](const __amdgpu_buffer_rsrc_t& r, int t0, uint32_t lane_off, uint4 (&x)[NLD], bool operand) {
+      const uint32_t base = t0 < T ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        uint32_t step;
+        if (!operand)
+          step = (uint32_t)i * 1024;
+        else if constexpr (C8 || F32)
+          step = (uint32_t)i * 64;                                          // the next pieces of the row(s)
+        else
+          step = (uint32_t)(i / KK) * (quad_row<D, TY>(0, 1) * RB) + (uint32_t)(i % KK) * 64;
+        x[i] = ld128<0>(r, base + lane_off + step);
+      }
+    };
+    // K in the operand's layout: lane (lc, lg) holds pieces 4 kk + lg of its token(s)
+    uint32_t k_off;
+    if constexpr (C8) {
+      constexpr int half = kC8Block / D / 2;
+      k_off = (uint32_t)(kC8Block * (lc / half) + 16 * ((lc % half) * (D / 8) + lg));
+    } else {
+      k_off = (uint32_t)((quad_row<D, TY>(lc >> 2, 0) + (lc & 3)) * RB + lg * 16);
+    }
+    const uint32_t v_off = (uint32_t)lane * 16;
+
+    Entries ek{}, ev{};
+    auto load_entries = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, int chunk, Entries& e) __attribute__((always_inline)) {
+      const uint32_t e0 = (uint32_t)t0 * k + 8u * (uint32_t)chunk;
+      const bool ok = t0 < T && chunk < TOK / 8 * k;
+      const uint32_t vo = ok ? e0 * C : kOob;
+      if constexpr (C == 1) {
+        const uint2 a = ld64(xr, vo);
+        e.v0 = make_uint4(a.x, a.y, 0, 0);
+      } else {
+        e.v0 = ld128<0>(xr, vo);
+        if constexpr (C == 4) e.v1 = ld128<0>(xr, vo + 16);
+      }
+      if (q4) {
+        const uint32_t io = ok ? e0 * 2 : kOob;
+        e.ix = ld128<0>(ir, io);
+        e.prev = ok && e0 > 0 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(ir, io - 2, 0, 0) : 0u;
+        e.nix = __builtin_amdgcn_raw_buffer_load_b32(ir, io + 16, 0, 0);
+        if constexpr (C == 1) {
+          e.nv0 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(xr, vo + 8, 0, 0);
+        } else if constexpr (C == 2) {
+          e.nv0 = __builtin_amdgcn_raw_buffer_load_b32(xr, vo + 16, 0, 0);
+        } else {
+          const uint2 a = ld64(xr, vo + 32);
+          e.nv0 = a.x;
+          e.nv1 = a.y;
+        }
+      } else {
+        const uint2 a = ld64(ir, ok ? e0 : kOob);
+        e.ix = make_uint4(a.x, a.y, 0, 0);
+      }
+    };
+    // entry i of the chunk as fp32 (8 and 9: the two after it)
+    auto value = [&](const Entries& e, int i) __attribute__((always_inline)) -> float {
+      if constexpr (C == 4) {
+        return as_f32(i < 4 ? word(e.v0, i) : i < 8 ? word(e.v1, i - 4) : i == 8 ? e.nv0 : e.nv1);
+      } else if constexpr (C == 2) {
+        const uint32_t w = i < 8 ? word(e.v0, i / 2) : e.nv0;
+        return (i & 1) ? bf16_hi(w) : bf16_lo(w);
+      } else {
+        const uint32_t raw = i < 8 ? word(e.v0, i / 4) : e.nv0;
+        const uint32_t w = (i & 2) && i < 8 ? e4m3x2_bf16<true>(raw) : e4m3x2_bf16<false>(raw);
+        return (i & 1) ? bf16_hi(w) : bf16_lo(w);
+      }
+    };
+    auto code = [&](const Entries& e, int i) __attribute__((always_inline)) -> uint32_t {  // blocks of four
+      const uint32_t w = i < 8 ? word(e.ix, i / 2) : e.nix;
+      return (i & 1) ? w >> 16 : w & 0xFFFFu;
+    };
+    auto put = [&](int t, int c, float x, bool rest) __attribute__((always_inline)) {
+      const uint32_t at = piece_at<D, TY>(t, c / (16 / S::E)) + (uint32_t)(c % (16 / S::E)) * S::E;
+      if constexpr (F32) {
+        *reinterpret_cast<float*>(rt + at) = x;
+      } else {
+        const uint32_t hi = f32_to_bf16_bits(x);
+        *reinterpret_cast<uint16_t*>(rt + at) = (uint16_t)(rest ? f32_to_bf16_bits(x - bf16_to_f32((uint16_t)hi)) : hi);
+      }
+    };
+    // The chunk's entries into R; rest: what their bf16 rounding leaves.
+    auto scatter_chunk = [&](const Entries& e, int chunk, int held, bool rest) __attribute__((always_inline)) {  // held: tokens of the tile
+      if (chunk >= TOK / 8 * k) return;
+      const int e0 = 8 * chunk;
+      int t = (int)P.by_topk.div((uint32_t)e0), j = e0 - t * k;  // token of the tile, entry of the token
+      if (!q4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (t < held) put(t, (int)((word(e.ix, i / 4) >> (8 * (i & 3))) & (D - 1)), w1 * value(e, i), false);
+          if (++j == k) {
+            j = 0;
+            ++t;
+          }
+        }
+        return;
+      }
+      // a channel's up to three frequencies are neighbours (codes 4 c + j ascend): the first of them adds up
+      auto weighted = [&](int i) __attribute__((always_inline)) -> float {
+        const uint32_t f = code(e, i) & 3u;
+        const float a = w1, b = w2, c = w3;  // (values: a choice among captured variables would keep them in memory)
+        return (f == 1 ? +a : f == 2 ? +b : +c) * value(e, i);
+      };
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t c = code(e, i) >> 2;
+        const uint32_t before = (i ? code(e, i - 1) : e.prev) >> 2;
+        if (t < held && (j == 0 || before != c)) {
+          float x = weighted(i);
+          if (j + 1 < k && (code(e, i + 1) >> 2) == c) {
+            x += weighted(i + 1);
+            if (j + 2 < k && (code(e, i + 2) >> 2) == c) x += weighted(i + 2);
+          }
+          put(t, (int)(c & (D - 1)), x, rest);
+        }
+        if (++j == k) {
+          j = 0;
+          ++t;
+        }
+      }
+    };
+    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, const Entries& e, bool rest) __attribute__((always_inline)) {
+      scatter_chunk(e, lane, T - t0, rest);
+      for (int c = lane + 64; c < TOK / 8 * k; c += 64) {  // more than eight entries a lane: loaded where they are used
+        Entries f{};
+        load_entries(ir, xr, t0, c, f);
+        scatter_chunk(f, c, T - t0, rest);
+      }
+    };
+
+    // token-level set: the tile's part of the mask and the set tokens before it
+    uint32_t set_mask = 0, set_rank = 0;
+    auto load_mask = [&](int t0, uint32_t& mw, uint32_t& rank) __attribute__((always_inline)) {
+      mw = 0;
+      rank = 0;
+      if (t0 >= T) return;
+      const int w = t0 >> 5;
+      rank = counts[t0 >> 7];
+      for (int i = w & ~3; i < w; ++i) rank += (uint32_t)__builtin_popcount(mask_words[i]);
+      mw = mask_words[w];
+      if constexpr (TOK == 16) {
+        if (t0 & 16) {
+          rank += (uint32_t)__builtin_popcount(mw & 0xFFFFu);
+          mw >>= 16;
+        } else {
+          mw &= 0xFFFFu;
+        }
+      }
+      if (T - t0 < TOK) mw &= (1u << (T - t0)) - 1u;
+    };
+    constexpr int HB = 16 / S::E * C;  // stored bytes of a 16-byte LDS piece
+    struct SetRows {
+      uint4 x[3];
+    };
+    SetRows sk{}, sv{};
+    // rows `from` .. of the tile's set tokens, RPL of them: the lane's piece
+    auto load_rows = [&](const __amdgpu_buffer_rsrc_t& r, uint32_t mw, uint32_t rank, int from, SetRows& x) __attribute__((always_inline)) {
+      const uint32_t row = rank + (uint32_t)(from + lane / NP);
+      const bool ok = from + lane / NP < __builtin_popcount(mw);
+#pragma unroll
+      for (int f = 0; f < 3; ++f) {
+        if (f > 0 && !q4) continue;
+        const uint32_t off = ok ? (row * (uint32_t)(nb - 1) + f) * (uint32_t)(D * C) + (uint32_t)(lane % NP) * HB : kOob;
+        if constexpr (HB == 8) {
+          const uint2 a = ld64(r, off);
+          x.x[f] = make_uint4(a.x, a.y, 0, 0);
+        } else {
+          x.x[f] = ld128<0>(r, off);
+        }
+      }
+    };
+    auto put_rows = [&](const SetRows& x, uint32_t mw, int from, bool rest) __attribute__((always_inline)) {
+      // token of the lane's row: the (from + lane / NP)-th set bit
+      uint32_t b = mw;
+      for (int i = 0; i < from; ++i) b &= b - 1;
+      int t = 0;
+      bool ok = false;
+#pragma unroll
+      for (int i = 0; i < RPL; ++i) {
+        if (lane / NP == i) {
+          ok = b != 0;
+          t = __builtin_ctz(b | 0x80000000u);
+        }
+        b &= b - 1;
+      }
+      if (!ok) return;
+      uint32_t ow[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) {
+          float y = w1 * as_f32(word(x.x[0], i));
+          if (q4) y = fmaf(w3, as_f32(word(x.x[2], i)), fmaf(w2, as_f32(word(x.x[1], i)), y));
+          ow[i] = as_u32(y);
+        } else {
+          auto pair = [&](const uint4& v) __attribute__((always_inline)) -> uint32_t {
+            if constexpr (C8) return (i & 1) ? e4m3x2_bf16<true>(word(v, i / 2)) : e4m3x2_bf16<false>(word(v, i / 2));
+            return word(v, i);
+          };
+          const uint32_t a = pair(x.x[0]);
+          float y0 = w1 * bf16_lo(a), y1 = w1 * bf16_hi(a);
+          if (q4) {
+            const uint32_t bb = pair(x.x[1]), cc = pair(x.x[2]);
+            y0 = fmaf(w3, bf16_lo(cc), fmaf(w2, bf16_lo(bb), y0));
+            y1 = fmaf(w3, bf16_hi(cc), fmaf(w2, bf16_hi(bb), y1));
+          }
+          const uint32_t hi = cvt_bf16x2(y0, y1);
+          ow[i] = rest ? cvt_bf16x2(y0 - bf16_lo(hi), y1 - bf16_hi(hi)) : hi;
+        }
+      }
+      *reinterpret_cast<uint4*>(rt + piece_at<D, TY>(t, lane % NP)) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
+    };
+    auto set_rows = [&](const __amdgpu_buffer_rsrc_t& r, const SetRows& x, bool rest) __attribute__((always_inline)) {
+      const int ns = __builtin_popcount(set_mask);
+      put_rows(x, set_mask, 0, rest);
+      for (int from = RPL; from < ns; from += RPL) {
+        SetRows y{};
+        load_rows(r, set_mask, set_rank, from, y);
+        put_rows(y, set_mask, from, rest);
+      }
+    };
+    auto clear_r = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) *reinterpret_cast<uint4*>(rt + i * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+    };
+
+    // ---- products
+    f32x4_t s[NQ][TI];
+    auto qk_piece = [&](const uint4& a, int i, int kk) __attribute__((always_inline)) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+            s[q][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(as_f32(word(a, j)), as_f32(word(qf[q][kk], j)), s[q][i], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+          s[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                            __builtin_bit_cast(bf16x8_t, qf[q][kk]), s[q][i], 0, 0, 0);
+      }
+    };
+    auto qk_residual = [&]() __attribute__((always_inline)) {
+      lds_fence();
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+          qk_piece(*reinterpret_cast<const uint4*>(rt + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, i) + (lc & 3), 4 * kk + lg)), i, kk);
+      lds_fence();
+    };
+    // probabilities of the lane's tokens: bf16 operand words, or fp32
+    uint32_t pb[NQ][4];
+    auto pv = [&](const uint8_t* tile) __attribute__((always_inline)) {
+      lds_fence();
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int ch = 16 * c + lc;
+            const float a = *reinterpret_cast<const float*>(tile + piece_at<D, TY>(4 * lg + i, ch / 4) + (ch & 3) * 4);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q)
+              acc[q][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, as_f32(pb[q][i]), acc[q][c], 0, 0, 0);
+          }
+        } else {
+          // rows quad .. quad + 3 of both operands, channels 16 c ..: lane i of a group names row i / 4, channels 4 (i % 4) ..
+          i16x4_t h[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint8_t* at = tile + piece_at<D, TY>(quad_row<D, TY>(lg, i) + (lc >> 2), 2 * c + ((lc & 3) >> 1)) + (lc & 1) * 8;
+            h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)at);
+          }
+          const i16x8_t a = {h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]};
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+            acc[q][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, make_uint4(pb[q][0], pb[q][1], pb[q][2], pb[q][3])),
+                acc[q][c], 0, 0, 0);
+        }
+      }
+      lds_fence();
+    };
+
+    if constexpr (RES != 0) clear_r();
+    int t0 = tile_token(0);
+    load_tile(kr, t0, k_off, kv, true);
+    load_tile(vr, t0, v_off, vv, false);
+    if constexpr (RES == 1) {
+      load_entries(ikr, xkr, t0, lane, ek);
+      load_entries(ivr, xvr, t0, lane, ev);
+    }
+    if constexpr (RES == 2) {
+      load_mask(t0, set_mask, set_rank);
+      load_rows(hkr, set_mask, set_rank, 0, sk);
+      load_rows(hvr, set_mask, set_rank, 0, sv);
+    }
+
+#pragma unroll 1
+    for (int it = 0; it < n; ++it) {
+      const int tn = tile_token(it + 1);
+      uint32_t next_mask = 0, next_rank = 0;
+      if constexpr (RES == 2) load_mask(tn, next_mask, next_rank);
+      const bool has = RES == 1 || (RES == 2 && set_mask != 0);
+
+      // K
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int i = 0; i < TI; ++i) s[q][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          uint4 a;
+          if constexpr (C8)
+            a = i ? widen8(kv[kk].z, kv[kk].w) : widen8(kv[kk].x, kv[kk].y);
+          else
+            a = kv[i * KK + kk];
+          qk_piece(a, i, kk);
+        }
+      load_tile(kr, tn, k_off, kv, true);
+      if (has) {
+        if constexpr (RES == 1) scatter(ikr, xkr, t0, ek, false);
+        if constexpr (RES == 2) set_rows(hkr, sk, false);
+        qk_residual();
+        if (!F32 && q4) {
+          if constexpr (RES == 1) scatter(ikr, xkr, t0, ek, true);
+          if constexpr (RES == 2) set_rows(hkr, sk, true);
+          qk_residual();
+        }
+        clear_r();
+        lds_fence();
+        if constexpr (RES == 1) scatter(ivr, xvr, t0, ev, false);
+        if constexpr (RES == 2) set_rows(hvr, sv, false);
+      }
+      if constexpr (RES == 1) {
+        load_entries(ikr, xkr, tn, lane, ek);
+        load_entries(ivr, xvr, tn, lane, ev);
+      }
+      if constexpr (RES == 2) {
+        load_rows(hkr, next_mask, next_rank, 0, sk);
+        load_rows(hvr, next_mask, next_rank, 0, sv);
+      }
+
+      // V into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        if constexpr (C8) {
+          constexpr int half = kC8Block / D / 2;
+          const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
+          uint4 a = widen8(vv[i].x, vv[i].y), b = widen8(vv[i].z, vv[i].w);
+          if (t0 + TOK > T) {
+            if (t0 + row >= T) a = make_uint4(0, 0, 0, 0);
+            if (t0 + row + half >= T) b = make_uint4(0, 0, 0, 0);
+          }
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = a;
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = b;
+        } else {
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = vv[i];
+        }
+      }
+      load_tile(vr, tn, v_off, vv, false);
+
+      // softmax
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float z = s[q][i][r] * P.scale_log2;
+            if (t0 + TOK > T && t0 + quad_row<D, TY>(lg, i) + r >= T) z = -INFINITY;
+            s[q][i][r] = z;
+            mx = fmaxf(mx, z);
+          }
+        mx = col_max(mx);
+        if (__any(mx > m[q] + kSlack)) {
+          const float mn = fmaxf(m[q], mx);
+          const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
+          m[q] = mn;
+          l[q] *= f;
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[q][c][r] *= f;
+        }
+        const float ref = m[q] == -INFINITY ? 0.f : m[q];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+          float p[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            p[r] = __builtin_amdgcn_exp2f(s[q][i][r] - ref);
+            sum += p[r];
+          }
+          if constexpr (F32) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pb[q][r] = as_u32(p[r]);
+          } else {
+            pb[q][2 * i] = cvt_bf16x2(p[0], p[1]);
+            pb[q][2 * i + 1] = cvt_bf16x2(p[2], p[3]);
+          }
+        }
+        l[q] += sum;
+      }
+
+      // V
+      pv(vt);
+      if (has) {
+        pv(rt);
+        clear_r();
+        lds_fence();
+      }
+      set_mask = next_mask;
+      set_rank = next_rank;
+      t0 = tn;
+    }
+  };
+
+  using std::integral_constant;
+  auto by_res = [&](auto c8_tag) __attribute__((always_inline)) {
+    if (mode == kResidual && P.tokres)
+      walk(c8_tag, integral_constant<int, 2>{});
+    else if (mode == kResidual && P.topk > 0)
+      walk(c8_tag, integral_constant<int, 1>{});
+    else
+      walk(c8_tag, integral_constant<int, 0>{});
+  };
+  if (n > 0) {
+    if constexpr (TY == kTyC8) {
+      if (mode == kExact)
+        walk(integral_constant<bool, false>{}, integral_constant<int, 0>{});
+      else
+        by_res(integral_constant<bool, true>{});
+    } else {
+      by_res(integral_constant<bool, false>{});
+    }
+  }
+
+  // ---- the waves' records of a column tile meet in LDS, one tile after the other
+  float* mg = reinterpret_cast<float*>(lds);  // [wave][column][MP]
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    if (P.shared && row0 + 16 * q >= rows) break;
+    __syncthreads();
+    const float ls = col_sum(l[q]);
+    if (lg == 0) {
+      ml_lds[wave][lc][0] = m[q];
+      ml_lds[wave][lc][1] = ls;
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      *reinterpret_cast<f32x4_t*>(mg + (wave * 16 + lc) * MP + 16 * c + 4 * lg) = acc[q][c];
+    __syncthreads();
+    const int col = threadIdx.x >> 4, part16 = threadIdx.x & 15;  // 16 threads a column
+    int sq, g;
+    if (row_of(16 * q + col, sq, g)) {
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, ml_lds[w][col][0]);
+      float wt[4], lt = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        wt[w] = merge_weight(ml_lds[w][col][0], M);
+        lt = fmaf(wt[w], ml_lds[w][col][1], lt);
+      }
+      float* rec = P.ws + ((((uint64_t)sq * hkv + head) * P.n_slots_total + slot) * G + g) * RS;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const int ch = 64 * c + 4 * part16;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) o += wt[w] * *reinterpret_cast<const f32x4_t*>(mg + (w * 16 + col) * MP + ch);
+        if (bad_unit) o = f32x4_t{NAN, NAN, NAN, NAN};
+        *reinterpret_cast<f32x4_t*>(rec + ch) = o;
+      }
+      if (part16 == 0) {
+        rec[D] = bad_unit ? 0.f : M;
+        rec[D + 1] = bad_unit ? 1.f : lt;
+      }
+    }
+  }
+}
+
+template <int D, int TY>
+static hipError_t launch_parts_ty(const PartsParams& P, hipStream_t s) {
+  const uint32_t items = (uint32_t)P.hkv * P.n_slots;
+  const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
+  if (P.nq == 1)
+    hipLaunchKernelGGL((parts_kernel<D, 1, TY>), grid, block, 0, s, P);
+  else if (P.nq == 2)
+    hipLaunchKernelGGL((parts_kernel<D, 2, TY>), grid, block, 0, s, P);
+  else
+    hipLaunchKernelGGL((parts_kernel<D, 4, TY>), grid, block, 0, s, P);
+  return hipGetLastError();
+}
+
+}  // namespace fdkv

@@ -1,0 +1,6 @@
+// Decode over parts: kernels of one cache type and head dimension (parts.h).
+#include "parts.h"
+
+namespace fdkv {
+hipError_t launch_parts_bf16_d64(const PartsParams& P, hipStream_t s) { return launch_parts_ty<64, parts::kTyBf16>(P, s); }
+}  // namespace fdkv
