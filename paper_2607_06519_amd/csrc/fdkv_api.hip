@@ -934,7 +934,7 @@ struct PartsPlan {
   int64_t own_slots, total_slots;
 };
 
-// Workgroups that fill the card: two of up to 32 query rows to a CU, or one of 64.
+// Workgroups that fill the card: two of up to 16 query rows to a CU, or one of more.
 constexpr int64_t kPartsWorkgroups = 512;
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
@@ -974,9 +974,11 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
   p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 256);
   p.rows = (int)(batch * G);
-  p.nq = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
+  // (more than eight entries a lane and 64 columns do not fit the registers together)
+  const bool many = dims->residual == FDKV_RES_CHANNELS && tok / 8 * dims->topk > 64;
+  p.nq = p.rows <= 16 ? 1 : p.rows <= 32 || many ? 2 : 4;
   p.row_groups = (p.rows + 16 * p.nq - 1) / (16 * p.nq);
-  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (p.nq == 4 ? 2 : 1) / (hkv * p.row_groups), 1 << 28);
+  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (p.nq > 1 ? 2 : 1) / (hkv * p.row_groups), 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {

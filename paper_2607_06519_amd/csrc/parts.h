@@ -144,8 +144,15 @@ struct Entries {
 
 }  // namespace parts
 
-template <int D, int NQ, int TY>
-__global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams P) {
+// Residual kinds of a launch: up to eight entries a lane and tile, more, a token-level set.
+enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
+
+// Workgroups to a CU that the registers have to leave room for.  A spill in the
+// walk would wait for every load in flight.
+constexpr int parts_per_cu(int NQ, int KIND, bool q4) { return NQ == 1 && !(KIND == kManyEntries && q4) ? 2 : 1; }
+
+template <int D, int NQ, int TY, int KIND, bool q4>
+__global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(PartsParams P) {
   using namespace parts;
   using S = TileOf<D, TY>;
   constexpr bool F32 = S::F32;
@@ -154,7 +161,9 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
   constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
   constexpr int kWaveLds = 2 * S::TILE_BYTES;
   static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kWaveLds];
+  // the queries of 64 columns stay in LDS (registers would not hold them besides the sums)
+  constexpr bool QL = NQ == 4;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kWaveLds + (QL ? 16 * NQ * RB : 0)];
   __shared__ float ml_lds[4][16][2];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, lane = threadIdx.x & 63;
@@ -222,8 +231,22 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     g = P.shared ? r & (G - 1) : r;
     return r < rows;
   };
-  uint4 qf[NQ][KK];
-  {
+  // piece of a column's query in LDS, permuted by the column against bank conflicts
+  auto q_at = [&](int q, int col, int piece) __attribute__((always_inline)) {
+    const int f = NP == 8 ? col >> 1 : col;
+    return lds + 4 * kWaveLds + (16 * q + col) * RB + ((piece ^ f) << 4);
+  };
+  uint4 qf[QL ? 1 : NQ][QL ? 1 : KK];
+  if constexpr (QL) {
+    for (int i = threadIdx.x; i < 16 * NQ * NP; i += 256) {
+      const int col = i / NP, piece = i % NP;
+      int s, g;
+      const bool ok = row_of(col, s, g);
+      const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
+      *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, piece)) = ok ? src[piece] : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+  } else {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       int s, g;
@@ -233,6 +256,12 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
       for (int kk = 0; kk < KK; ++kk) qf[q][kk] = ok ? src[4 * kk + lg] : make_uint4(0, 0, 0, 0);
     }
   }
+  auto query = [&](int q, int kk) __attribute__((always_inline)) -> uint4 {
+    if constexpr (QL)
+      return *reinterpret_cast<const uint4*>(q_at(q, lc, 4 * kk + lg));
+    else
+      return qf[q][kk];
+  };
 
   float m[NQ], l[NQ];
   f32x4_t acc[NQ][CT];
@@ -248,14 +277,19 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
   uint8_t* rt = vt + S::TILE_BYTES;                    // R
   const uint8_t* seg = pt.cache + seg_off;
 
-  // RES: 0 none, 1 per-token entries, 2 a token-level set
+  // The walk is compiled for each kind of unit, so that every load of a tile is
+  // issued unconditionally (a tile that the wave has not takes the out-of-range
+  // offset) and the compiler can wait for exactly the loads it needs: with the
+  // block size and the entries a lane decided at run time a residual unit's tile
+  // took 11 us instead of TODO.
   auto walk = [&](auto c8_tag, auto res_tag) __attribute__((always_inline)) {
     constexpr bool C8 = decltype(c8_tag)::value;       // shared planes and residual values in E4M3
-    constexpr int RES = decltype(res_tag)::value;
+    constexpr int RES = decltype(res_tag)::value ? KIND : 0;
+    constexpr bool ENT = RES == kFewEntries || RES == kManyEntries, SET = RES == kTokenSet;
+    constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
     const int nb = P.bsize, k = P.topk;
-    const bool q4 = nb == 4;
     const float w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2];
 
     // ---- planes
@@ -270,7 +304,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     }
     const auto kr = rsrc(kb, dense), vr = rsrc(vb, dense);
     // residual entries
-    const uint32_t ib = RES == 1 ? (uint32_t)T * k * (q4 ? 2 : 1) : 0, xb = RES == 1 ? (uint32_t)T * k * C : 0;
+    const uint32_t ib = ENT ? (uint32_t)T * k * (q4 ? 2 : 1) : 0, xb = ENT ? (uint32_t)T * k * C : 0;
     const uint32_t ip = (ib + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign, xp = (xb + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign;
     const uint8_t* ent = seg + 2 * (uint64_t)plane;
     // (whole 16-byte pieces: a load whose last word lies half behind the bytes would read 0 for all of it.  The
@@ -281,7 +315,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     // token-level set
     TokLayout L{};
     uint64_t set_bytes = 0;
-    if constexpr (RES == 2) {
+    if constexpr (SET) {
       const int ppm = unit_ppm(P.res_ppm, P.n_rates, P.rates_ppm, mbyte);
       L = tok_layout(mode, (uint64_t)T, D, ppm, S::E, C, nb);
       set_bytes = residual_token_count((uint64_t)T, ppm) * (uint64_t)(nb - 1) * D * C;
@@ -335,7 +369,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     }
     const uint32_t v_off = (uint32_t)lane * 16;
 
-    Entries ek{}, ev{};
+    Entries ek[NCH], ev[NCH];
     auto load_entries = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, int chunk, Entries& e) __attribute__((always_inline)) {
       const uint32_t e0 = (uint32_t)t0 * k + 8u * (uint32_t)chunk;
       const bool ok = t0 < T && chunk < TOK / 8 * k;
@@ -347,10 +381,10 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
         e.v0 = ld128<0>(xr, vo);
         if constexpr (C == 4) e.v1 = ld128<0>(xr, vo + 16);
       }
-      if (q4) {
+      if constexpr (q4) {
         const uint32_t io = ok ? e0 * 2 : kOob;
         e.ix = ld128<0>(ir, io);
-        e.prev = ok && e0 > 0 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(ir, io - 2, 0, 0) : 0u;
+        e.prev = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(ir, ok && e0 > 0 ? io - 2 : kOob, 0, 0);
         e.nix = __builtin_amdgcn_raw_buffer_load_b32(ir, io + 16, 0, 0);
         if constexpr (C == 1) {
           e.nv0 = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(xr, vo + 8, 0, 0);
@@ -397,7 +431,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
       if (chunk >= TOK / 8 * k) return;
       const int e0 = 8 * chunk;
       int t = (int)P.by_topk.div((uint32_t)e0), j = e0 - t * k;  // token of the tile, entry of the token
-      if (!q4) {
+      if constexpr (!q4) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (t < held) put(t, (int)((word(e.ix, i / 4) >> (8 * (i & 3))) & (D - 1)), w1 * value(e, i), false);
@@ -432,12 +466,22 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
         }
       }
     };
-    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, const Entries& e, bool rest) __attribute__((always_inline)) {
-      scatter_chunk(e, lane, T - t0, rest);
-      for (int c = lane + 64; c < TOK / 8 * k; c += 64) {  // more than eight entries a lane: loaded where they are used
-        Entries f{};
-        load_entries(ir, xr, t0, c, f);
-        scatter_chunk(f, c, T - t0, rest);
+    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, const Entries (&e)[NCH], bool rest) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) scatter_chunk(e[i], lane + 64 * i, T - t0, rest);
+      if constexpr (RES == kManyEntries) {
+        for (int c = lane + 64 * NCH; c < TOK / 8 * k; c += 64) {
+          Entries f;
+          load_entries(ir, xr, t0, c, f);
+          scatter_chunk(f, c, T - t0, rest);
+        }
+      }
+    };
+    auto load_all = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        load_entries(ikr, xkr, t0, lane + 64 * i, ek[i]);
+        load_entries(ivr, xvr, t0, lane + 64 * i, ev[i]);
       }
     };
 
@@ -472,7 +516,9 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
       const bool ok = from + lane / NP < __builtin_popcount(mw);
 #pragma unroll
       for (int f = 0; f < 3; ++f) {
-        if (f > 0 && !q4) continue;
+        if constexpr (!q4) {
+          if (f > 0) break;
+        }
         const uint32_t off = ok ? (row * (uint32_t)(nb - 1) + f) * (uint32_t)(D * C) + (uint32_t)(lane % NP) * HB : kOob;
         if constexpr (HB == 8) {
           const uint2 a = ld64(r, off);
@@ -502,7 +548,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
       for (int i = 0; i < 4; ++i) {
         if constexpr (F32) {
           float y = w1 * as_f32(word(x.x[0], i));
-          if (q4) y = fmaf(w3, as_f32(word(x.x[2], i)), fmaf(w2, as_f32(word(x.x[1], i)), y));
+          if constexpr (q4) y = fmaf(w3, as_f32(word(x.x[2], i)), fmaf(w2, as_f32(word(x.x[1], i)), y));
           ow[i] = as_u32(y);
         } else {
           auto pair = [&](const uint4& v) __attribute__((always_inline)) -> uint32_t {
@@ -511,7 +557,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
           };
           const uint32_t a = pair(x.x[0]);
           float y0 = w1 * bf16_lo(a), y1 = w1 * bf16_hi(a);
-          if (q4) {
+          if constexpr (q4) {
             const uint32_t bb = pair(x.x[1]), cc = pair(x.x[2]);
             y0 = fmaf(w3, bf16_lo(cc), fmaf(w2, bf16_lo(bb), y0));
             y1 = fmaf(w3, bf16_hi(cc), fmaf(w2, bf16_hi(bb), y1));
@@ -538,27 +584,36 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
 
     // ---- products
     f32x4_t s[NQ][TI];
-    auto qk_piece = [&](const uint4& a, int i, int kk) __attribute__((always_inline)) {
+    auto qk_piece = [&](const uint4& a, const uint4& b, int q, int i) __attribute__((always_inline)) {
       if constexpr (F32) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int q = 0; q < NQ; ++q)
-            s[q][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(as_f32(word(a, j)), as_f32(word(qf[q][kk], j)), s[q][i], 0, 0, 0);
+          s[q][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(as_f32(word(a, j)), as_f32(word(b, j)), s[q][i], 0, 0, 0);
       } else {
+        s[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
+                                                          s[q][i], 0, 0, 0);
+      }
+    };
+    // piece(i, kk): the A operand of 16 tokens and the kk-th channels
+    auto qk = [&](auto piece) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q)
-          s[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
-                                                            __builtin_bit_cast(bf16x8_t, qf[q][kk]), s[q][i], 0, 0, 0);
+      for (int kk = 0; kk < KK; ++kk) {
+        uint4 a[TI];
+#pragma unroll
+        for (int i = 0; i < TI; ++i) a[i] = piece(i, kk);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          const uint4 b = query(q, kk);
+#pragma unroll
+          for (int i = 0; i < TI; ++i) qk_piece(a[i], b, q, i);
+        }
       }
     };
     auto qk_residual = [&]() __attribute__((always_inline)) {
       lds_fence();
-#pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-          qk_piece(*reinterpret_cast<const uint4*>(rt + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, i) + (lc & 3), 4 * kk + lg)), i, kk);
+      qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
+        return *reinterpret_cast<const uint4*>(rt + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, i) + (lc & 3), 4 * kk + lg));
+      });
       lds_fence();
     };
     // probabilities of the lane's tokens: bf16 operand words, or fp32
@@ -599,11 +654,8 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     int t0 = tile_token(0);
     load_tile(kr, t0, k_off, kv, true);
     load_tile(vr, t0, v_off, vv, false);
-    if constexpr (RES == 1) {
-      load_entries(ikr, xkr, t0, lane, ek);
-      load_entries(ivr, xvr, t0, lane, ev);
-    }
-    if constexpr (RES == 2) {
+    if constexpr (ENT) load_all(t0);
+    if constexpr (SET) {
       load_mask(t0, set_mask, set_rank);
       load_rows(hkr, set_mask, set_rank, 0, sk);
       load_rows(hvr, set_mask, set_rank, 0, sv);
@@ -613,45 +665,37 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
     for (int it = 0; it < n; ++it) {
       const int tn = tile_token(it + 1);
       uint32_t next_mask = 0, next_rank = 0;
-      if constexpr (RES == 2) load_mask(tn, next_mask, next_rank);
-      const bool has = RES == 1 || (RES == 2 && set_mask != 0);
+      if constexpr (SET) load_mask(tn, next_mask, next_rank);
+      const bool has = ENT || (SET && set_mask != 0);
 
       // K
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int i = 0; i < TI; ++i) s[q][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          uint4 a;
-          if constexpr (C8)
-            a = i ? widen8(kv[kk].z, kv[kk].w) : widen8(kv[kk].x, kv[kk].y);
-          else
-            a = kv[i * KK + kk];
-          qk_piece(a, i, kk);
-        }
+      qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
+        if constexpr (C8)
+          return i ? widen8(kv[kk].z, kv[kk].w) : widen8(kv[kk].x, kv[kk].y);
+        else
+          return kv[i * KK + kk];
+      });
       load_tile(kr, tn, k_off, kv, true);
       if (has) {
-        if constexpr (RES == 1) scatter(ikr, xkr, t0, ek, false);
-        if constexpr (RES == 2) set_rows(hkr, sk, false);
+        if constexpr (ENT) scatter(ikr, xkr, t0, ek, false);
+        if constexpr (SET) set_rows(hkr, sk, false);
         qk_residual();
-        if (!F32 && q4) {
-          if constexpr (RES == 1) scatter(ikr, xkr, t0, ek, true);
-          if constexpr (RES == 2) set_rows(hkr, sk, true);
+        if constexpr (!F32 && q4) {
+          if constexpr (ENT) scatter(ikr, xkr, t0, ek, true);
+          if constexpr (SET) set_rows(hkr, sk, true);
           qk_residual();
         }
         clear_r();
         lds_fence();
-        if constexpr (RES == 1) scatter(ivr, xvr, t0, ev, false);
-        if constexpr (RES == 2) set_rows(hvr, sv, false);
+        if constexpr (ENT) scatter(ivr, xvr, t0, ev, false);
+        if constexpr (SET) set_rows(hvr, sv, false);
       }
-      if constexpr (RES == 1) {
-        load_entries(ikr, xkr, tn, lane, ek);
-        load_entries(ivr, xvr, tn, lane, ev);
-      }
-      if constexpr (RES == 2) {
+      if constexpr (ENT) load_all(tn);
+      if constexpr (SET) {
         load_rows(hkr, next_mask, next_rank, 0, sk);
         load_rows(hvr, next_mask, next_rank, 0, sv);
       }
@@ -734,22 +778,22 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
   };
 
   using std::integral_constant;
-  auto by_res = [&](auto c8_tag) __attribute__((always_inline)) {
-    if (mode == kResidual && P.tokres)
-      walk(c8_tag, integral_constant<int, 2>{});
-    else if (mode == kResidual && P.topk > 0)
-      walk(c8_tag, integral_constant<int, 1>{});
-    else
-      walk(c8_tag, integral_constant<int, 0>{});
-  };
+  using no = integral_constant<bool, false>;
+  using yes = integral_constant<bool, true>;
+  const bool res = mode == kResidual && (KIND == kTokenSet || P.topk > 0);
   if (n > 0) {
     if constexpr (TY == kTyC8) {
       if (mode == kExact)
-        walk(integral_constant<bool, false>{}, integral_constant<int, 0>{});
+        walk(no{}, no{});
+      else if (res)
+        walk(yes{}, yes{});
       else
-        by_res(integral_constant<bool, true>{});
+        walk(yes{}, no{});
     } else {
-      by_res(integral_constant<bool, false>{});
+      if (res)
+        walk(no{}, yes{});
+      else
+        walk(no{}, no{});
     }
   }
 
@@ -798,17 +842,27 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void parts_kernel(PartsParams
   }
 }
 
-template <int D, int TY>
-static hipError_t launch_parts_ty(const PartsParams& P, hipStream_t s) {
+template <int D, int TY, int KIND, bool q4>
+static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
   const uint32_t items = (uint32_t)P.hkv * P.n_slots;
   const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
   if (P.nq == 1)
-    hipLaunchKernelGGL((parts_kernel<D, 1, TY>), grid, block, 0, s, P);
+    hipLaunchKernelGGL((parts_kernel<D, 1, TY, KIND, q4>), grid, block, 0, s, P);
   else if (P.nq == 2)
-    hipLaunchKernelGGL((parts_kernel<D, 2, TY>), grid, block, 0, s, P);
+    hipLaunchKernelGGL((parts_kernel<D, 2, TY, KIND, q4>), grid, block, 0, s, P);
   else
-    hipLaunchKernelGGL((parts_kernel<D, 4, TY>), grid, block, 0, s, P);
+    hipLaunchKernelGGL((parts_kernel<D, 4, TY, KIND, q4>), grid, block, 0, s, P);
   return hipGetLastError();
+}
+
+template <int D, int TY>
+static hipError_t launch_parts_ty(const PartsParams& P, hipStream_t s) {
+  const bool quad = P.bsize == 4;
+  if (P.tokres)
+    return quad ? launch_parts_kind<D, TY, kTokenSet, true>(P, s) : launch_parts_kind<D, TY, kTokenSet, false>(P, s);
+  if (parts::TileOf<D, TY>::TOK / 8 * P.topk <= 64)
+    return quad ? launch_parts_kind<D, TY, kFewEntries, true>(P, s) : launch_parts_kind<D, TY, kFewEntries, false>(P, s);
+  return quad ? launch_parts_kind<D, TY, kManyEntries, true>(P, s) : launch_parts_kind<D, TY, kManyEntries, false>(P, s);
 }
 
 }  // namespace fdkv
