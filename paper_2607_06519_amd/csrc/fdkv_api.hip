@@ -974,8 +974,8 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
   p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 256);
   p.rows = (int)(batch * G);
-  // (more than eight entries a lane and 64 columns do not fit the registers together)
-  const bool many = dims->residual == FDKV_RES_CHANNELS && tok / 8 * dims->topk > 64;
+  // (the kernels of many entries and 64 columns do not fit the registers together)
+  const bool many = dims->residual == FDKV_RES_CHANNELS && (dims->topk % 8 || tok / 8 * dims->topk > 64);
   p.nq = p.rows <= 16 ? 1 : p.rows <= 32 || many ? 2 : 4;
   p.row_groups = (p.rows + 16 * p.nq - 1) / (16 * p.nq);
   p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (p.nq > 1 ? 2 : 1) / (hkv * p.row_groups), 1 << 28);

@@ -144,7 +144,8 @@ struct Entries {
 
 }  // namespace parts
 
-// Residual kinds of a launch: up to eight entries a lane and tile, more, a token-level set.
+// Residual kinds of a launch: up to eight entries a lane and tile, eight at a time of one token (k a multiple of
+// eight); any other number of entries; a token-level set.
 enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
 
 // Workgroups to a CU that the registers have to leave room for.  A spill in the
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
   constexpr int RS = D + 4;
   constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
-  constexpr int kWaveLds = 2 * S::TILE_BYTES;
+  constexpr int kWaveLds = 2 * S::TILE_BYTES + RB;  // the V tile, R, and a row of R that takes what has no place
   static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
   // the queries of 64 columns stay in LDS (registers would not hold them besides the sums)
   constexpr bool QL = NQ == 4;
@@ -417,63 +418,106 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       const uint32_t w = i < 8 ? word(e.ix, i / 2) : e.nix;
       return (i & 1) ? w >> 16 : w & 0xFFFFu;
     };
-    auto put = [&](int t, int c, float x, bool rest) __attribute__((always_inline)) {
-      const uint32_t at = piece_at<D, TY>(t, c / (16 / S::E)) + (uint32_t)(c % (16 / S::E)) * S::E;
-      if constexpr (F32) {
-        *reinterpret_cast<float*>(rt + at) = x;
-      } else {
-        const uint32_t hi = f32_to_bf16_bits(x);
-        *reinterpret_cast<uint16_t*>(rt + at) = (uint16_t)(rest ? f32_to_bf16_bits(x - bf16_to_f32((uint16_t)hi)) : hi);
-      }
+    // Where the chunk's entries go in R and what goes there.  No branch: an entry that has no place (of a token
+    // behind the last, of a chunk behind the tile, or summed into its channel's first) goes to the row behind R, so
+    // that the products of the rest of the tile can fill the waits.
+    struct Placed {
+      uint32_t at[8];
+      float x[8];       // blocks of four, fp32
+      uint32_t w[4];    // pairs in bf16: the stored values with the layer's sign, two a word
     };
-    // The chunk's entries into R; rest: what their bf16 rounding leaves.
-    auto scatter_chunk = [&](const Entries& e, int chunk, int held, bool rest) __attribute__((always_inline)) {  // held: tokens of the tile
-      if (chunk >= TOK / 8 * k) return;
+    auto place = [&](const Entries& e, int chunk, int held, Placed& p) __attribute__((always_inline)) {  // held: tokens of the tile
+      const bool live = chunk < TOK / 8 * k;
       const int e0 = 8 * chunk;
       int t = (int)P.by_topk.div((uint32_t)e0), j = e0 - t * k;  // token of the tile, entry of the token
-      if constexpr (!q4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (t < held) put(t, (int)((word(e.ix, i / 4) >> (8 * (i & 3))) & (D - 1)), w1 * value(e, i), false);
-          if (++j == k) {
-            j = 0;
-            ++t;
-          }
-        }
-        return;
-      }
-      // a channel's up to three frequencies are neighbours (codes 4 c + j ascend): the first of them adds up
-      auto weighted = [&](int i) __attribute__((always_inline)) -> float {
-        const uint32_t f = code(e, i) & 3u;
-        const float a = w1, b = w2, c = w3;  // (values: a choice among captured variables would keep them in memory)
-        return (f == 1 ? +a : f == 2 ? +b : +c) * value(e, i);
-      };
+      uint32_t base[8], perm[8];  // of an entry's row: its first byte, the permutation of its channels
+      bool starts[10];            // the entry is its token's first
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t c = code(e, i) >> 2;
-        const uint32_t before = (i ? code(e, i - 1) : e.prev) >> 2;
-        if (t < held && (j == 0 || before != c)) {
-          float x = weighted(i);
-          if (j + 1 < k && (code(e, i + 1) >> 2) == c) {
-            x += weighted(i + 1);
-            if (j + 2 < k && (code(e, i + 2) >> 2) == c) x += weighted(i + 2);
-          }
-          put(t, (int)(c & (D - 1)), x, rest);
+        if (RES == kFewEntries && i > 0) {  // k is a multiple of eight: a chunk is of one token
+          base[i] = base[0];
+          perm[i] = perm[0];
+          starts[i] = false;
+          continue;
         }
-        if (++j == k) {
-          j = 0;
-          ++t;
+        const int r = live && t < held ? t : TOK;
+        base[i] = (uint32_t)(r * RB);
+        perm[i] = (piece_at<D, TY>(r, 0) - base[i]) / S::E;
+        starts[i] = j == 0;
+        if constexpr (RES == kManyEntries) {
+          const bool next = ++j == k;
+          j = next ? 0 : j;
+          t += next;
+        }
+      }
+      if constexpr (RES == kFewEntries) {
+        starts[8] = j + 8 == k;
+        starts[9] = false;
+      } else {
+        starts[8] = j == 0;
+        starts[9] = j + 1 == k || k == 1;
+      }
+      if constexpr (!q4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.at[i] = base[i] + (((word(e.ix, i / 4) >> (8 * (i & 3))) & (D - 1)) ^ perm[i]) * S::E;
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p.x[i] = w1 * value(e, i);
+        } else {
+          const uint4 v = C8 ? widen8(e.v0.x, e.v0.y) : e.v0;
+          const uint32_t sign = w1 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p.w[i] = word(v, i) ^ sign;
+        }
+      } else {
+        // a channel's up to three frequencies are neighbours (codes 4 c + j ascend): the first of them takes the sum
+        float x[10];
+        const float a = w1, b = w2, c = w3;
+#pragma unroll
+        for (int i = 0; i < 10; ++i) {
+          const uint32_t f = code(e, i) & 3u;
+          const float lo = f == 1u ? a : b;
+          x[i] = (f == 3u ? c : lo) * value(e, i);
+        }
+#pragma unroll
+        for (int i = 8; i >= 0; --i) x[i] += !starts[i + 1] && (code(e, i + 1) ^ code(e, i)) < 4u ? x[i + 1] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool first = starts[i] || ((i ? code(e, i - 1) : e.prev) ^ code(e, i)) >= 4u;
+          p.at[i] = (first ? base[i] : (uint32_t)(TOK * RB)) + (((code(e, i) >> 2) & (D - 1)) ^ perm[i]) * S::E;
+          p.x[i] = x[i];
         }
       }
     };
-    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, const Entries (&e)[NCH], bool rest) __attribute__((always_inline)) {
+    // rest: what the bf16 rounding of the values leaves
+    auto store = [&](const Placed& p, bool rest) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) scatter_chunk(e[i], lane + 64 * i, T - t0, rest);
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (F32) {
+          *reinterpret_cast<float*>(rt + p.at[i]) = p.x[i];
+        } else if constexpr (!q4) {
+          *reinterpret_cast<uint16_t*>(rt + p.at[i]) = (uint16_t)((i & 1) ? p.w[i / 2] >> 16 : p.w[i / 2]);
+        } else {
+          const uint32_t hi = f32_to_bf16_bits(p.x[i]);
+          *reinterpret_cast<uint16_t*>(rt + p.at[i]) = (uint16_t)(rest ? f32_to_bf16_bits(p.x[i] - bf16_to_f32((uint16_t)hi)) : hi);
+        }
+      }
+    };
+    Placed placed[NCH];
+    auto place_all = [&](const Entries (&e)[NCH], int t0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) place(e[i], lane + 64 * i, T - t0, placed[i]);
+    };
+    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, bool rest) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) store(placed[i], rest);
       if constexpr (RES == kManyEntries) {
         for (int c = lane + 64 * NCH; c < TOK / 8 * k; c += 64) {
           Entries f;
           load_entries(ir, xr, t0, c, f);
-          scatter_chunk(f, c, T - t0, rest);
+          Placed p;
+          place(f, c, T - t0, p);
+          store(p, rest);
         }
       }
     };
@@ -681,17 +725,23 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       });
       load_tile(kr, tn, k_off, kv, true);
       if (has) {
-        if constexpr (ENT) scatter(ikr, xkr, t0, ek, false);
+        if constexpr (ENT) {
+          place_all(ek, t0);
+          scatter(ikr, xkr, t0, false);
+        }
         if constexpr (SET) set_rows(hkr, sk, false);
         qk_residual();
         if constexpr (!F32 && q4) {
-          if constexpr (ENT) scatter(ikr, xkr, t0, ek, true);
+          if constexpr (ENT) scatter(ikr, xkr, t0, true);
           if constexpr (SET) set_rows(hkr, sk, true);
           qk_residual();
         }
         clear_r();
         lds_fence();
-        if constexpr (ENT) scatter(ivr, xvr, t0, ev, false);
+        if constexpr (ENT) {
+          place_all(ev, t0);
+          scatter(ivr, xvr, t0, false);
+        }
         if constexpr (SET) set_rows(hvr, sv, false);
       }
       if constexpr (ENT) load_all(tn);
@@ -860,7 +910,7 @@ static hipError_t launch_parts_ty(const PartsParams& P, hipStream_t s) {
   const bool quad = P.bsize == 4;
   if (P.tokres)
     return quad ? launch_parts_kind<D, TY, kTokenSet, true>(P, s) : launch_parts_kind<D, TY, kTokenSet, false>(P, s);
-  if (parts::TileOf<D, TY>::TOK / 8 * P.topk <= 64)
+  if (P.topk % 8 == 0 && parts::TileOf<D, TY>::TOK / 8 * P.topk <= 64)
     return quad ? launch_parts_kind<D, TY, kFewEntries, true>(P, s) : launch_parts_kind<D, TY, kFewEntries, false>(P, s);
   return quad ? launch_parts_kind<D, TY, kManyEntries, true>(P, s) : launch_parts_kind<D, TY, kManyEntries, false>(P, s);
 }
