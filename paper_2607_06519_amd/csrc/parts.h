@@ -160,6 +160,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
   constexpr int RS = D + 4;
   constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
+  constexpr int DEPTH = NQ == 2 && KIND != kManyEntries ? 2 : 1;  // tiles in flight behind the current one
   constexpr int kWaveLds = 2 * S::TILE_BYTES + RB;  // the V tile, R, and a row of R that takes what has no place
   static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
   // the queries of 64 columns stay in LDS (registers would not hold them besides the sums)
@@ -237,6 +238,16 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     const int f = NP == 8 ? col >> 1 : col;
     return lds + 4 * kWaveLds + (16 * q + col) * RB + ((piece ^ f) << 4);
   };
+  // The scale's sign goes to the queries, so that a column's largest product is its largest logit; a scale of zero
+  // zeroes them.
+  const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
+  const uint32_t q_sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
+  const bool q_zero = P.scale_log2 == 0.f;
+  auto signed_query = [&](bool ok, const uint4* src) __attribute__((always_inline)) -> uint4 {
+    if (!ok || q_zero) return make_uint4(0, 0, 0, 0);
+    const uint4 v = *src;
+    return make_uint4(v.x ^ q_sign, v.y ^ q_sign, v.z ^ q_sign, v.w ^ q_sign);
+  };
   uint4 qf[QL ? 1 : NQ][QL ? 1 : KK];
   if constexpr (QL) {
     for (int i = threadIdx.x; i < 16 * NQ * NP; i += 256) {
@@ -244,7 +255,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       int s, g;
       const bool ok = row_of(col, s, g);
       const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
-      *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, piece)) = ok ? src[piece] : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, piece)) = signed_query(ok, src + piece);
     }
     __syncthreads();
   } else {
@@ -254,7 +265,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       const bool ok = row_of(16 * q + lc, s, g);
       const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[q][kk] = ok ? src[4 * kk + lg] : make_uint4(0, 0, 0, 0);
+      for (int kk = 0; kk < KK; ++kk) qf[q][kk] = signed_query(ok, src + 4 * kk + lg);
     }
   }
   auto query = [&](int q, int kk) __attribute__((always_inline)) -> uint4 {
@@ -345,7 +356,6 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     };
 
     // ---- loads
-    uint4 kv[NLD], vv[NLD];
     auto load_tile = [&](const __amdgpu_buffer_rsrc_t& r, int t0, uint32_t lane_off, uint4 (&x)[NLD], bool operand) {
       const uint32_t base = t0 < T ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
 #pragma unroll
@@ -370,7 +380,6 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     }
     const uint32_t v_off = (uint32_t)lane * 16;
 
-    Entries ek[NCH], ev[NCH];
     auto load_entries = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, int chunk, Entries& e) __attribute__((always_inline)) {
       const uint32_t e0 = (uint32_t)t0 * k + 8u * (uint32_t)chunk;
       const bool ok = t0 < T && chunk < TOK / 8 * k;
@@ -521,49 +530,33 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         }
       }
     };
-    auto load_all = [&](int t0) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        load_entries(ikr, xkr, t0, lane + 64 * i, ek[i]);
-        load_entries(ivr, xvr, t0, lane + 64 * i, ev[i]);
-      }
-    };
 
-    // token-level set: the tile's part of the mask and the set tokens before it
-    uint32_t set_mask = 0, set_rank = 0;
+    // token-level set: the tile's part of the mask, and the set tokens before it
     auto load_mask = [&](int t0, uint32_t& mw, uint32_t& rank) __attribute__((always_inline)) {
-      mw = 0;
-      rank = 0;
-      if (t0 >= T) return;
-      const int w = t0 >> 5;
-      rank = counts[t0 >> 7];
-      for (int i = w & ~3; i < w; ++i) rank += (uint32_t)__builtin_popcount(mask_words[i]);
-      mw = mask_words[w];
+      const int t = min(t0, T - 1), w = t >> 5;  // (one read of the chunk's four words: a mask plane is padded)
+      const auto* quad = mask_words + (w & ~3);
+      const uint32_t m0 = quad[0], m1 = quad[1], m2 = quad[2], m3 = quad[3], before = counts[t >> 7];
+      const int i = w & 3;
+      mw = i == 0 ? m0 : i == 1 ? m1 : i == 2 ? m2 : m3;
+      rank = before + (i > 0 ? __builtin_popcount(m0) : 0) + (i > 1 ? __builtin_popcount(m1) : 0) + (i > 2 ? __builtin_popcount(m2) : 0);
       if constexpr (TOK == 16) {
-        if (t0 & 16) {
-          rank += (uint32_t)__builtin_popcount(mw & 0xFFFFu);
-          mw >>= 16;
-        } else {
-          mw &= 0xFFFFu;
-        }
+        rank += t & 16 ? __builtin_popcount(mw & 0xFFFFu) : 0;
+        mw = t & 16 ? mw >> 16 : mw & 0xFFFFu;
       }
-      if (T - t0 < TOK) mw &= (1u << (T - t0)) - 1u;
+      const int held = T - t0;
+      mw = held <= 0 ? 0u : held < TOK ? mw & ((1u << held) - 1u) : mw;
     };
     constexpr int HB = 16 / S::E * C;  // stored bytes of a 16-byte LDS piece
     struct SetRows {
-      uint4 x[3];
+      uint4 x[q4 ? 3 : 1];
     };
-    SetRows sk{}, sv{};
     // rows `from` .. of the tile's set tokens, RPL of them: the lane's piece
     auto load_rows = [&](const __amdgpu_buffer_rsrc_t& r, uint32_t mw, uint32_t rank, int from, SetRows& x) __attribute__((always_inline)) {
       const uint32_t row = rank + (uint32_t)(from + lane / NP);
       const bool ok = from + lane / NP < __builtin_popcount(mw);
 #pragma unroll
-      for (int f = 0; f < 3; ++f) {
-        if constexpr (!q4) {
-          if (f > 0) break;
-        }
-        const uint32_t off = ok ? (row * (uint32_t)(nb - 1) + f) * (uint32_t)(D * C) + (uint32_t)(lane % NP) * HB : kOob;
+      for (int f = 0; f < (q4 ? 3 : 1); ++f) {
+        const uint32_t off = ok ? (row * (q4 ? 3u : 1u) + f) * (uint32_t)(D * C) + (uint32_t)(lane % NP) * HB : kOob;
         if constexpr (HB == 8) {
           const uint2 a = ld64(r, off);
           x.x[f] = make_uint4(a.x, a.y, 0, 0);
@@ -572,21 +565,16 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         }
       }
     };
-    auto put_rows = [&](const SetRows& x, uint32_t mw, int from, bool rest) __attribute__((always_inline)) {
-      // token of the lane's row: the (from + lane / NP)-th set bit
-      uint32_t b = mw;
-      for (int i = 0; i < from; ++i) b &= b - 1;
-      int t = 0;
-      bool ok = false;
+    // The rows into R: the lane's is that of the (lane / NP)-th set bit of `left`, which loses RPL bits.  A lane past
+    // the set writes to the row behind R.
+    auto put_rows = [&](const SetRows& x, uint32_t& left, bool rest) __attribute__((always_inline)) {
+      int t = TOK;
 #pragma unroll
       for (int i = 0; i < RPL; ++i) {
-        if (lane / NP == i) {
-          ok = b != 0;
-          t = __builtin_ctz(b | 0x80000000u);
-        }
-        b &= b - 1;
+        const int ti = left ? __builtin_ctz(left) : TOK;
+        t = lane / NP == i ? ti : t;
+        left &= left - 1;
       }
-      if (!ok) return;
       uint32_t ow[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -600,25 +588,26 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
             return word(v, i);
           };
           const uint32_t a = pair(x.x[0]);
-          float y0 = w1 * bf16_lo(a), y1 = w1 * bf16_hi(a);
           if constexpr (q4) {
             const uint32_t bb = pair(x.x[1]), cc = pair(x.x[2]);
-            y0 = fmaf(w3, bf16_lo(cc), fmaf(w2, bf16_lo(bb), y0));
-            y1 = fmaf(w3, bf16_hi(cc), fmaf(w2, bf16_hi(bb), y1));
+            const float y0 = fmaf(w3, bf16_lo(cc), fmaf(w2, bf16_lo(bb), w1 * bf16_lo(a)));
+            const float y1 = fmaf(w3, bf16_hi(cc), fmaf(w2, bf16_hi(bb), w1 * bf16_hi(a)));
+            const uint32_t hi = cvt_bf16x2(y0, y1);
+            ow[i] = rest ? cvt_bf16x2(y0 - bf16_lo(hi), y1 - bf16_hi(hi)) : hi;
+          } else {
+            ow[i] = a ^ (w1 < 0.f ? 0x80008000u : 0u);
           }
-          const uint32_t hi = cvt_bf16x2(y0, y1);
-          ow[i] = rest ? cvt_bf16x2(y0 - bf16_lo(hi), y1 - bf16_hi(hi)) : hi;
         }
       }
       *reinterpret_cast<uint4*>(rt + piece_at<D, TY>(t, lane % NP)) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
     };
-    auto set_rows = [&](const __amdgpu_buffer_rsrc_t& r, const SetRows& x, bool rest) __attribute__((always_inline)) {
-      const int ns = __builtin_popcount(set_mask);
-      put_rows(x, set_mask, 0, rest);
-      for (int from = RPL; from < ns; from += RPL) {
-        SetRows y{};
-        load_rows(r, set_mask, set_rank, from, y);
-        put_rows(y, set_mask, from, rest);
+    auto set_rows = [&](const __amdgpu_buffer_rsrc_t& r, const SetRows& x, uint32_t mw, uint32_t rank, bool rest) __attribute__((always_inline)) {
+      uint32_t left = mw;
+      put_rows(x, left, rest);
+      for (int from = RPL; left; from += RPL) {  // more rows than travel ahead: loaded where they are used
+        SetRows y;
+        load_rows(r, mw, rank, from, y);
+        put_rows(y, left, rest);
       }
     };
     auto clear_r = [&]() __attribute__((always_inline)) {
@@ -694,23 +683,52 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       lds_fence();
     };
 
-    if constexpr (RES != 0) clear_r();
-    int t0 = tile_token(0);
-    load_tile(kr, t0, k_off, kv, true);
-    load_tile(vr, t0, v_off, vv, false);
-    if constexpr (ENT) load_all(t0);
-    if constexpr (SET) {
-      load_mask(t0, set_mask, set_rank);
-      load_rows(hkr, set_mask, set_rank, 0, sk);
-      load_rows(hvr, set_mask, set_rank, 0, sv);
-    }
+    // ---- what travels ahead of a tile
+    struct Ahead {
+      uint4 kv[NLD], vv[NLD];
+      Entries ek[NCH], ev[NCH];
+      SetRows sk, sv;
+      uint32_t mask, rank;
+      int t0;
+    };
+    auto load_res = [&](Ahead& b) __attribute__((always_inline)) {
+      if constexpr (ENT) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+          load_entries(ikr, xkr, b.t0, lane + 64 * i, b.ek[i]);
+          load_entries(ivr, xvr, b.t0, lane + 64 * i, b.ev[i]);
+        }
+      }
+      if constexpr (SET) {
+        load_rows(hkr, b.mask, b.rank, 0, b.sk);
+        load_rows(hvr, b.mask, b.rank, 0, b.sv);
+      }
+    };
+    // Tile `it` from its buffer, which then takes tile it + DEPTH.
+    auto step = [&](Ahead& b, int it) __attribute__((always_inline)) {
+      const int t0 = b.t0, tn = tile_token(it + DEPTH);
+      const uint32_t mask = b.mask, rank = b.rank;
+      b.t0 = tn;
+      if constexpr (SET) load_mask(tn, b.mask, b.rank);
+      const bool has = ENT || (SET && mask != 0);
+      const bool edge = t0 + TOK > T;  // tokens of the tile past the last one
 
-#pragma unroll 1
-    for (int it = 0; it < n; ++it) {
-      const int tn = tile_token(it + 1);
-      uint32_t next_mask = 0, next_rank = 0;
-      if constexpr (SET) load_mask(tn, next_mask, next_rank);
-      const bool has = ENT || (SET && set_mask != 0);
+      // V into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        if constexpr (C8) {
+          constexpr int half = kC8Block / D / 2;
+          const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
+          uint4 x = widen8(b.vv[i].x, b.vv[i].y), y = widen8(b.vv[i].z, b.vv[i].w);
+          if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
+          if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = x;
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = y;
+        } else {
+          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = b.vv[i];
+        }
+      }
+      load_tile(vr, tn, v_off, b.vv, false);
 
       // K
 #pragma unroll
@@ -719,72 +737,59 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         for (int i = 0; i < TI; ++i) s[q][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
         if constexpr (C8)
-          return i ? widen8(kv[kk].z, kv[kk].w) : widen8(kv[kk].x, kv[kk].y);
+          return i ? widen8(b.kv[kk].z, b.kv[kk].w) : widen8(b.kv[kk].x, b.kv[kk].y);
         else
-          return kv[i * KK + kk];
+          return b.kv[i * KK + kk];
       });
-      load_tile(kr, tn, k_off, kv, true);
+      load_tile(kr, tn, k_off, b.kv, true);
       if (has) {
         if constexpr (ENT) {
-          place_all(ek, t0);
+          place_all(b.ek, t0);
           scatter(ikr, xkr, t0, false);
         }
-        if constexpr (SET) set_rows(hkr, sk, false);
+        if constexpr (SET) set_rows(hkr, b.sk, mask, rank, false);
         qk_residual();
         if constexpr (!F32 && q4) {
           if constexpr (ENT) scatter(ikr, xkr, t0, true);
-          if constexpr (SET) set_rows(hkr, sk, true);
+          if constexpr (SET) set_rows(hkr, b.sk, mask, rank, true);
           qk_residual();
         }
         clear_r();
         lds_fence();
         if constexpr (ENT) {
-          place_all(ev, t0);
+          place_all(b.ev, t0);
           scatter(ivr, xvr, t0, false);
         }
-        if constexpr (SET) set_rows(hvr, sv, false);
+        if constexpr (SET) set_rows(hvr, b.sv, mask, rank, false);
       }
-      if constexpr (ENT) load_all(tn);
-      if constexpr (SET) {
-        load_rows(hkr, next_mask, next_rank, 0, sk);
-        load_rows(hvr, next_mask, next_rank, 0, sv);
-      }
-
-      // V into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
-#pragma unroll
-      for (int i = 0; i < NLD; ++i) {
-        if constexpr (C8) {
-          constexpr int half = kC8Block / D / 2;
-          const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
-          uint4 a = widen8(vv[i].x, vv[i].y), b = widen8(vv[i].z, vv[i].w);
-          if (t0 + TOK > T) {
-            if (t0 + row >= T) a = make_uint4(0, 0, 0, 0);
-            if (t0 + row + half >= T) b = make_uint4(0, 0, 0, 0);
-          }
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = a;
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = b;
-        } else {
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = vv[i];
-        }
-      }
-      load_tile(vr, tn, v_off, vv, false);
+      load_res(b);
 
       // softmax
+      if (edge) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (t0 + quad_row<D, TY>(lg, i) + r >= T) s[q][i][r] = -INFINITY;
+      }
+      float mx[NQ];
+      bool move = false;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
-        float mx = -INFINITY;
+        mx[q] = s[q][0][0];
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float z = s[q][i][r] * P.scale_log2;
-            if (t0 + TOK > T && t0 + quad_row<D, TY>(lg, i) + r >= T) z = -INFINITY;
-            s[q][i][r] = z;
-            mx = fmaxf(mx, z);
-          }
-        mx = col_max(mx);
-        if (__any(mx > m[q] + kSlack)) {
-          const float mn = fmaxf(m[q], mx);
+          for (int r = 0; r < 4; ++r) mx[q] = fmaxf(mx[q], s[q][i][r]);
+        mx[q] = scale * col_max(mx[q]);
+        move = move || mx[q] > m[q] + kSlack;
+      }
+      if (__any(move)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          const float mn = fmaxf(m[q], mx[q]);
           const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
           m[q] = mn;
           l[q] *= f;
@@ -793,6 +798,9 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[q][c][r] *= f;
         }
+      }
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
         const float ref = m[q] == -INFINITY ? 0.f : m[q];
         float sum = 0.f;
 #pragma unroll
@@ -800,7 +808,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
           float p[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            p[r] = __builtin_amdgcn_exp2f(s[q][i][r] - ref);
+            p[r] = __builtin_amdgcn_exp2f(fmaf(s[q][i][r], scale, -ref));
             sum += p[r];
           }
           if constexpr (F32) {
@@ -821,9 +829,24 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         clear_r();
         lds_fence();
       }
-      set_mask = next_mask;
-      set_rank = next_rank;
-      t0 = tn;
+    };
+
+    if constexpr (RES != 0) clear_r();
+    Ahead ahead[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      Ahead& b = ahead[d];
+      b.t0 = tile_token(d);
+      b.mask = b.rank = 0;
+      if constexpr (SET) load_mask(b.t0, b.mask, b.rank);
+      load_tile(vr, b.t0, v_off, b.vv, false);
+      load_tile(kr, b.t0, k_off, b.kv, true);
+      load_res(b);
+    }
+#pragma unroll 1
+    for (int it = 0; it < n; it += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) step(ahead[d], it + d);  // (one past the last: every token masked)
     }
   };
 
@@ -896,12 +919,14 @@ template <int D, int TY, int KIND, bool q4>
 static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
   const uint32_t items = (uint32_t)P.hkv * P.n_slots;
   const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
-  if (P.nq == 1)
+  if (P.nq == 1) {
     hipLaunchKernelGGL((parts_kernel<D, 1, TY, KIND, q4>), grid, block, 0, s, P);
-  else if (P.nq == 2)
+  } else if (P.nq == 2) {
     hipLaunchKernelGGL((parts_kernel<D, 2, TY, KIND, q4>), grid, block, 0, s, P);
-  else
-    hipLaunchKernelGGL((parts_kernel<D, 4, TY, KIND, q4>), grid, block, 0, s, P);
+  } else {
+    // (64 columns and many entries do not fit the registers: the plan gives such a call 32)
+    if constexpr (KIND != kManyEntries) hipLaunchKernelGGL((parts_kernel<D, 4, TY, KIND, q4>), grid, block, 0, s, P);
+  }
   return hipGetLastError();
 }
 
