@@ -86,11 +86,47 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(BoundsParams P) {
 }
 
 // ---------------------------------------------------------------- scores
-__device__ __forceinline__ double shfl_xor_f64(double x, int o) {
+// Lane exchanges of fp64 values without LDS: DPP within rows of 16 lanes, permlane swaps across them.
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double x) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = __shfl_xor((uint32_t)u, o, 64), hi = __shfl_xor((uint32_t)(u >> 32), o, 64);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
   return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
+// The two halves that a swap of 16 (32) lanes pairs up, in either order.
+template <int N, class F>
+__device__ __forceinline__ double swap_f64(double x, F f) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32);
+  if constexpr (N == 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    return f(__builtin_bit_cast(double, ((uint64_t)b[0] << 32) | a[0]), __builtin_bit_cast(double, ((uint64_t)b[1] << 32) | a[1]));
+  } else {
+    const auto a = __builtin_amdgcn_permlane32_swap(lo, lo, false, false), b = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return f(__builtin_bit_cast(double, ((uint64_t)b[0] << 32) | a[0]), __builtin_bit_cast(double, ((uint64_t)b[1] << 32) | a[1]));
+  }
+}
+// f over aligned groups of N lanes; every lane gets its group's value.
+template <int N, class F>
+__device__ __forceinline__ double group_f64(double x, F f) {
+  if constexpr (N >= 2) x = f(x, dpp_f64<kDppQuadXor1>(x));
+  if constexpr (N >= 4) x = f(x, dpp_f64<kDppQuadXor2>(x));
+  if constexpr (N >= 8) x = f(x, dpp_f64<kDppRowHalfMirror>(x));
+  if constexpr (N >= 16) x = f(x, dpp_f64<kDppRowMirror>(x));
+  if constexpr (N >= 32) x = swap_f64<16>(x, f);
+  if constexpr (N >= 64) x = swap_f64<32>(x, f);
+  return x;
+}
+struct AddF64 {
+  __device__ __forceinline__ double operator()(double a, double b) const { return a + b; }
+};
+struct MaxF64 {
+  __device__ __forceinline__ double operator()(double a, double b) const { return fmax(a, b); }
+};
+struct MinF64 {
+  __device__ __forceinline__ double operator()(double a, double b) const { return fmin(a, b); }
+};
 
 template <int D, int G, bool BF16>
 __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
@@ -138,9 +174,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
       }
     }
 #pragma unroll
-    for (int o = 1; o < NP; o *= 2)
-#pragma unroll
-      for (int g = 0; g < G; ++g) acc[g] += shfl_xor_f64(acc[g], o);
+    for (int g = 0; g < G; ++g) acc[g] = group_f64<NP>(acc[g], AddF64{});
     if (j < nb && pc == 0) {
 #pragma unroll
       for (int g = 0; g < G; ++g) P.ws[((uint64_t)sh * G + g) * P.cap + j] = acc[g];
@@ -154,16 +188,7 @@ constexpr int kChooseWaves = kChooseThreads / 64;
 constexpr int kChooseBins = 1024;
 constexpr int kChooseList = 1024;
 
-__device__ __forceinline__ double wave_max_f64(double x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x = fmax(x, shfl_xor_f64(x, o));
-  return x;
-}
-__device__ __forceinline__ double wave_min_f64(double x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x = fmin(x, shfl_xor_f64(x, o));
-  return x;
-}
+constexpr int kChooseHeld = 4096;  // ranks that a workgroup keeps in LDS (32 KB)
 
 // A rank as an unsigned number of the same order.
 __device__ __forceinline__ uint64_t order_of(double x) {
@@ -171,16 +196,16 @@ __device__ __forceinline__ uint64_t order_of(double x) {
   return (u >> 63) ? ~u : u | (1ull << 63);
 }
 
-template <int G>
+// HELD: the ranks stay in LDS (sequences of at most 4096 blocks), else in the first head's scores.
+template <int G, bool HELD>
 __global__ __launch_bounds__(kChooseThreads) void block_choose_kernel(SelectParams P) {
-  __shared__ double red[kChooseWaves][G];
-  __shared__ double best_s[G], worst_s;
+  __shared__ double held[HELD ? kChooseHeld : 1];
+  __shared__ double red[kChooseWaves];
   __shared__ uint32_t hist[kChooseBins];
   __shared__ uint64_t list[kChooseList];
-  __shared__ uint32_t wsum[kChooseWaves], wsum2[kChooseWaves];
-  __shared__ uint32_t s_bin, s_need, s_count, s_n;
+  __shared__ uint32_t wsum[2][kChooseWaves];
+  __shared__ uint32_t s_bin, s_need, s_count, s_n, s_take;
   __shared__ uint64_t s_key;
-  __shared__ uint32_t s_take;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int sh = blockIdx.x, seq = sh / P.hkv;
   const int T = min(max(P.seq_lens[seq], 0), P.max_seq_len);
@@ -194,52 +219,55 @@ __global__ __launch_bounds__(kChooseThreads) void block_choose_kernel(SelectPara
     return;
   }
   // more blocks than are selected: n_first + n_last <= n_sel < nb, so the two ends are apart
-  const int first = P.n_first, last = nb - P.n_last;  // candidates are [first, last)
+  const int first = P.n_first, last = nb - P.n_last;           // candidates are [first, last)
+  const uint32_t need = (uint32_t)(n - P.n_first - P.n_last);  // of them
   double* sc = P.ws + (uint64_t)sh * G * P.cap;
+  double* rank = HELD ? held : sc;
 
-  // every head's best block
+  // Every head's best block: 16 / G waves a head (sixteen waves share four SIMDs, so a reduction of every head in
+  // every wave would cost G times its instructions).
+  constexpr int WPH = kChooseWaves / G;
+  double mine[G];  // the thread's first block, requested with the others
+#pragma unroll
+  for (int g = 0; g < G; ++g) mine[g] = tid < nb ? sc[(uint64_t)g * P.cap + tid] : -INFINITY;
+  {
+    const double* one = sc + (uint64_t)(wave / WPH) * P.cap;
+    double x = -INFINITY;
+#pragma unroll 4
+    for (int j = (wave % WPH) * 64 + lane; j < nb; j += WPH * 64) x = fmax(x, one[j]);
+    x = group_f64<64>(x, MaxF64{});
+    if (lane == 0) red[wave] = x;
+  }
+  hist[tid] = 0;
+  if (tid == 0) {
+    s_n = s_count = 0;
+    s_key = ~0ull;
+    s_take = 0;
+  }
+  __syncthreads();
   double m[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) m[g] = -INFINITY;
-  for (int j = tid; j < nb; j += kChooseThreads)
-#pragma unroll
-    for (int g = 0; g < G; ++g) m[g] = fmax(m[g], sc[(uint64_t)g * P.cap + j]);
-#pragma unroll
   for (int g = 0; g < G; ++g) {
-    m[g] = wave_max_f64(m[g]);
-    if (lane == 0) red[wave][g] = m[g];
-  }
-  __syncthreads();
-  if (tid < G) {
-    double x = red[0][tid];
-    for (int w = 1; w < kChooseWaves; ++w) x = fmax(x, red[w][tid]);
-    best_s[tid] = x;
-  }
-  for (int i = tid; i < kChooseBins; i += kChooseThreads) hist[i] = 0;
-  __syncthreads();
+    m[g] = red[g * WPH];
 #pragma unroll
-  for (int g = 0; g < G; ++g) m[g] = best_s[g];
+    for (int w = 1; w < WPH; ++w) m[g] = fmax(m[g], red[g * WPH + w]);
+  }
 
-  // the ranks (over their own score plane: every thread keeps its blocks), the worst finite one
+  // the ranks (every thread keeps its blocks), and the worst finite one
   double worst = 0.0;
   for (int j = tid; j < nb; j += kChooseThreads) {
     double r = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < G; ++g) r = fmax(r, sc[(uint64_t)g * P.cap + j] - m[g]);
-    sc[j] = r;
+    for (int g = 0; g < G; ++g) r = fmax(r, (j == tid ? mine[g] : sc[(uint64_t)g * P.cap + j]) - m[g]);
+    rank[j] = r;
     if (j >= first && j < last && r > -INFINITY) worst = fmin(worst, r);
   }
-  worst = wave_min_f64(worst);
-  if (lane == 0) red[wave][0] = worst;
+  worst = group_f64<64>(worst, MinF64{});
+  __syncthreads();  // red is read above
+  if (lane == 0) red[wave] = worst;
   __syncthreads();
-  if (tid == 0) {
-    double x = red[0][0];
-    for (int w = 1; w < kChooseWaves; ++w) x = fmin(x, red[w][0]);
-    worst_s = x;
-    s_n = 0;
-  }
-  __syncthreads();
-  worst = worst_s;
+#pragma unroll
+  for (int w = 0; w < kChooseWaves; ++w) worst = fmin(worst, red[w]);
   // bins of equal width, the best ranks first; any scale keeps the order
   const double scale = worst < 0.0 ? (double)(kChooseBins - 1) / -worst : 0.0;
   auto bin_of = [&](double r) -> uint32_t {
@@ -247,118 +275,110 @@ __global__ __launch_bounds__(kChooseThreads) void block_choose_kernel(SelectPara
     const double x = -r * scale;
     return x >= (double)(kChooseBins - 1) ? kChooseBins - 1 : (uint32_t)x;
   };
-  const uint32_t need = (uint32_t)(n - P.n_first - P.n_last);  // of the candidates
-  for (int j = first + tid; j < last; j += kChooseThreads) atomicAdd(&hist[bin_of(sc[j])], 1u);
+  for (int j = tid; j < nb; j += kChooseThreads)  // (its own blocks: no barrier since they were written)
+    if (j >= first && j < last) atomicAdd(&hist[bin_of(rank[j])], 1u);
   __syncthreads();
   // the bin of the need-th best: a running sum over the bins, one a thread
   {
     static_assert(kChooseBins == kChooseThreads, "one bin a thread");
-    uint32_t c = hist[tid], x = c;
+    const uint32_t c = hist[tid];
+    uint32_t x = c;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
       const uint32_t y = __shfl_up(x, o, 64);
       if (lane >= o) x += y;
     }
-    if (lane == 63) wsum[wave] = x;
+    if (lane == 63) wsum[0][wave] = x;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < wave; ++w) before += wsum[w];
-    x += before;
+#pragma unroll
+    for (int w = 0; w < kChooseWaves; ++w) x += w < wave ? wsum[0][w] : 0u;
     if (need > 0 && x >= need && x - c < need) {
       s_bin = (uint32_t)tid;
       s_need = need - (x - c);
       s_count = c;
     }
-    if (need == 0 && tid == 0) s_count = 0;
   }
   __syncthreads();
   // the order of the last selected candidate, and how many of that very order are selected
-  const uint32_t cut = s_bin, in_bin = s_count, left = s_need;
-  if (need == 0) {
-    if (tid == 0) {
-      s_key = ~0ull;
-      s_take = 0;
-    }
-  } else if (in_bin <= kChooseList) {
-    for (int j = first + tid; j < last; j += kChooseThreads)
-      if (bin_of(sc[j]) == cut) list[atomicAdd(&s_n, 1u)] = order_of(sc[j]);
-    __syncthreads();
-    if (tid < (int)in_bin) {
-      const uint64_t mine = list[tid];
-      uint32_t above = 0, same = 0;
-      for (uint32_t i = 0; i < in_bin; ++i) {
-        above += list[i] > mine ? 1u : 0u;
-        same += list[i] == mine ? 1u : 0u;
-      }
-      if (above < left && above + same >= left) {  // equal ranks all write the same
-        s_key = mine;
-        s_take = left - above;
-      }
-    }
-  } else {
-    uint64_t key = 0, mask = 0;
-    uint32_t want = left;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+  if (need > 0) {
+    const uint32_t cut = s_bin, in_bin = s_count, left = s_need;
+    if (in_bin <= kChooseList) {
+      for (int j = tid; j < nb; j += kChooseThreads)
+        if (j >= first && j < last && bin_of(rank[j]) == cut) list[atomicAdd(&s_n, 1u)] = order_of(rank[j]);
       __syncthreads();
-      for (int j = first + tid; j < last; j += kChooseThreads) {
-        const double r = sc[j];
-        const uint64_t o = order_of(r);
-        if (bin_of(r) == cut && (o & mask) == key) atomicAdd(&hist[(o >> shift) & 255u], 1u);
+      if (tid < (int)in_bin) {
+        const uint64_t o = list[tid];
+        uint32_t above = 0, same = 0;
+        for (uint32_t i = 0; i < in_bin; ++i) {
+          above += list[i] > o ? 1u : 0u;
+          same += list[i] == o ? 1u : 0u;
+        }
+        if (above < left && above + same >= left) {  // equal ranks all write the same
+          s_key = o;
+          s_take = left - above;
+        }
       }
-      __syncthreads();
+    } else {
+      uint64_t key = 0, mask = 0;
+      uint32_t want = left;
+      for (int shift = 56; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < nb; j += kChooseThreads) {
+          const double r = rank[j];
+          const uint64_t o = order_of(r);
+          if (j >= first && j < last && bin_of(r) == cut && (o & mask) == key) atomicAdd(&hist[(o >> shift) & 255u], 1u);
+        }
+        __syncthreads();
+        if (tid == 0) {
+          uint32_t sum = 0;
+          int d = 255;
+          while (d > 0 && sum + hist[d] < want) sum += hist[d--];
+          s_bin = (uint32_t)d;
+          s_need = want - sum;
+        }
+        __syncthreads();
+        key |= (uint64_t)s_bin << shift;
+        mask |= 255ull << shift;
+        want = s_need;
+        __syncthreads();
+      }
       if (tid == 0) {
-        uint32_t sum = 0;
-        int d = 255;
-        while (d > 0 && sum + hist[d] < want) sum += hist[d--];
-        s_bin = (uint32_t)d;
-        s_need = want - sum;
+        s_key = key;
+        s_take = want;
       }
-      __syncthreads();
-      key |= (uint64_t)s_bin << shift;
-      mask |= 255ull << shift;
-      want = s_need;
-      __syncthreads();
-    }
-    if (tid == 0) {
-      s_key = key;
-      s_take = want;
     }
   }
   __syncthreads();
   const uint64_t key = s_key;
   const uint32_t take = s_take;
 
-  // the selected blocks, ascending: equals of `key` taken from the lowest on
-  uint32_t done = 0, equal_before = 0;
+  // The selected blocks, ascending: those above `key`, the ends, and the first `take` equal to it.  A block's place is
+  // the number of the former before it and of the latter, up to `take`.
+  uint32_t above = 0, equal = 0;  // in the chunks before
   for (int j0 = 0; j0 < nb; j0 += kChooseThreads) {
     const int j = j0 + tid;
     const bool live = j < nb, ends = live && (j < first || j >= last);
-    const uint64_t o = live ? order_of(sc[j]) : 0;
-    const bool eq = live && !ends && need > 0 && o == key;
-    const uint64_t beq = __ballot(eq);
-    if (lane == 0) wsum[wave] = (uint32_t)__popcll(beq);
-    __syncthreads();
-    uint32_t eqb = equal_before, eqt = 0;
-    for (int w = 0; w < kChooseWaves; ++w) {
-      if (w < wave) eqb += wsum[w];
-      eqt += wsum[w];
+    const uint64_t o = live ? order_of(rank[j]) : 0;
+    const bool gt = ends || (live && need > 0 && o > key), eq = live && !ends && need > 0 && o == key;
+    const uint64_t bg = __ballot(gt), be = __ballot(eq);
+    if (lane == 0) {
+      wsum[0][wave] = (uint32_t)__popcll(bg);
+      wsum[1][wave] = (uint32_t)__popcll(be);
     }
-    eqb += (uint32_t)__popcll(beq & ((1ull << lane) - 1));
-    const bool sel = ends || (live && need > 0 && (o > key || (eq && eqb < take)));
-    const uint64_t bs = __ballot(sel);
-    if (lane == 0) wsum2[wave] = (uint32_t)__popcll(bs);
     __syncthreads();
-    uint32_t at = done, tot = 0;
+    uint32_t g_at = above + (uint32_t)__popcll(bg & ((1ull << lane) - 1)), e_at = equal + (uint32_t)__popcll(be & ((1ull << lane) - 1));
+#pragma unroll
     for (int w = 0; w < kChooseWaves; ++w) {
-      if (w < wave) at += wsum2[w];
-      tot += wsum2[w];
+      const uint32_t a = wsum[0][w], e = wsum[1][w];
+      g_at += w < wave ? a : 0u;
+      e_at += w < wave ? e : 0u;
+      above += a;
+      equal += e;
     }
-    at += (uint32_t)__popcll(bs & ((1ull << lane) - 1));
-    if (sel && at < (uint32_t)n) out[at] = j;
-    done += tot;
-    equal_before += eqt;
-    __syncthreads();
+    const uint32_t at = g_at + min(e_at, take);
+    if ((gt || (eq && e_at < take)) && at < (uint32_t)n) out[at] = j;
+    if (j0 + kChooseThreads < nb) __syncthreads();
   }
 }
 
@@ -373,7 +393,11 @@ hipError_t launch_select_dg(const SelectParams& P, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((block_choose_kernel<G>), dim3((unsigned)(P.batch * P.hkv)), dim3(kChooseThreads), 0, s, P);
+  const dim3 units((unsigned)(P.batch * P.hkv));
+  if (P.cap <= kChooseHeld)
+    hipLaunchKernelGGL((block_choose_kernel<G, true>), units, dim3(kChooseThreads), 0, s, P);
+  else
+    hipLaunchKernelGGL((block_choose_kernel<G, false>), units, dim3(kChooseThreads), 0, s, P);
   return hipGetLastError();
 }
 
