@@ -193,86 +193,96 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   }
   slot += P.slot0;
   int part = P.part0;
-#pragma unroll 1
-  while (part + 1 < P.part_end && slot >= P.part_base[part + 1]) ++part;
+#pragma unroll
+  for (int i = 1; i < kMaxParts; ++i) part += i > P.part0 && i < P.part_end && slot >= P.part_base[i] ? 1 : 0;
   const PartsPart pt = P.part[part];
   const bool tail = pt.cache == nullptr;
   const int useq = P.shared ? 0 : seq;
-  const int T = min(max(as_const(pt.lens)[useq], 0), pt.max_len);
   const int chunk0 = (slot - P.part_base[part]) * P.tiles_per_wg;  // first tile
 
-  // ---- the unit
-  uint32_t mbyte = (uint32_t)kExact;
-  uint64_t seg_off = 0;
-  if (!tail) {
-    const uint64_t u = ((uint64_t)useq * P.n_blocks + P.block) * hkv + head;
-    mbyte = (as_const(reinterpret_cast<const uint32_t*>(pt.modes))[u >> 2] >> (8 * (u & 3))) & 0xFFu;
-    seg_off = as_const(pt.seg_off)[u];
+  // ---- queries, requested first (a column past the rows repeats the last one's and is zeroed)
+  const uint8_t* q_all = static_cast<const uint8_t*>(P.q);
+  const int rows = P.shared ? P.rows : G;
+  auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // of the call: (sequence, head of the group)
+    const int r = row0 + col, rc = min(r, rows - 1);
+    s = P.shared ? rc >> P.g_shift : seq;
+    g = P.shared ? rc & (G - 1) : rc;
+    return r < rows;
+  };
+  auto q_row = [&](int s, int g) __attribute__((always_inline)) {
+    return reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
+  };
+  // 64 columns: the thread's share on its way into LDS; else the lane's column of each column tile
+  constexpr int QR = QL ? 16 * NQ * NP / 256 : NQ, QP = QL ? 1 : KK;
+  uint4 qf[QR][QP];
+  bool q_ok[QR];
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {
+    int s, g;
+    const int at = threadIdx.x + 256 * i;
+    q_ok[i] = row_of(QL ? at / NP : 16 * i + lc, s, g);
+    const uint4* src = q_row(s, g);
+#pragma unroll
+    for (int j = 0; j < QP; ++j) qf[i][j] = src[QL ? at % NP : 4 * j + lg];
   }
+
+  // ---- what the unit's arrays say, requested in one go: a length, the mode's word, the segment's offset, the number
+  // of selected blocks, and the blocks of the wave's tiles (lane i: tile i).  What a part has not (the tail: modes and
+  // offsets, others: blocks) is read from its lengths and not used.
+  const uint64_t u = tail ? 0 : ((uint64_t)useq * P.n_blocks + P.block) * hkv + head;
+  const bool picked = pt.blocks != nullptr;
+  const int64_t unit = (int64_t)seq * hkv + head;
+  const auto* words = as_const(reinterpret_cast<const uint32_t*>(tail ? reinterpret_cast<const uint8_t*>(pt.lens) : pt.modes));
+  const auto* offs = as_const(reinterpret_cast<const uint32_t*>(tail ? reinterpret_cast<const uint64_t*>(pt.lens) : pt.seg_off));
+  const auto* picks = as_const(picked ? pt.counts + unit : pt.lens);
+  const int32_t* list = picked ? pt.blocks + unit * pt.n_sel : pt.lens;
+  const int my_pick = (chunk0 + wave + 4 * lane) / S::TPB;
+  const int len = as_const(pt.lens)[useq];
+  const uint32_t mode_word = words[u >> 2], off_lo = offs[2 * u], off_hi = offs[tail ? 0 : 2 * u + 1];
+  const int n_picked = picks[0];
+  int my_block = list[picked ? min(my_pick, pt.n_sel - 1) : 0];
+  asm volatile("" ::"s"(len), "s"(mode_word), "s"(off_lo), "s"(off_hi), "s"(n_picked));
+  const int T = min(max(len, 0), pt.max_len);
+  const uint32_t mbyte = tail ? (uint32_t)kExact : (mode_word >> (8 * (u & 3))) & 0xFFu;
+  const uint64_t seg_off = tail ? 0 : ((uint64_t)off_hi << 32) | off_lo;
   const bool bad_unit = !unit_byte_ok(mbyte, P.tokres ? P.n_rates : 0) || (seg_off & (kPlaneAlign - 1));
   const int mode = mode_of(mbyte);
-  int n_tiles;  // of the part
-  const int32_t* list = nullptr;
-  if (pt.blocks) {
-    const int64_t at = (int64_t)seq * hkv + head;
-    list = pt.blocks + at * pt.n_sel;
-    n_tiles = min(max(as_const(pt.counts)[at], 0), pt.n_sel) * S::TPB;
-  } else {
-    n_tiles = (T + TOK - 1) / TOK;
-  }
+  const int n_tiles = picked && T > 0 ? min(max(n_picked, 0), pt.n_sel) * S::TPB : (T + TOK - 1) / TOK;  // of the part
+  if (my_block < 0 || my_block >= (T + kBlockTokens - 1) / kBlockTokens) my_block = -1;
   const int end = min(chunk0 + P.tiles_per_wg, n_tiles);
   int n = chunk0 + wave < end ? (end - chunk0 - wave + 3) / 4 : 0;  // the wave's tiles: chunk0 + wave + 4 i
   if (bad_unit) n = 0;
 
-  // ---- queries
-  const uint8_t* q_all = static_cast<const uint8_t*>(P.q);
-  const int rows = P.shared ? P.rows : G;
-  auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // of the call: (sequence, head of the group)
-    const int r = row0 + col;
-    s = P.shared ? r >> P.g_shift : seq;
-    g = P.shared ? r & (G - 1) : r;
-    return r < rows;
-  };
   // piece of a column's query in LDS, permuted by the column against bank conflicts
   auto q_at = [&](int q, int col, int piece) __attribute__((always_inline)) {
     const int f = NP == 8 ? col >> 1 : col;
     return lds + 4 * kWaveLds + (16 * q + col) * RB + ((piece ^ f) << 4);
   };
   // The scale's sign goes to the queries, so that a column's largest product is its largest logit; a scale of zero
-  // zeroes them.
+  // zeroes them.  (Once the first tile is requested: the queries were before it.)
   const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
-  const uint32_t q_sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
-  const bool q_zero = P.scale_log2 == 0.f;
-  auto signed_query = [&](bool ok, const uint4* src) __attribute__((always_inline)) -> uint4 {
-    if (!ok || q_zero) return make_uint4(0, 0, 0, 0);
-    const uint4 v = *src;
-    return make_uint4(v.x ^ q_sign, v.y ^ q_sign, v.z ^ q_sign, v.w ^ q_sign);
+  auto settle_queries = [&]() __attribute__((always_inline)) {
+    const uint32_t sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
+#pragma unroll
+    for (int i = 0; i < QR; ++i) {
+      const uint32_t keep = q_ok[i] && P.scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+      for (int j = 0; j < QP; ++j) {
+        uint4& v = qf[i][j];
+        v = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
+        if constexpr (QL) {
+          const int at = threadIdx.x + 256 * i, col = at / NP;
+          *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, at % NP)) = v;
+        }
+      }
+    }
+    if constexpr (QL) __syncthreads();
   };
-  uint4 qf[QL ? 1 : NQ][QL ? 1 : KK];
-  if constexpr (QL) {
-    for (int i = threadIdx.x; i < 16 * NQ * NP; i += 256) {
-      const int col = i / NP, piece = i % NP;
-      int s, g;
-      const bool ok = row_of(col, s, g);
-      const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
-      *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, piece)) = signed_query(ok, src + piece);
-    }
-    __syncthreads();
-  } else {
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      int s, g;
-      const bool ok = row_of(16 * q + lc, s, g);
-      const uint4* src = reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[q][kk] = signed_query(ok, src + 4 * kk + lg);
-    }
-  }
   auto query = [&](int q, int kk) __attribute__((always_inline)) -> uint4 {
     if constexpr (QL)
       return *reinterpret_cast<const uint4*>(q_at(q, lc, 4 * kk + lg));
     else
-      return qf[q][kk];
+      return qf[QL ? 0 : q][QL ? 0 : kk];
   };
 
   float m[NQ], l[NQ];
@@ -337,18 +347,11 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     const auto* counts = as_const(reinterpret_cast<const uint32_t*>(seg + L.count));
 
     // ---- the wave's tiles
-    int my_block = 0;  // lane i: the block of the wave's tile i
-    if (list) {
-      const int u = chunk0 + wave + 4 * lane;
-      my_block = lane < n ? list[u / S::TPB] : 0;
-      const int total = (T + kBlockTokens - 1) / kBlockTokens;
-      if (my_block < 0 || my_block >= total) my_block = -1;
-    }
     // first token of the wave's tile i; T where it has none (every load reads zeros, every token is masked)
     auto tile_token = [&](int i) __attribute__((always_inline)) -> int {
       const int u = chunk0 + wave + 4 * i;
       int t = u * TOK;
-      if (list) {
+      if (picked) {
         const int b = __builtin_amdgcn_readlane(my_block, i & 63);
         t = b < 0 ? T : b * kBlockTokens + (u % S::TPB) * TOK;
       }
@@ -843,6 +846,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       load_tile(kr, b.t0, k_off, b.kv, true);
       load_res(b);
     }
+    settle_queries();
 #pragma unroll 1
     for (int it = 0; it < n; it += DEPTH) {
 #pragma unroll
@@ -854,7 +858,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   using no = integral_constant<bool, false>;
   using yes = integral_constant<bool, true>;
   const bool res = mode == kResidual && (KIND == kTokenSet || P.topk > 0);
-  if (n > 0) {
+  if (chunk0 < end && !bad_unit) {  // (the whole workgroup: the walk has a barrier)
     if constexpr (TY == kTyC8) {
       if (mode == kExact)
         walk(no{}, no{});
