@@ -1073,56 +1073,50 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
   p.by_hkv.set((uint32_t)p.hkv);
   p.by_topk.set((uint32_t)std::max(p.topk, 1));
   p.n_slots_total = (int)plan.total_slots;
-  int base = 0;
-  for (int i = 0; i < plan.n_own + plan.n_shared; ++i) {
-    const int at = i < plan.n_own ? plan.own[i] : plan.shared[i - plan.n_own];
-    PartsPart& o = p.part[i];
-    p.part_base[i] = base;
-    base += (int)plan.slots[i];
-    if (at < 0) {
-      o.lens = tail->lens;
-      o.max_len = tail->cap;
-      p.tail_k = tail->k;
-      p.tail_v = tail->v;
-      p.tail_cap = tail->cap;
-      continue;
-    }
-    const fdkv_part& pt = parts[at];
-    o.lens = pt.seq_lens;
-    o.max_len = pt.max_seq_len;
-    o.cache = static_cast<const uint8_t*>(pt.cache);
-    o.modes = pt.modes;
-    o.seg_off = pt.seg_offsets;
-    if (pt.kind == FDKV_PART_BLOCKS) {
-      o.blocks = pt.blocks;
-      o.counts = pt.counts;
-      o.n_sel = pt.n_sel;
-    }
+  if (tail) {
+    p.tail_k = tail->k;
+    p.tail_v = tail->v;
+    p.tail_cap = tail->cap;
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (plan.own_slots > 0) {
-    p.shared = false;
-    p.nq = 1;
-    p.tiles_per_wg = plan.own_tiles_per_wg;
-    p.slot0 = 0;
-    p.n_slots = (int)plan.own_slots;
-    p.part0 = 0;
-    p.part_end = plan.n_own;
+  for (int shared = 0; shared < 2; ++shared) {  // a launch for the parts of single sequences, one for the shared ones
+    const int n = shared ? plan.n_shared : plan.n_own;
+    const int64_t* slots = plan.slots + (shared ? plan.n_own : 0);
+    p.n_slots = (int)(shared ? plan.total_slots - plan.own_slots : plan.own_slots);
+    if (p.n_slots == 0) continue;
+    int base = 0;
+    for (int i = 0; i < kMaxParts; ++i) {
+      PartsPart& o = p.part[i];
+      o = PartsPart{};
+      p.part_base[i] = i < n ? base : INT32_MAX;
+      if (i >= n) continue;
+      base += (int)slots[i];
+      const int at = shared ? plan.shared[i] : plan.own[i];
+      o.lens = at < 0 ? tail->lens : parts[at].seq_lens;
+      // what a part has not points to memory that may be read
+      o.modes = reinterpret_cast<const uint8_t*>(o.lens);
+      o.seg_off = reinterpret_cast<const uint64_t*>(o.lens);
+      o.blocks = o.counts = o.lens;
+      o.max_len = at < 0 ? tail->cap : parts[at].max_seq_len;
+      if (at < 0) continue;
+      const fdkv_part& pt = parts[at];
+      o.cache = static_cast<const uint8_t*>(pt.cache);
+      o.modes = pt.modes;
+      o.seg_off = pt.seg_offsets;
+      if (pt.kind == FDKV_PART_BLOCKS) {
+        o.blocks = pt.blocks;
+        o.counts = pt.counts;
+        o.n_sel = pt.n_sel;
+      }
+    }
+    p.shared = shared;
+    p.nq = shared ? plan.nq : 1;
+    p.rows = shared ? plan.rows : p.G;
+    p.row_groups = shared ? plan.row_groups : 1;
+    p.tiles_per_wg = shared ? plan.shared_tiles_per_wg : plan.own_tiles_per_wg;
+    p.slot0 = shared ? (int)plan.own_slots : 0;
     p.by_slots.set((uint32_t)p.n_slots);
-    const hipError_t e = launch_parts(p, s);
-    if (e != hipSuccess) return hip_fail(e, "decode_parts");
-  }
-  if (plan.total_slots > plan.own_slots) {
-    p.shared = true;
-    p.nq = plan.nq;
-    p.rows = plan.rows;
-    p.row_groups = plan.row_groups;
     p.by_groups.set((uint32_t)p.row_groups);
-    p.tiles_per_wg = plan.shared_tiles_per_wg;
-    p.slot0 = (int)plan.own_slots;
-    p.n_slots = (int)(plan.total_slots - plan.own_slots);
-    p.part0 = plan.n_own;
-    p.part_end = plan.n_own + plan.n_shared;
     const hipError_t e = launch_parts(p, s);
     if (e != hipSuccess) return hip_fail(e, "decode_parts");
   }

@@ -150,33 +150,33 @@ __device__ __forceinline__ int decode_part(const DecodeParams& P, int r) {
 struct PartsPart {
   const int32_t* lens;         // [batch] ([1] of a shared part)
   const uint8_t* cache;        // null: the exact tail
-  const uint8_t* modes;        // [batch][blocks][hkv], 4-byte aligned ([1][..][..] of a shared part)
-  const uint64_t* seg_off;
-  const int32_t* blocks;       // [batch][hkv][n_sel] selected blocks, or null: every token
-  const int32_t* counts;       // [batch][hkv]
-  int n_sel, max_len;
+  const uint8_t* modes;        // [batch][blocks][hkv], 4-byte aligned ([1][..][..] of a shared part); the tail: lens
+  const uint64_t* seg_off;     // as modes
+  const int32_t* blocks;       // [batch][hkv][n_sel] selected blocks; every token: lens
+  const int32_t* counts;       // [batch][hkv]; every token: lens
+  int n_sel, max_len;          // n_sel 0: every token
 };
 
-// One launch: the parts of single sequences, or the shared ones.
+// One launch: the parts of single sequences, or the shared ones.  What a
+// workgroup needs before it can ask for anything else comes first: it fetches
+// that in one go.
 struct PartsParams {
-  DivU by_slots, by_hkv, by_groups, by_topk;
+  DivU by_slots, by_hkv, by_groups;
+  int hkv, hq, G, g_shift, n_slots, tiles_per_wg, row_groups, rows;  // rows: query rows of a sequence, or of the batch
+  int n_blocks, block, slot0, shared;
   const void* q;               // [batch][hq][d]
+  PartsPart part[kMaxParts];   // this launch's parts
+  int part_base[kMaxParts];    // first slot of each, from 0; INT32_MAX past the last
+  DivU by_topk;
   float* ws;                   // records [batch][hkv][n_slots_total][G][d + 4]
   const void* tail_k;          // [batch][hkv][tail_cap][d]
   const void* tail_v;
-  int hkv, hq, G, g_shift, batch, n_blocks, block, pos, bsize, topk, d, tail_cap;
+  int batch, pos, bsize, topk, d, tail_cap, n_slots_total;
   float wres[3], scale_log2;
   int res_ppm, n_rates;
   int rates_ppm[kMaxRates];
-  bool tokres, shared, bf16, coef8;
+  bool tokres, bf16, coef8;
   int nq;                      // column tiles of a wave (16 query rows each): 1, 2 or 4
-  int rows, row_groups;        // shared: query rows of the batch, groups of 16 nq of them
-  int tiles_per_wg;            // tiles of a chunk (one record), a multiple of 4
-  int slot0, n_slots;          // record slots of this launch's parts
-  int n_slots_total;
-  int part0, part_end;         // this launch's parts
-  PartsPart part[kMaxParts];
-  int part_base[kMaxParts];    // first record slot of each part
 };
 
 // generation: append one token's K / V rows of one layer to the exact tail

@@ -170,47 +170,58 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, lane = threadIdx.x & 63;
   const int lc = lane & 15, lg = lane >> 4;  // column (or operand row) and lane group
-  const int G = P.G, hkv = P.hkv;
+  // ---- what the launch says, fetched in one go and kept (left to itself the compiler reads it piece by piece, each
+  // piece a trip to memory)
+  DivU by_slots = P.by_slots, by_hkv = P.by_hkv, by_groups = P.by_groups;
+  int hkv = P.hkv, hq = P.hq, G = P.G, g_shift = P.g_shift, n_slots = P.n_slots, tiles_per_wg = P.tiles_per_wg;
+  int row_groups = P.row_groups, rows = P.rows, n_blocks = P.n_blocks, block = P.block, slot0 = P.slot0, shared = P.shared;
+  const void* q_all = P.q;
+  PartsPart pt = P.part[0], pt1 = P.part[1];
+  int base1 = P.part_base[1], base2 = P.part_base[2];
+  asm volatile("" : "+s"(by_slots.mul), "+s"(by_slots.shift), "+s"(by_hkv.mul), "+s"(by_hkv.shift), "+s"(by_groups.mul),
+               "+s"(by_groups.shift), "+s"(hkv), "+s"(hq), "+s"(G), "+s"(g_shift), "+s"(n_slots), "+s"(tiles_per_wg),
+               "+s"(row_groups), "+s"(rows));
+  asm volatile("" : "+s"(n_blocks), "+s"(block), "+s"(slot0), "+s"(shared), "+s"(q_all), "+s"(base1), "+s"(base2), "+s"(pt.lens),
+               "+s"(pt.cache), "+s"(pt.modes), "+s"(pt.seg_off), "+s"(pt.blocks), "+s"(pt.counts), "+s"(pt.n_sel), "+s"(pt.max_len));
+  asm volatile("" : "+s"(pt1.lens), "+s"(pt1.cache), "+s"(pt1.modes), "+s"(pt1.seg_off), "+s"(pt1.blocks), "+s"(pt1.counts),
+               "+s"(pt1.n_sel), "+s"(pt1.max_len));
 
   // ---- which chunk
-  int seq, head, slot, row0;
-  if (P.shared) {
+  uint32_t w = blockIdx.x;
+  int row0 = 0;
+  if (shared) {
     // the row groups of one chunk follow each other on one XCD (workgroups go to the XCDs in turn)
-    const uint32_t x = blockIdx.x & 7u, y = blockIdx.x >> 3;
-    const uint32_t ym = P.by_groups.div(y);
-    const uint32_t w = ym * 8 + x;
-    if (w >= (uint32_t)(hkv * P.n_slots)) return;
-    slot = (int)P.by_hkv.div(w);
-    head = (int)w - slot * hkv;
-    row0 = (int)(y - ym * P.row_groups) * 16 * NQ;
-    seq = 0;
-  } else {
-    const uint32_t sl = P.by_hkv.div(blockIdx.x);
-    head = (int)(blockIdx.x - sl * hkv);
-    seq = (int)P.by_slots.div(sl);
-    slot = (int)sl - seq * P.n_slots;
-    row0 = 0;
+    const uint32_t y = w >> 3, ym = by_groups.div(y);
+    row0 = (int)(y - ym * row_groups) * 16 * NQ;
+    w = ym * 8 + (w & 7u);
+    if (w >= (uint32_t)(hkv * n_slots)) return;
   }
-  slot += P.slot0;
-  int part = P.part0;
-#pragma unroll
-  for (int i = 1; i < kMaxParts; ++i) part += i > P.part0 && i < P.part_end && slot >= P.part_base[i] ? 1 : 0;
-  const PartsPart pt = P.part[part];
-  const bool tail = pt.cache == nullptr;
-  const int useq = P.shared ? 0 : seq;
-  const int chunk0 = (slot - P.part_base[part]) * P.tiles_per_wg;  // first tile
+  const uint32_t sl = by_hkv.div(w);
+  const int head = (int)(w - sl * hkv), seq = (int)by_slots.div(sl);  // (shared: sequence 0)
+  int slot = (int)sl - seq * n_slots, chunk0 = slot;
+  if (slot >= base1) {
+    pt = pt1;
+    chunk0 = slot - base1;
+    if (slot >= base2) {
+      int i = 2;
+      while (i + 1 < kMaxParts && slot >= P.part_base[i + 1]) ++i;
+      pt = P.part[i];
+      chunk0 = slot - P.part_base[i];
+    }
+  }
+  chunk0 *= tiles_per_wg;  // the chunk's first tile
+  slot += slot0;
+  const bool tail = pt.cache == nullptr, picked = pt.n_sel > 0;
 
   // ---- queries, requested first (a column past the rows repeats the last one's and is zeroed)
-  const uint8_t* q_all = static_cast<const uint8_t*>(P.q);
-  const int rows = P.shared ? P.rows : G;
-  auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // of the call: (sequence, head of the group)
+  auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // (sequence, head of the group)
     const int r = row0 + col, rc = min(r, rows - 1);
-    s = P.shared ? rc >> P.g_shift : seq;
-    g = P.shared ? rc & (G - 1) : rc;
+    s = seq + (rc >> g_shift);
+    g = rc & (G - 1);
     return r < rows;
   };
   auto q_row = [&](int s, int g) __attribute__((always_inline)) {
-    return reinterpret_cast<const uint4*>(q_all + ((uint64_t)s * P.hq + (uint64_t)head * G + g) * RB);
+    return reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q_all) + ((uint64_t)s * hq + (uint64_t)head * G + g) * RB);
   };
   // 64 columns: the thread's share on its way into LDS; else the lane's column of each column tile
   constexpr int QR = QL ? 16 * NQ * NP / 256 : NQ, QP = QL ? 1 : KK;
@@ -227,29 +238,25 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   }
 
   // ---- what the unit's arrays say, requested in one go: a length, the mode's word, the segment's offset, the number
-  // of selected blocks, and the blocks of the wave's tiles (lane i: tile i).  What a part has not (the tail: modes and
-  // offsets, others: blocks) is read from its lengths and not used.
-  const uint64_t u = tail ? 0 : ((uint64_t)useq * P.n_blocks + P.block) * hkv + head;
-  const bool picked = pt.blocks != nullptr;
-  const int64_t unit = (int64_t)seq * hkv + head;
-  const auto* words = as_const(reinterpret_cast<const uint32_t*>(tail ? reinterpret_cast<const uint8_t*>(pt.lens) : pt.modes));
-  const auto* offs = as_const(reinterpret_cast<const uint32_t*>(tail ? reinterpret_cast<const uint64_t*>(pt.lens) : pt.seg_off));
-  const auto* picks = as_const(picked ? pt.counts + unit : pt.lens);
-  const int32_t* list = picked ? pt.blocks + unit * pt.n_sel : pt.lens;
-  const int my_pick = (chunk0 + wave + 4 * lane) / S::TPB;
-  const int len = as_const(pt.lens)[useq];
+  // of selected blocks, and the blocks of the wave's tiles (lane i: tile i).  (What a part has not points to its
+  // lengths and is not used.)
+  const uint64_t u = tail ? 0 : ((uint64_t)seq * n_blocks + block) * hkv + head;
+  const int64_t unit = picked ? (int64_t)seq * hkv + head : 0;
+  const auto* words = as_const(reinterpret_cast<const uint32_t*>(pt.modes));
+  const auto* offs = as_const(reinterpret_cast<const uint32_t*>(pt.seg_off));
+  const int len = as_const(pt.lens)[seq];
   const uint32_t mode_word = words[u >> 2], off_lo = offs[2 * u], off_hi = offs[tail ? 0 : 2 * u + 1];
-  const int n_picked = picks[0];
-  int my_block = list[picked ? min(my_pick, pt.n_sel - 1) : 0];
+  const int n_picked = as_const(pt.counts)[unit];
+  int my_block = pt.blocks[unit * pt.n_sel + (picked ? min((chunk0 + wave + 4 * lane) / S::TPB, pt.n_sel - 1) : 0)];
   asm volatile("" ::"s"(len), "s"(mode_word), "s"(off_lo), "s"(off_hi), "s"(n_picked));
   const int T = min(max(len, 0), pt.max_len);
   const uint32_t mbyte = tail ? (uint32_t)kExact : (mode_word >> (8 * (u & 3))) & 0xFFu;
   const uint64_t seg_off = tail ? 0 : ((uint64_t)off_hi << 32) | off_lo;
-  const bool bad_unit = !unit_byte_ok(mbyte, P.tokres ? P.n_rates : 0) || (seg_off & (kPlaneAlign - 1));
+  const bool bad_unit = !unit_byte_ok(mbyte, KIND == kTokenSet ? P.n_rates : 0) || (seg_off & (kPlaneAlign - 1));
   const int mode = mode_of(mbyte);
   const int n_tiles = picked && T > 0 ? min(max(n_picked, 0), pt.n_sel) * S::TPB : (T + TOK - 1) / TOK;  // of the part
   if (my_block < 0 || my_block >= (T + kBlockTokens - 1) / kBlockTokens) my_block = -1;
-  const int end = min(chunk0 + P.tiles_per_wg, n_tiles);
+  const int end = min(chunk0 + tiles_per_wg, n_tiles);
   int n = chunk0 + wave < end ? (end - chunk0 - wave + 3) / 4 : 0;  // the wave's tiles: chunk0 + wave + 4 i
   if (bad_unit) n = 0;
 
@@ -878,7 +885,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   float* mg = reinterpret_cast<float*>(lds);  // [wave][column][MP]
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
-    if (P.shared && row0 + 16 * q >= rows) break;
+    if (row0 + 16 * q >= rows) break;
     __syncthreads();
     const float ls = col_sum(l[q]);
     if (lg == 0) {
