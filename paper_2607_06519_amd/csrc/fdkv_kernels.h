@@ -165,14 +165,15 @@ struct PartsParams {
   int hkv, hq, G, g_shift, n_slots, tiles_per_wg, row_groups, rows;  // rows: query rows of a sequence, or of the batch
   int n_blocks, block, slot0, shared;
   const void* q;               // [batch][hq][d]
-  PartsPart part[kMaxParts];   // this launch's parts
-  int part_base[kMaxParts];    // first slot of each, from 0; INT32_MAX past the last
-  DivU by_topk;
   float* ws;                   // records [batch][hkv][n_slots_total][G][d + 4]
   const void* tail_k;          // [batch][hkv][tail_cap][d]
   const void* tail_v;
-  int batch, pos, bsize, topk, d, tail_cap, n_slots_total;
+  DivU by_topk;
+  int pos, bsize, topk, tail_cap, n_slots_total;
   float wres[3], scale_log2;
+  int part_base[kMaxParts];    // first slot of each part, from 0; INT32_MAX past the last
+  PartsPart part[kMaxParts];   // this launch's parts
+  int batch, d;
   int res_ppm, n_rates;
   int rates_ppm[kMaxRates];
   bool tokres, bf16, coef8;

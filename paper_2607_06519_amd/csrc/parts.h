@@ -186,6 +186,14 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   asm volatile("" : "+s"(pt1.lens), "+s"(pt1.cache), "+s"(pt1.modes), "+s"(pt1.seg_off), "+s"(pt1.blocks), "+s"(pt1.counts),
                "+s"(pt1.n_sel), "+s"(pt1.max_len));
 
+  float* ws = P.ws;
+  const void *tail_k = P.tail_k, *tail_v = P.tail_v;
+  DivU by_topk = P.by_topk;
+  int pos = P.pos, nb = P.bsize, k = P.topk, tail_cap = P.tail_cap, n_slots_total = P.n_slots_total;
+  float w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2], scale_log2 = P.scale_log2;
+  asm volatile("" : "+s"(ws), "+s"(tail_k), "+s"(tail_v), "+s"(by_topk.mul), "+s"(by_topk.shift), "+s"(pos), "+s"(nb), "+s"(k),
+               "+s"(tail_cap), "+s"(n_slots_total), "+s"(w1), "+s"(w2), "+s"(w3), "+s"(scale_log2));
+
   // ---- which chunk
   uint32_t w = blockIdx.x;
   int row0 = 0;
@@ -267,12 +275,12 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   };
   // The scale's sign goes to the queries, so that a column's largest product is its largest logit; a scale of zero
   // zeroes them.  (Once the first tile is requested: the queries were before it.)
-  const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
+  const float scale = scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
   auto settle_queries = [&]() __attribute__((always_inline)) {
-    const uint32_t sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
+    const uint32_t sign = scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
     for (int i = 0; i < QR; ++i) {
-      const uint32_t keep = q_ok[i] && P.scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
+      const uint32_t keep = q_ok[i] && scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
 #pragma unroll
       for (int j = 0; j < QP; ++j) {
         uint4& v = qf[i][j];
@@ -318,18 +326,16 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
-    const int nb = P.bsize, k = P.topk;
-    const float w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2];
 
     // ---- planes
     const uint32_t dense = C8 ? ((uint32_t)T * D + kC8Block - 1) / kC8Block * kC8Block : (uint32_t)T * RB;
     const uint32_t plane = (dense + kPlaneAlign - 1) / kPlaneAlign * kPlaneAlign;
-    const uint8_t* kb = seg + (uint64_t)(mode == kExact ? P.pos : 0) * plane;
+    const uint8_t* kb = seg + (uint64_t)(mode == kExact ? pos : 0) * plane;
     const uint8_t* vb = kb + (uint64_t)(mode == kExact ? nb : 1) * plane;
     if (tail) {
-      const uint64_t off = ((uint64_t)seq * hkv + head) * (uint64_t)P.tail_cap * RB;
-      kb = static_cast<const uint8_t*>(P.tail_k) + off;
-      vb = static_cast<const uint8_t*>(P.tail_v) + off;
+      const uint64_t off = ((uint64_t)seq * hkv + head) * (uint64_t)tail_cap * RB;
+      kb = static_cast<const uint8_t*>(tail_k) + off;
+      vb = static_cast<const uint8_t*>(tail_v) + off;
     }
     const auto kr = rsrc(kb, dense), vr = rsrc(vb, dense);
     // residual entries
@@ -448,7 +454,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     auto place = [&](const Entries& e, int chunk, int held, Placed& p) __attribute__((always_inline)) {  // held: tokens of the tile
       const bool live = chunk < TOK / 8 * k;
       const int e0 = 8 * chunk;
-      int t = (int)P.by_topk.div((uint32_t)e0), j = e0 - t * k;  // token of the tile, entry of the token
+      int t = (int)by_topk.div((uint32_t)e0), j = e0 - t * k;  // token of the tile, entry of the token
       uint32_t base[8], perm[8];  // of an entry's row: its first byte, the permutation of its channels
       bool starts[10];            // the entry is its token's first
 #pragma unroll
@@ -864,7 +870,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   using std::integral_constant;
   using no = integral_constant<bool, false>;
   using yes = integral_constant<bool, true>;
-  const bool res = mode == kResidual && (KIND == kTokenSet || P.topk > 0);
+  const bool res = mode == kResidual && (KIND == kTokenSet || k > 0);
   if (chunk0 < end && !bad_unit) {  // (the whole workgroup: the walk has a barrier)
     if constexpr (TY == kTyC8) {
       if (mode == kExact)
@@ -908,7 +914,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         wt[w] = merge_weight(ml_lds[w][col][0], M);
         lt = fmaf(wt[w], ml_lds[w][col][1], lt);
       }
-      float* rec = P.ws + ((((uint64_t)sq * hkv + head) * P.n_slots_total + slot) * G + g) * RS;
+      float* rec = ws + ((((uint64_t)sq * hkv + head) * n_slots_total + slot) * G + g) * RS;
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         const int ch = 64 * c + 4 * part16;
