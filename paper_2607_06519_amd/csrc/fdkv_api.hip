@@ -930,12 +930,24 @@ struct PartsPlan {
   int n_own, n_shared;          // parts (the tail among the own ones)
   int own[kMaxParts], shared[kMaxParts];  // their indices in the call; -1: the tail
   int own_tiles_per_wg, shared_tiles_per_wg, nq, rows, row_groups;
+  int res_cost;                 // PartsParams::res_cost
+  int64_t shared_wgs;           // workgroups of a row group and head of the shared parts, on average
   int64_t slots[kMaxParts];     // record slots of each part, own ones first
   int64_t own_slots, total_slots;
 };
 
 // Workgroups that fill the card: two of up to 16 query rows to a CU, or one of more.
 constexpr int64_t kPartsWorkgroups = 512;
+
+// A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
+// dimension 128): one head's share of the workgroups.
+int parts_res_cost(const fdkv_dims* dims) {
+  const bool quads = dims->schedule != FDKV_SCHED_PAIRS;
+  if (tokens_mode(dims)) return quads ? 32 : 24;
+  if (dims->topk == 0) return 16;
+  if (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16)) return 48;
+  return quads ? 34 : 21;
+}
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
                        PartsPlan* out) {
@@ -983,7 +995,15 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {
     const int64_t n = ((int64_t)parts[p.shared[i]].max_seq_len + tok - 1) / tok;
-    p.total_slots += p.slots[p.n_own + i] = (n + p.shared_tiles_per_wg - 1) / p.shared_tiles_per_wg;
+    p.shared_wgs += p.slots[p.n_own + i] = (n + p.shared_tiles_per_wg - 1) / p.shared_tiles_per_wg;
+  }
+  p.total_slots += p.shared_wgs;
+  // One shared part: its workgroups are dealt to the heads by cost, so a residual head may take more record slots than
+  // the average, at most as many as if it were the only one.  (With few workgroups a head the shares round too far.)
+  if (p.n_shared == 1 && hkv <= 64 && p.shared_wgs >= 4 && p.shared_wgs * hkv < (1 << 20)) {
+    p.res_cost = parts_res_cost(dims);
+    p.slots[p.n_own] = p.shared_wgs * hkv * p.res_cost / (p.res_cost + 16 * (hkv - 1)) + 1;
+    p.total_slots = p.own_slots + p.slots[p.n_own];
   }
   // workgroups and record slots are counted in 31 bits
   if (batch * hkv * std::max<int64_t>(p.total_slots, 1) >= (1ll << 31) ||
@@ -993,8 +1013,13 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   return FDKV_OK;
 }
 
-uint64_t parts_bytes(const fdkv_dims* dims, int32_t batch, const PartsPlan& p) {
+uint64_t parts_record_bytes(const fdkv_dims* dims, int32_t batch, const PartsPlan& p) {
   return (uint64_t)batch * dims->n_kv_heads * std::max<int64_t>(p.total_slots, 1) * record_bytes(dims);
+}
+
+uint64_t parts_bytes(const fdkv_dims* dims, int32_t batch, const PartsPlan& p) {
+  // records, then the shared slots of each head
+  return parts_record_bytes(dims, batch, p) + (p.res_cost ? plane_bytes((uint64_t)dims->n_kv_heads * 4) : 0);
 }
 
 hipError_t launch_parts(const PartsParams& p, hipStream_t s) {
@@ -1082,7 +1107,7 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
   for (int shared = 0; shared < 2; ++shared) {  // a launch for the parts of single sequences, one for the shared ones
     const int n = shared ? plan.n_shared : plan.n_own;
     const int64_t* slots = plan.slots + (shared ? plan.n_own : 0);
-    p.n_slots = (int)(shared ? plan.total_slots - plan.own_slots : plan.own_slots);
+    p.n_slots = (int)(shared ? plan.shared_wgs : plan.own_slots);
     if (p.n_slots == 0) continue;
     int base = 0;
     for (int i = 0; i < kMaxParts; ++i) {
@@ -1110,6 +1135,8 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
       }
     }
     p.shared = shared;
+    p.res_cost = shared ? plan.res_cost : 0;
+    p.shared_counts = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + parts_record_bytes(dims, batch, plan));
     p.nq = shared ? plan.nq : 1;
     p.rows = shared ? plan.rows : p.G;
     p.row_groups = shared ? plan.row_groups : 1;
@@ -1120,18 +1147,22 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
     const hipError_t e = launch_parts(p, s);
     if (e != hipSuccess) return hip_fail(e, "decode_parts");
   }
-  DecodeParams mp{};
-  mp.out = out;
+  PartsMergeParams mp{};
+  mp.by_hq.set((uint32_t)p.hq);
   mp.ws = p.ws;
-  mp.hkv = p.hkv;
-  mp.hq = p.hq;
-  mp.d = p.d;
+  mp.shared_counts = plan.res_cost ? p.shared_counts : nullptr;
+  mp.own_slots = (int)plan.own_slots;
+  mp.n_slots_total = p.n_slots_total;
   mp.batch = batch;
+  mp.hq = p.hq;
+  mp.hkv = p.hkv;
+  mp.G = p.G;
+  mp.g_shift = p.g_shift;
+  mp.d = p.d;
   mp.bf16 = p.bf16;
-  mp.n_chunks_total = p.n_slots_total;
-  mp.n_sub = 1;
-  const hipError_t e = launch_decode_merge(mp, s);
-  if (e != hipSuccess) return hip_fail(e, "decode_merge");
+  mp.out = out;
+  const hipError_t e = launch_parts_merge(mp, s);
+  if (e != hipSuccess) return hip_fail(e, "parts_merge");
   return FDKV_OK;
 }
 

@@ -164,6 +164,9 @@ struct PartsParams {
   DivU by_slots, by_hkv, by_groups;
   int hkv, hq, G, g_shift, n_slots, tiles_per_wg, row_groups, rows;  // rows: query rows of a sequence, or of the batch
   int n_blocks, block, slot0, shared;
+  int res_cost;                // a residual head's time per token, a plain one's being 16; 0: every head takes n_slots
+                               // workgroups (shared parts only)
+  int* shared_counts;          // [hkv] out: record slots that a head of the shared part fills (res_cost > 0)
   const void* q;               // [batch][hq][d]
   float* ws;                   // records [batch][hkv][n_slots_total][G][d + 4]
   const void* tail_k;          // [batch][hkv][tail_cap][d]
@@ -178,6 +181,15 @@ struct PartsParams {
   int rates_ppm[kMaxRates];
   bool tokres, bf16, coef8;
   int nq;                      // column tiles of a wave (16 query rows each): 1, 2 or 4
+};
+
+struct PartsMergeParams {
+  DivU by_hq;
+  const float* ws;             // records [batch][hkv][n_slots_total][G][d + 4]
+  const int* shared_counts;    // [hkv] slots in use after the first own_slots, or null: all of n_slots_total
+  int own_slots, n_slots_total, batch, hq, hkv, G, g_shift, d;
+  bool bf16;
+  void* out;                   // [batch][hq][d]
 };
 
 // generation: append one token's K / V rows of one layer to the exact tail
@@ -267,6 +279,7 @@ hipError_t launch_parts_bf16_d64(const PartsParams& P, hipStream_t s);
 hipError_t launch_parts_bf16_d128(const PartsParams& P, hipStream_t s);
 hipError_t launch_parts_c8_d64(const PartsParams& P, hipStream_t s);
 hipError_t launch_parts_c8_d128(const PartsParams& P, hipStream_t s);
+hipError_t launch_parts_merge(const PartsMergeParams& P, hipStream_t s);
 hipError_t launch_append(const AppendParams& P, hipStream_t s);
 hipError_t launch_rope_append(const RopeParams& P, hipStream_t s);
 hipError_t launch_key_bounds(const BoundsParams& P, hipStream_t s);

@@ -174,13 +174,13 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   // piece a trip to memory)
   DivU by_slots = P.by_slots, by_hkv = P.by_hkv, by_groups = P.by_groups;
   int hkv = P.hkv, hq = P.hq, G = P.G, g_shift = P.g_shift, n_slots = P.n_slots, tiles_per_wg = P.tiles_per_wg;
-  int row_groups = P.row_groups, rows = P.rows, n_blocks = P.n_blocks, block = P.block, slot0 = P.slot0, shared = P.shared;
+  int res_cost = P.res_cost, row_groups = P.row_groups, rows = P.rows, n_blocks = P.n_blocks, block = P.block, slot0 = P.slot0, shared = P.shared;
   const void* q_all = P.q;
   PartsPart pt = P.part[0], pt1 = P.part[1];
   int base1 = P.part_base[1], base2 = P.part_base[2];
   asm volatile("" : "+s"(by_slots.mul), "+s"(by_slots.shift), "+s"(by_hkv.mul), "+s"(by_hkv.shift), "+s"(by_groups.mul),
                "+s"(by_groups.shift), "+s"(hkv), "+s"(hq), "+s"(G), "+s"(g_shift), "+s"(n_slots), "+s"(tiles_per_wg),
-               "+s"(row_groups), "+s"(rows));
+               "+s"(row_groups), "+s"(rows), "+s"(res_cost));
   asm volatile("" : "+s"(n_blocks), "+s"(block), "+s"(slot0), "+s"(shared), "+s"(q_all), "+s"(base1), "+s"(base2), "+s"(pt.lens),
                "+s"(pt.cache), "+s"(pt.modes), "+s"(pt.seg_off), "+s"(pt.blocks), "+s"(pt.counts), "+s"(pt.n_sel), "+s"(pt.max_len));
   asm volatile("" : "+s"(pt1.lens), "+s"(pt1.cache), "+s"(pt1.modes), "+s"(pt1.seg_off), "+s"(pt1.blocks), "+s"(pt1.counts),
@@ -205,8 +205,25 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     if (w >= (uint32_t)(hkv * n_slots)) return;
   }
   const uint32_t sl = by_hkv.div(w);
-  const int head = (int)(w - sl * hkv), seq = (int)by_slots.div(sl);  // (shared: sequence 0)
-  int slot = (int)sl - seq * n_slots, chunk0 = slot;
+  int head = (int)(w - sl * hkv), seq = (int)by_slots.div(sl);  // (shared: sequence 0)
+  int slot = (int)sl - seq * n_slots, chunk0 = slot, head_slots = 0;
+  if (res_cost) {
+    // A residual head's tokens take longer, and one workgroup to a CU is all there is: the workgroups go to the heads
+    // by what their tokens take.  Lane h: head h.
+    const uint32_t b = lane < hkv ? pt.modes[block * hkv + lane] : 0u;
+    uint32_t c = lane < hkv ? (mode_of(b) == kResidual ? (uint32_t)res_cost : 16u) : 0u;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const uint32_t y = __shfl_up(c, o, 64);
+      c += lane >= o ? y : 0u;
+    }
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)c, 63);
+    const uint32_t end = (uint32_t)(hkv * n_slots) * c / total;  // first workgroup behind head h's
+    head = __builtin_popcountll(__ballot(lane < hkv && end <= w));
+    const int from = head ? __builtin_amdgcn_readlane((int)end, head - 1) : 0;
+    head_slots = __builtin_amdgcn_readlane((int)end, head) - from;
+    slot = chunk0 = (int)w - from;
+  }
   if (slot >= base1) {
     pt = pt1;
     chunk0 = slot - base1;
@@ -217,7 +234,6 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       chunk0 = slot - P.part_base[i];
     }
   }
-  chunk0 *= tiles_per_wg;  // the chunk's first tile
   slot += slot0;
   const bool tail = pt.cache == nullptr, picked = pt.n_sel > 0;
 
@@ -255,6 +271,8 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   const int len = as_const(pt.lens)[seq];
   const uint32_t mode_word = words[u >> 2], off_lo = offs[2 * u], off_hi = offs[tail ? 0 : 2 * u + 1];
   const int n_picked = as_const(pt.counts)[unit];
+  if (res_cost) tiles_per_wg = ((min(max(len, 0), pt.max_len) + TOK - 1) / TOK + 4 * head_slots - 1) / (4 * head_slots) * 4;
+  chunk0 *= tiles_per_wg;  // the chunk's first tile
   int my_block = pt.blocks[unit * pt.n_sel + (picked ? min((chunk0 + wave + 4 * lane) / S::TPB, pt.n_sel - 1) : 0)];
   asm volatile("" ::"s"(len), "s"(mode_word), "s"(off_lo), "s"(off_hi), "s"(n_picked));
   const int T = min(max(len, 0), pt.max_len);
@@ -886,6 +904,8 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         walk(no{}, no{});
     }
   }
+
+  if (res_cost && slot == slot0 && row0 == 0 && threadIdx.x == 0) P.shared_counts[head] = head_slots;
 
   // ---- the waves' records of a column tile meet in LDS, one tile after the other
   float* mg = reinterpret_cast<float*>(lds);  // [wave][column][MP]

@@ -108,8 +108,9 @@ def test_decode_parts_refuses(lib):
     assert lib.fdkv_decode_parts_workspace(ctypes.byref(dm), 1 << 30, 0, None, -1, ctypes.byref(n)) == -2
 
 
-def test_parts_workspace_covers_every_length(lib):
-    """The split of a call goes by its bounds alone: a bound's workspace is the same whatever the lengths."""
+def test_parts_workspace(lib):
+    """Records of every part's slots, a slot at least per 64 tokens of the bound (a shared part: or as many as one
+    residual head among plain ones may take), and never less for a longer bound at the same split."""
     for dtype in ("bf16", "f32", "bf16_e4m3"):
         dm = B.dims(2, 8, 32, 128, 16, dtype)
         rec = 4 * 132 * 4
@@ -118,4 +119,5 @@ def test_parts_workspace_covers_every_length(lib):
                 for T in (0, 1, 32, 33, 5000, 131072):
                     n = B.decode_parts_workspace(dm, batch, [_part(kind, T)], -1)
                     slots = n // (batch * 8 * rec)
-                    assert n % (batch * 8 * rec) == 0 and 1 <= slots <= max(1, -(-T // 64))
+                    assert 1 <= slots <= max(1, -(-T // 64)) * (3 if kind == 2 else 1) + 1
+                    assert n - slots * batch * 8 * rec in (0, 256)
