@@ -943,10 +943,10 @@ constexpr int64_t kPartsWorkgroups = 512;
 // dimension 128): one head's share of the workgroups.
 int parts_res_cost(const fdkv_dims* dims) {
   const bool quads = dims->schedule != FDKV_SCHED_PAIRS;
-  if (tokens_mode(dims)) return quads ? 32 : 24;
+  if (tokens_mode(dims)) return quads ? 36 : 29;
   if (dims->topk == 0) return 16;
   if (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16)) return 48;
-  return quads ? 34 : 21;
+  return quads ? 38 : 26;
 }
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,

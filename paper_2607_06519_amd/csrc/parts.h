@@ -160,7 +160,6 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
   constexpr int RS = D + 4;
   constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
-  constexpr int DEPTH = NQ == 2 && KIND != kManyEntries ? 2 : 1;  // tiles in flight behind the current one
   constexpr int kWaveLds = 2 * S::TILE_BYTES + RB;  // the V tile, R, and a row of R that takes what has no place
   static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
   // the queries of 64 columns stay in LDS (registers would not hold them besides the sums)
@@ -341,6 +340,8 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     constexpr bool C8 = decltype(c8_tag)::value;       // shared planes and residual values in E4M3
     constexpr int RES = decltype(res_tag)::value ? KIND : 0;
     constexpr bool ENT = RES == kFewEntries || RES == kManyEntries, SET = RES == kTokenSet;
+    // tiles in flight behind the current one
+    constexpr int DEPTH = NQ == 2 && RES != kManyEntries ? 2 : 1;
     constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
@@ -754,8 +755,10 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
           constexpr int half = kC8Block / D / 2;
           const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
           uint4 x = widen8(b.vv[i].x, b.vv[i].y), y = widen8(b.vv[i].z, b.vv[i].w);
-          if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
-          if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+          if (edge) {
+            if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
+            if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+          }
           *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = x;
           *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = y;
         } else {
