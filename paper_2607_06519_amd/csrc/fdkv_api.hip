@@ -929,14 +929,14 @@ namespace {
 struct PartsPlan {
   int n_own, n_shared;          // parts (the tail among the own ones)
   int own[kMaxParts], shared[kMaxParts];  // their indices in the call; -1: the tail
-  int own_tiles_per_wg, shared_tiles_per_wg, nq, rows, row_groups;
+  int own_tiles_per_wg, shared_tiles_per_wg, cols, rows, row_groups;
   int res_cost;                 // PartsParams::res_cost
   int64_t shared_wgs;           // workgroups of a row group and head of the shared parts, on average
   int64_t slots[kMaxParts];     // record slots of each part, own ones first
   int64_t own_slots, total_slots;
 };
 
-// Workgroups that fill the card: two of up to 16 query rows to a CU, or one of more.
+// Workgroups that fill the card: two to a CU.
 constexpr int64_t kPartsWorkgroups = 512;
 
 // A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
@@ -979,18 +979,17 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
     own_tiles += tiles[p.n_own];
     p.own[p.n_own++] = -1;
   }
-  auto per_wg = [](int64_t tiles, int64_t groups, int64_t most) {
+  auto per_wg = [](int64_t tiles, int64_t groups, int64_t each, int64_t most) {  // each: token groups of a workgroup
     const int64_t n = (tiles + std::max<int64_t>(groups, 1) - 1) / std::max<int64_t>(groups, 1);
-    return (int)std::min<int64_t>(most, std::max<int64_t>(4, (n + 3) / 4 * 4));
+    return (int)std::min<int64_t>(most, std::max<int64_t>(1, (n + each - 1) / each) * each);
   };
   // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
-  p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 256);
+  p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 4, 256);
   p.rows = (int)(batch * G);
-  // (the kernels of many entries and 64 columns do not fit the registers together)
-  const bool many = dims->residual == FDKV_RES_CHANNELS && (dims->topk % 8 || tok / 8 * dims->topk > 64);
-  p.nq = p.rows <= 16 ? 1 : p.rows <= 32 || many ? 2 : 4;
-  p.row_groups = (p.rows + 16 * p.nq - 1) / (16 * p.nq);
-  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (p.nq > 1 ? 2 : 1) / (hkv * p.row_groups), 1 << 28);
+  p.cols = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+  p.row_groups = (p.rows + p.cols - 1) / p.cols;
+  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (hkv * p.row_groups),
+                                 p.cols == 16 ? 4 : p.cols == 128 ? 1 : 2, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {
@@ -1137,7 +1136,7 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
     p.shared = shared;
     p.res_cost = shared ? plan.res_cost : 0;
     p.shared_counts = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + parts_record_bytes(dims, batch, plan));
-    p.nq = shared ? plan.nq : 1;
+    p.cols = shared ? plan.cols : 16;
     p.rows = shared ? plan.rows : p.G;
     p.row_groups = shared ? plan.row_groups : 1;
     p.tiles_per_wg = shared ? plan.shared_tiles_per_wg : plan.own_tiles_per_wg;

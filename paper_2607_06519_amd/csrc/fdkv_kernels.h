@@ -180,7 +180,7 @@ struct PartsParams {
   int res_ppm, n_rates;
   int rates_ppm[kMaxRates];
   bool tokres, bf16, coef8;
-  int nq;                      // column tiles of a wave (16 query rows each): 1, 2 or 4
+  int cols;                    // query rows of a workgroup: 16, 32, 64 or 128
 };
 
 struct PartsMergeParams {

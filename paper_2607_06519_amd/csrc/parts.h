@@ -150,25 +150,32 @@ enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
 
 // Workgroups to a CU that the registers have to leave room for.  A spill in the
 // walk would wait for every load in flight.
-constexpr int parts_per_cu(int NQ, int KIND, bool q4) { return NQ == 1 && !(KIND == kManyEntries && q4) ? 2 : 1; }
+constexpr int parts_per_cu(int KIND, bool q4) { return KIND == kManyEntries && q4 ? 1 : 2; }
 
-template <int D, int NQ, int TY, int KIND, bool q4>
-__global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(PartsParams P) {
+// CG column groups of 16 NQ columns each, a wave apiece, by TG = 4 / CG token
+// groups.  With CG > 1 the waves of a token group walk the same tiles: each
+// stages its share of V, one places the residual entries of K, one those of V
+// (one the rest of K's), and two barriers a tile hand the tiles over.
+template <int D, int NQ, int CG, int TY, int KIND, bool q4>
+__global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(PartsParams P) {
   using namespace parts;
   using S = TileOf<D, TY>;
   constexpr bool F32 = S::F32;
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
+  constexpr int TG = 4 / CG, COLS = 16 * NQ * CG;
   constexpr int RS = D + 4;
   constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
-  constexpr int kWaveLds = 2 * S::TILE_BYTES + RB;  // the V tile, R, and a row of R that takes what has no place
-  static_assert(4 * 16 * MP * 4 <= 4 * kWaveLds, "the merge of a column tile fits the tiles' space");
-  // the queries of 64 columns stay in LDS (registers would not hold them besides the sums)
-  constexpr bool QL = NQ == 4;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kWaveLds + (QL ? 16 * NQ * RB : 0)];
+  // a token group's LDS: the V tile, then R (CG > 1: of K, of V and, where K's has one, of K's rest), each with a row
+  // behind it that takes what has no place
+  constexpr bool REST = q4 && !F32;  // K's residual has a bf16 rest
+  constexpr int kRt = S::TILE_BYTES + RB, kGroupLds = S::TILE_BYTES + (CG == 1 ? 1 : REST ? 3 : 2) * kRt;
+  constexpr int kLds = TG * kGroupLds > 4 * 16 * MP * 4 ? TG * kGroupLds : 4 * 16 * MP * 4;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
   __shared__ float ml_lds[4][16][2];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, lane = threadIdx.x & 63;
   const int lc = lane & 15, lg = lane >> 4;  // column (or operand row) and lane group
+  const int tg = wave / CG, cg = wave % CG;
   // ---- what the launch says, fetched in one go and kept (left to itself the compiler reads it piece by piece, each
   // piece a trip to memory)
   DivU by_slots = P.by_slots, by_hkv = P.by_hkv, by_groups = P.by_groups;
@@ -199,7 +206,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   if (shared) {
     // the row groups of one chunk follow each other on one XCD (workgroups go to the XCDs in turn)
     const uint32_t y = w >> 3, ym = by_groups.div(y);
-    row0 = (int)(y - ym * row_groups) * 16 * NQ;
+    row0 = (int)(y - ym * row_groups) * COLS;
     w = ym * 8 + (w & 7u);
     if (w >= (uint32_t)(hkv * n_slots)) return;
   }
@@ -246,18 +253,15 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   auto q_row = [&](int s, int g) __attribute__((always_inline)) {
     return reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q_all) + ((uint64_t)s * hq + (uint64_t)head * G + g) * RB);
   };
-  // 64 columns: the thread's share on its way into LDS; else the lane's column of each column tile
-  constexpr int QR = QL ? 16 * NQ * NP / 256 : NQ, QP = QL ? 1 : KK;
-  uint4 qf[QR][QP];
-  bool q_ok[QR];
+  uint4 qf[NQ][KK];
+  bool q_ok[NQ];
 #pragma unroll
-  for (int i = 0; i < QR; ++i) {
+  for (int i = 0; i < NQ; ++i) {
     int s, g;
-    const int at = threadIdx.x + 256 * i;
-    q_ok[i] = row_of(QL ? at / NP : 16 * i + lc, s, g);
+    q_ok[i] = row_of(16 * (cg * NQ + i) + lc, s, g);
     const uint4* src = q_row(s, g);
 #pragma unroll
-    for (int j = 0; j < QP; ++j) qf[i][j] = src[QL ? at % NP : 4 * j + lg];
+    for (int j = 0; j < KK; ++j) qf[i][j] = src[4 * j + lg];
   }
 
   // ---- what the unit's arrays say, requested in one go: a length, the mode's word, the segment's offset, the number
@@ -270,9 +274,9 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   const int len = as_const(pt.lens)[seq];
   const uint32_t mode_word = words[u >> 2], off_lo = offs[2 * u], off_hi = offs[tail ? 0 : 2 * u + 1];
   const int n_picked = as_const(pt.counts)[unit];
-  if (res_cost) tiles_per_wg = ((min(max(len, 0), pt.max_len) + TOK - 1) / TOK + 4 * head_slots - 1) / (4 * head_slots) * 4;
+  if (res_cost) tiles_per_wg = ((min(max(len, 0), pt.max_len) + TOK - 1) / TOK + TG * head_slots - 1) / (TG * head_slots) * TG;
   chunk0 *= tiles_per_wg;  // the chunk's first tile
-  int my_block = pt.blocks[unit * pt.n_sel + (picked ? min((chunk0 + wave + 4 * lane) / S::TPB, pt.n_sel - 1) : 0)];
+  int my_block = pt.blocks[unit * pt.n_sel + (picked ? min((chunk0 + tg + TG * lane) / S::TPB, pt.n_sel - 1) : 0)];
   asm volatile("" ::"s"(len), "s"(mode_word), "s"(off_lo), "s"(off_hi), "s"(n_picked));
   const int T = min(max(len, 0), pt.max_len);
   const uint32_t mbyte = tail ? (uint32_t)kExact : (mode_word >> (8 * (u & 3))) & 0xFFu;
@@ -282,39 +286,23 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   const int n_tiles = picked && T > 0 ? min(max(n_picked, 0), pt.n_sel) * S::TPB : (T + TOK - 1) / TOK;  // of the part
   if (my_block < 0 || my_block >= (T + kBlockTokens - 1) / kBlockTokens) my_block = -1;
   const int end = min(chunk0 + tiles_per_wg, n_tiles);
-  int n = chunk0 + wave < end ? (end - chunk0 - wave + 3) / 4 : 0;  // the wave's tiles: chunk0 + wave + 4 i
-  if (bad_unit) n = 0;
+  // the wave's tiles: chunk0 + tg + TG i, i < n (CG > 1: the same number for every wave, for the barriers)
+  const int n = CG == 1 ? (chunk0 + tg < end ? (end - chunk0 - tg + TG - 1) / TG : 0) : (end - chunk0 + TG - 1) / TG;
 
-  // piece of a column's query in LDS, permuted by the column against bank conflicts
-  auto q_at = [&](int q, int col, int piece) __attribute__((always_inline)) {
-    const int f = NP == 8 ? col >> 1 : col;
-    return lds + 4 * kWaveLds + (16 * q + col) * RB + ((piece ^ f) << 4);
-  };
   // The scale's sign goes to the queries, so that a column's largest product is its largest logit; a scale of zero
   // zeroes them.  (Once the first tile is requested: the queries were before it.)
   const float scale = scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
   auto settle_queries = [&]() __attribute__((always_inline)) {
     const uint32_t sign = scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
-    for (int i = 0; i < QR; ++i) {
+    for (int i = 0; i < NQ; ++i) {
       const uint32_t keep = q_ok[i] && scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
 #pragma unroll
-      for (int j = 0; j < QP; ++j) {
+      for (int j = 0; j < KK; ++j) {
         uint4& v = qf[i][j];
         v = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
-        if constexpr (QL) {
-          const int at = threadIdx.x + 256 * i, col = at / NP;
-          *reinterpret_cast<uint4*>(q_at(col / 16, col % 16, at % NP)) = v;
-        }
       }
     }
-    if constexpr (QL) __syncthreads();
-  };
-  auto query = [&](int q, int kk) __attribute__((always_inline)) -> uint4 {
-    if constexpr (QL)
-      return *reinterpret_cast<const uint4*>(q_at(q, lc, 4 * kk + lg));
-    else
-      return qf[QL ? 0 : q][QL ? 0 : kk];
   };
 
   float m[NQ], l[NQ];
@@ -327,8 +315,19 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     for (int c = 0; c < CT; ++c) acc[q][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  uint8_t* vt = lds + wave * kWaveLds;                 // the V tile
-  uint8_t* rt = vt + S::TILE_BYTES;                    // R
+  uint8_t* vt = lds + tg * kGroupLds;                  // the V tile
+  uint8_t* r_k = vt + S::TILE_BYTES;                   // R of K, of V, of K's rest (CG == 1: one after the other)
+  uint8_t* r_v = CG == 1 ? r_k : r_k + kRt;
+  uint8_t* r_rest = CG == 1 ? r_k : r_k + 2 * kRt;
+  // CG > 1: the wave's tile of R (0: K, 1: V, 2: K's rest; CG == 2: wave 0 has K's rest too)
+  const int role = CG == 1 ? 0 : cg, roles = CG == 4 && REST ? 3 : 2;
+  uint8_t* rt = r_k + (CG == 1 ? 0 : role < roles ? role : 0) * kRt;
+  // Hands LDS tiles from the waves that wrote them to those that read them.
+  auto hand_over = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    lds_fence();
+  };
   const uint8_t* seg = pt.cache + seg_off;
 
   // The walk is compiled for each kind of unit, so that every load of a tile is
@@ -341,7 +340,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     constexpr int RES = decltype(res_tag)::value ? KIND : 0;
     constexpr bool ENT = RES == kFewEntries || RES == kManyEntries, SET = RES == kTokenSet;
     // tiles in flight behind the current one
-    constexpr int DEPTH = NQ == 2 && RES != kManyEntries ? 2 : 1;
+    constexpr int DEPTH = 1;
     constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
@@ -364,7 +363,10 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     // (whole 16-byte pieces: a load whose last word lies half behind the bytes would read 0 for all of it.  The
     // plane's padding may hold anything; entries of tokens behind the last are not used.)
     const uint32_t ibr = (ib + 15) & ~15u, xbr = (xb + 15) & ~15u;
-    const auto ikr = rsrc(ent, ibr), xkr = rsrc(ent + ip, xbr);
+    // (CG > 1: the wave reads the entries of its role, K's or V's, into what is K's buffer here)
+    const uint64_t k_at = CG > 1 && role == 1 ? (uint64_t)ip + xp : 0;
+    const uint32_t live = CG > 1 && role >= roles ? 0u : ~0u;
+    const auto ikr = rsrc(ent + k_at, ibr & live), xkr = rsrc(ent + k_at + ip, xbr & live);
     const auto ivr = rsrc(ent + ip + xp, ibr), xvr = rsrc(ent + 2 * (uint64_t)ip + xp, xbr);
     // token-level set
     TokLayout L{};
@@ -374,36 +376,43 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       L = tok_layout(mode, (uint64_t)T, D, ppm, S::E, C, nb);
       set_bytes = residual_token_count((uint64_t)T, ppm) * (uint64_t)(nb - 1) * D * C;
     }
-    const auto hkr = rsrc(seg + L.hk, set_bytes), hvr = rsrc(seg + L.hv, set_bytes);
+    const auto hkr = rsrc(seg + (CG > 1 && role == 1 ? L.hv : L.hk), CG > 1 && role >= roles ? 0 : set_bytes);
+    const auto hvr = rsrc(seg + L.hv, set_bytes);
     const auto* mask_words = as_const(reinterpret_cast<const uint32_t*>(seg + L.mask));
     const auto* counts = as_const(reinterpret_cast<const uint32_t*>(seg + L.count));
 
     // ---- the wave's tiles
     // first token of the wave's tile i; T where it has none (every load reads zeros, every token is masked)
     auto tile_token = [&](int i) __attribute__((always_inline)) -> int {
-      const int u = chunk0 + wave + 4 * i;
+      const int u = chunk0 + tg + TG * i;
       int t = u * TOK;
       if (picked) {
         const int b = __builtin_amdgcn_readlane(my_block, i & 63);
         t = b < 0 ? T : b * kBlockTokens + (u % S::TPB) * TOK;
       }
-      return i < n ? t : T;
+      return i < n && u < end ? t : T;
     };
 
     // ---- loads
-    auto load_tile = [&](const __amdgpu_buffer_rsrc_t& r, int t0, uint32_t lane_off, uint4 (&x)[NLD], bool operand) {
+    auto load_k = [&](int t0, uint32_t lane_off, uint4 (&x)[NLD]) __attribute__((always_inline)) {
       const uint32_t base = t0 < T ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
         uint32_t step;
-        if (!operand)
-          step = (uint32_t)i * 1024;
-        else if constexpr (C8 || F32)
+        if constexpr (C8 || F32)
           step = (uint32_t)i * 64;                                          // the next pieces of the row(s)
         else
           step = (uint32_t)(i / KK) * (quad_row<D, TY>(0, 1) * RB) + (uint32_t)(i % KK) * 64;
-        x[i] = ld128<0>(r, base + lane_off + step);
+        x[i] = ld128<0>(kr, base + lane_off + step);
       }
+    };
+    // V row by row: the wave's share of the tile's loads
+    constexpr int VLD = NLD > CG ? NLD / CG : 1;
+    const bool v_live = cg * VLD < NLD;
+    auto load_v = [&](int t0, uint4 (&x)[VLD]) __attribute__((always_inline)) {
+      const uint32_t base = t0 < T && v_live ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
+#pragma unroll
+      for (int i = 0; i < VLD; ++i) x[i] = ld128<0>(vr, base + (uint32_t)lane * 16 + (uint32_t)(cg * VLD + i) * 1024);
     };
     // K in the operand's layout: lane (lc, lg) holds pieces 4 kk + lg of its token(s)
     uint32_t k_off;
@@ -413,7 +422,6 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     } else {
       k_off = (uint32_t)((quad_row<D, TY>(lc >> 2, 0) + (lc & 3)) * RB + lg * 16);
     }
-    const uint32_t v_off = (uint32_t)lane * 16;
 
     auto load_entries = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, int chunk, Entries& e) __attribute__((always_inline)) {
       const uint32_t e0 = (uint32_t)t0 * k + 8u * (uint32_t)chunk;
@@ -534,7 +542,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       }
     };
     // rest: what the bf16 rounding of the values leaves
-    auto store = [&](const Placed& p, bool rest) __attribute__((always_inline)) {
+    auto store = [&](uint8_t* rt, const Placed& p, bool rest) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if constexpr (F32) {
@@ -552,16 +560,16 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 #pragma unroll
       for (int i = 0; i < NCH; ++i) place(e[i], lane + 64 * i, T - t0, placed[i]);
     };
-    auto scatter = [&](const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, bool rest) __attribute__((always_inline)) {
+    auto scatter = [&](uint8_t* rt, const __amdgpu_buffer_rsrc_t& ir, const __amdgpu_buffer_rsrc_t& xr, int t0, bool rest) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) store(placed[i], rest);
+      for (int i = 0; i < NCH; ++i) store(rt, placed[i], rest);
       if constexpr (RES == kManyEntries) {
         for (int c = lane + 64 * NCH; c < TOK / 8 * k; c += 64) {
           Entries f;
           load_entries(ir, xr, t0, c, f);
           Placed p;
           place(f, c, T - t0, p);
-          store(p, rest);
+          store(rt, p, rest);
         }
       }
     };
@@ -602,7 +610,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     };
     // The rows into R: the lane's is that of the (lane / NP)-th set bit of `left`, which loses RPL bits.  A lane past
     // the set writes to the row behind R.
-    auto put_rows = [&](const SetRows& x, uint32_t& left, bool rest) __attribute__((always_inline)) {
+    auto put_rows = [&](uint8_t* rt, const SetRows& x, uint32_t& left, bool rest) __attribute__((always_inline)) {
       int t = TOK;
 #pragma unroll
       for (int i = 0; i < RPL; ++i) {
@@ -636,16 +644,16 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       }
       *reinterpret_cast<uint4*>(rt + piece_at<D, TY>(t, lane % NP)) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
     };
-    auto set_rows = [&](const __amdgpu_buffer_rsrc_t& r, const SetRows& x, uint32_t mw, uint32_t rank, bool rest) __attribute__((always_inline)) {
+    auto set_rows = [&](uint8_t* rt, const __amdgpu_buffer_rsrc_t& r, const SetRows& x, uint32_t mw, uint32_t rank, bool rest) __attribute__((always_inline)) {
       uint32_t left = mw;
-      put_rows(x, left, rest);
+      put_rows(rt, x, left, rest);
       for (int from = RPL; left; from += RPL) {  // more rows than travel ahead: loaded where they are used
         SetRows y;
         load_rows(r, mw, rank, from, y);
-        put_rows(y, left, rest);
+        put_rows(rt, y, left, rest);
       }
     };
-    auto clear_r = [&]() __attribute__((always_inline)) {
+    auto clear_r = [&](uint8_t* rt) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) *reinterpret_cast<uint4*>(rt + i * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
     };
@@ -671,13 +679,13 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         for (int i = 0; i < TI; ++i) a[i] = piece(i, kk);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          const uint4 b = query(q, kk);
+          const uint4 b = qf[q][kk];
 #pragma unroll
           for (int i = 0; i < TI; ++i) qk_piece(a[i], b, q, i);
         }
       }
     };
-    auto qk_residual = [&]() __attribute__((always_inline)) {
+    auto qk_residual = [&](const uint8_t* rt) __attribute__((always_inline)) {
       lds_fence();
       qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
         return *reinterpret_cast<const uint4*>(rt + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, i) + (lc & 3), 4 * kk + lg));
@@ -720,7 +728,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 
     // ---- what travels ahead of a tile
     struct Ahead {
-      uint4 kv[NLD], vv[NLD];
+      uint4 kv[NLD], vv[VLD];
       Entries ek[NCH], ev[NCH];
       SetRows sk, sv;
       uint32_t mask, rank;
@@ -731,12 +739,12 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 #pragma unroll
         for (int i = 0; i < NCH; ++i) {
           load_entries(ikr, xkr, b.t0, lane + 64 * i, b.ek[i]);
-          load_entries(ivr, xvr, b.t0, lane + 64 * i, b.ev[i]);
+          if constexpr (CG == 1) load_entries(ivr, xvr, b.t0, lane + 64 * i, b.ev[i]);
         }
       }
       if constexpr (SET) {
         load_rows(hkr, b.mask, b.rank, 0, b.sk);
-        load_rows(hvr, b.mask, b.rank, 0, b.sv);
+        if constexpr (CG == 1) load_rows(hvr, b.mask, b.rank, 0, b.sv);
       }
     };
     // Tile `it` from its buffer, which then takes tile it + DEPTH.
@@ -749,23 +757,43 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       const bool edge = t0 + TOK > T;  // tokens of the tile past the last one
 
       // V into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
+      if (CG == 1 || v_live) {
 #pragma unroll
-      for (int i = 0; i < NLD; ++i) {
-        if constexpr (C8) {
-          constexpr int half = kC8Block / D / 2;
-          const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
-          uint4 x = widen8(b.vv[i].x, b.vv[i].y), y = widen8(b.vv[i].z, b.vv[i].w);
-          if (edge) {
-            if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
-            if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < VLD; ++j) {
+          const int i = cg * VLD + j;
+          if constexpr (C8) {
+            constexpr int half = kC8Block / D / 2;
+            const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
+            uint4 x = widen8(b.vv[j].x, b.vv[j].y), y = widen8(b.vv[j].z, b.vv[j].w);
+            if (edge) {
+              if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
+              if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+            }
+            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = x;
+            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = y;
+          } else {
+            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = b.vv[j];
           }
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = x;
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = y;
-        } else {
-          *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = b.vv[i];
         }
       }
-      load_tile(vr, tn, v_off, b.vv, false);
+      load_v(tn, b.vv);
+      if constexpr (CG > 1 && RES != 0) {
+        if (has && role < roles) {
+          const bool rest = CG == 4 && REST && role == 2;
+          if constexpr (ENT) {
+            place_all(b.ek, t0);
+            scatter(rt, ikr, xkr, t0, rest);
+          }
+          if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, rest);
+          if constexpr (CG == 2 && REST) {
+            if (role == 0) {
+              if constexpr (ENT) scatter(r_rest, ikr, xkr, t0, true);
+              if constexpr (SET) set_rows(r_rest, hkr, b.sk, mask, rank, true);
+            }
+          }
+        }
+        load_res(b);
+      }
 
       // K
 #pragma unroll
@@ -778,28 +806,36 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
         else
           return b.kv[i * KK + kk];
       });
-      load_tile(kr, tn, k_off, b.kv, true);
-      if (has) {
-        if constexpr (ENT) {
-          place_all(b.ek, t0);
-          scatter(ikr, xkr, t0, false);
+      load_k(tn, k_off, b.kv);
+      if constexpr (CG > 1) {
+        hand_over();
+        if (has) {
+          qk_residual(r_k);
+          if constexpr (REST) qk_residual(r_rest);
         }
-        if constexpr (SET) set_rows(hkr, b.sk, mask, rank, false);
-        qk_residual();
-        if constexpr (!F32 && q4) {
-          if constexpr (ENT) scatter(ikr, xkr, t0, true);
-          if constexpr (SET) set_rows(hkr, b.sk, mask, rank, true);
-          qk_residual();
+      } else {
+        if (has) {
+          if constexpr (ENT) {
+            place_all(b.ek, t0);
+            scatter(rt, ikr, xkr, t0, false);
+          }
+          if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, false);
+          qk_residual(rt);
+          if constexpr (REST) {
+            if constexpr (ENT) scatter(rt, ikr, xkr, t0, true);
+            if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, true);
+            qk_residual(rt);
+          }
+          clear_r(rt);
+          lds_fence();
+          if constexpr (ENT) {
+            place_all(b.ev, t0);
+            scatter(rt, ivr, xvr, t0, false);
+          }
+          if constexpr (SET) set_rows(rt, hvr, b.sv, mask, rank, false);
         }
-        clear_r();
-        lds_fence();
-        if constexpr (ENT) {
-          place_all(b.ev, t0);
-          scatter(ivr, xvr, t0, false);
-        }
-        if constexpr (SET) set_rows(hvr, b.sv, mask, rank, false);
+        load_res(b);
       }
-      load_res(b);
 
       // softmax
       if (edge) {
@@ -861,14 +897,25 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
 
       // V
       pv(vt);
-      if (has) {
-        pv(rt);
-        clear_r();
+      if (has) pv(r_v);
+      if constexpr (CG > 1) hand_over();
+      if (has && role < roles) {
+        clear_r(rt);
+        if constexpr (CG == 2 && REST) {
+          if (role == 0) clear_r(r_rest);
+        }
         lds_fence();
       }
     };
 
-    if constexpr (RES != 0) clear_r();
+    if constexpr (RES != 0) {
+      if (role < roles) {
+        clear_r(rt);
+        if constexpr (CG == 2 && REST) {
+          if (role == 0) clear_r(r_rest);
+        }
+      }
+    }
     Ahead ahead[DEPTH];
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
@@ -876,8 +923,8 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
       b.t0 = tile_token(d);
       b.mask = b.rank = 0;
       if constexpr (SET) load_mask(b.t0, b.mask, b.rank);
-      load_tile(vr, b.t0, v_off, b.vv, false);
-      load_tile(kr, b.t0, k_off, b.kv, true);
+      load_v(b.t0, b.vv);
+      load_k(b.t0, k_off, b.kv);
       load_res(b);
     }
     settle_queries();
@@ -892,7 +939,7 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
   using no = integral_constant<bool, false>;
   using yes = integral_constant<bool, true>;
   const bool res = mode == kResidual && (KIND == kTokenSet || k > 0);
-  if (chunk0 < end && !bad_unit) {  // (the whole workgroup: the walk has a barrier)
+  if (chunk0 < end && !bad_unit) {  // (the whole workgroup: the walk may have barriers)
     if constexpr (TY == kTyC8) {
       if (mode == kExact)
         walk(no{}, no{});
@@ -925,29 +972,30 @@ __global__ __launch_bounds__(256, parts_per_cu(NQ, KIND, q4)) void parts_kernel(
     for (int c = 0; c < CT; ++c)
       *reinterpret_cast<f32x4_t*>(mg + (wave * 16 + lc) * MP + 16 * c + 4 * lg) = acc[q][c];
     __syncthreads();
-    const int col = threadIdx.x >> 4, part16 = threadIdx.x & 15;  // 16 threads a column
+    constexpr int TPC = 16 / CG;  // threads of a column
+    const int col = threadIdx.x / TPC, sub = threadIdx.x % TPC, gr = col / 16, cl = col % 16;
     int sq, g;
-    if (row_of(16 * q + col, sq, g)) {
+    if (row_of(16 * (gr * NQ + q) + cl, sq, g)) {
       float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, ml_lds[w][col][0]);
-      float wt[4], lt = 0.f;
+      for (int t = 0; t < TG; ++t) M = fmaxf(M, ml_lds[t * CG + gr][cl][0]);
+      float wt[TG], lt = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        wt[w] = merge_weight(ml_lds[w][col][0], M);
-        lt = fmaf(wt[w], ml_lds[w][col][1], lt);
+      for (int t = 0; t < TG; ++t) {
+        wt[t] = merge_weight(ml_lds[t * CG + gr][cl][0], M);
+        lt = fmaf(wt[t], ml_lds[t * CG + gr][cl][1], lt);
       }
       float* rec = ws + ((((uint64_t)sq * hkv + head) * n_slots_total + slot) * G + g) * RS;
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const int ch = 64 * c + 4 * part16;
+      for (int c = 0; c < D / (4 * TPC); ++c) {
+        const int ch = 4 * (TPC * c + sub);
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) o += wt[w] * *reinterpret_cast<const f32x4_t*>(mg + (w * 16 + col) * MP + ch);
+        for (int t = 0; t < TG; ++t) o += wt[t] * *reinterpret_cast<const f32x4_t*>(mg + ((t * CG + gr) * 16 + cl) * MP + ch);
         if (bad_unit) o = f32x4_t{NAN, NAN, NAN, NAN};
         *reinterpret_cast<f32x4_t*>(rec + ch) = o;
       }
-      if (part16 == 0) {
+      if (sub == 0) {
         rec[D] = bad_unit ? 0.f : M;
         rec[D + 1] = bad_unit ? 1.f : lt;
       }
@@ -959,14 +1007,14 @@ template <int D, int TY, int KIND, bool q4>
 static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
   const uint32_t items = (uint32_t)P.hkv * P.n_slots;
   const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
-  if (P.nq == 1) {
-    hipLaunchKernelGGL((parts_kernel<D, 1, TY, KIND, q4>), grid, block, 0, s, P);
-  } else if (P.nq == 2) {
-    hipLaunchKernelGGL((parts_kernel<D, 2, TY, KIND, q4>), grid, block, 0, s, P);
-  } else {
-    // (64 columns and many entries do not fit the registers: the plan gives such a call 32)
-    if constexpr (KIND != kManyEntries) hipLaunchKernelGGL((parts_kernel<D, 4, TY, KIND, q4>), grid, block, 0, s, P);
-  }
+  if (P.cols == 16)
+    hipLaunchKernelGGL((parts_kernel<D, 1, 1, TY, KIND, q4>), grid, block, 0, s, P);
+  else if (P.cols == 32)
+    hipLaunchKernelGGL((parts_kernel<D, 1, 2, TY, KIND, q4>), grid, block, 0, s, P);
+  else if (P.cols == 64)
+    hipLaunchKernelGGL((parts_kernel<D, 2, 2, TY, KIND, q4>), grid, block, 0, s, P);
+  else
+    hipLaunchKernelGGL((parts_kernel<D, 2, 4, TY, KIND, q4>), grid, block, 0, s, P);
   return hipGetLastError();
 }
 
