@@ -986,10 +986,10 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
   p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 4, 256);
   p.rows = (int)(batch * G);
-  p.cols = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+  p.cols = p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
   p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (hkv * p.row_groups),
-                                 p.cols == 16 ? 4 : p.cols == 128 ? 1 : 2, 1 << 28);
+                                 p.cols == 16 ? 4 : 1, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {

@@ -32,6 +32,9 @@
 // a tile takes to arrive (a CU gets some 13 bytes a cycle; a tile of 16 KB on one
 // SIMD of it takes 5000 cycles, its products at 64 columns 1100).
 #pragma once
+#ifndef PARTS_DEPTH
+#define PARTS_DEPTH 2
+#endif
 
 #include <type_traits>
 
@@ -168,7 +171,8 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
   // a token group's LDS: the V tile, then R (CG > 1: of K, of V and, where K's has one, of K's rest), each with a row
   // behind it that takes what has no place
   constexpr bool REST = q4 && !F32;  // K's residual has a bf16 rest
-  constexpr int kRt = S::TILE_BYTES + RB, kGroupLds = S::TILE_BYTES + (CG == 1 ? 1 : REST ? 3 : 2) * kRt;
+  constexpr int kRt = S::TILE_BYTES + RB, kGroupLds = CG == 1 ? S::TILE_BYTES + kRt : 2 * S::TILE_BYTES + (REST ? 3 : 2) * kRt;
+  static_assert(kGroupLds % RB == 0 && S::TILE_BYTES % RB == 0, "tiles start at a multiple of a row");
   constexpr int kLds = TG * kGroupLds > 4 * 16 * MP * 4 ? TG * kGroupLds : 4 * 16 * MP * 4;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
   __shared__ float ml_lds[4][16][2];
@@ -316,7 +320,8 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
   }
 
   uint8_t* vt = lds + tg * kGroupLds;                  // the V tile
-  uint8_t* r_k = vt + S::TILE_BYTES;                   // R of K, of V, of K's rest (CG == 1: one after the other)
+  uint8_t* kt = vt + S::TILE_BYTES;                    // CG > 1: the K tile
+  uint8_t* r_k = kt + (CG == 1 ? 0 : S::TILE_BYTES);   // R of K, of V, of K's rest (CG == 1: one after the other)
   uint8_t* r_v = CG == 1 ? r_k : r_k + kRt;
   uint8_t* r_rest = CG == 1 ? r_k : r_k + 2 * kRt;
   // CG > 1: the wave's tile of R (0: K, 1: V, 2: K's rest; CG == 2: wave 0 has K's rest too)
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
     constexpr int RES = decltype(res_tag)::value ? KIND : 0;
     constexpr bool ENT = RES == kFewEntries || RES == kManyEntries, SET = RES == kTokenSet;
     // tiles in flight behind the current one
-    constexpr int DEPTH = 1;
+    constexpr int DEPTH = CG == 1 || NQ == 2 ? 1 : PARTS_DEPTH;
     constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
@@ -394,6 +399,7 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
     };
 
     // ---- loads
+    // K in the operand's layout: lane (lc, lg) holds pieces 4 kk + lg of its token(s)
     auto load_k = [&](int t0, uint32_t lane_off, uint4 (&x)[NLD]) __attribute__((always_inline)) {
       const uint32_t base = t0 < T ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
 #pragma unroll
@@ -406,15 +412,35 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
         x[i] = ld128<0>(kr, base + lane_off + step);
       }
     };
-    // V row by row: the wave's share of the tile's loads
+    // A tile row by row on its way to LDS: the wave's share of its loads
     constexpr int VLD = NLD > CG ? NLD / CG : 1;
     const bool v_live = cg * VLD < NLD;
-    auto load_v = [&](int t0, uint4 (&x)[VLD]) __attribute__((always_inline)) {
+    auto load_rowwise = [&](const __amdgpu_buffer_rsrc_t& r, int t0, uint4 (&x)[VLD]) __attribute__((always_inline)) {
       const uint32_t base = t0 < T && v_live ? (uint32_t)t0 * (C8 ? D : RB) : kOob;
 #pragma unroll
-      for (int i = 0; i < VLD; ++i) x[i] = ld128<0>(vr, base + (uint32_t)lane * 16 + (uint32_t)(cg * VLD + i) * 1024);
+      for (int i = 0; i < VLD; ++i) x[i] = ld128<0>(r, base + (uint32_t)lane * 16 + (uint32_t)(cg * VLD + i) * 1024);
     };
-    // K in the operand's layout: lane (lc, lg) holds pieces 4 kk + lg of its token(s)
+    // ... and into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
+    auto stage = [&](uint8_t* tile, const uint4 (&v)[VLD], int t0) __attribute__((always_inline)) {
+      if (CG > 1 && !v_live) return;
+#pragma unroll
+      for (int j = 0; j < VLD; ++j) {
+        const int i = cg * VLD + j;
+        if constexpr (C8) {
+          constexpr int half = kC8Block / D / 2;
+          const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
+          uint4 x = widen8(v[j].x, v[j].y), y = widen8(v[j].z, v[j].w);
+          if (t0 + TOK > T) {
+            if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
+            if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
+          }
+          *reinterpret_cast<uint4*>(tile + piece_at<D, TY>(row, pc)) = x;
+          *reinterpret_cast<uint4*>(tile + piece_at<D, TY>(row + half, pc)) = y;
+        } else {
+          *reinterpret_cast<uint4*>(tile + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = v[j];
+        }
+      }
+    };
     uint32_t k_off;
     if constexpr (C8) {
       constexpr int half = kC8Block / D / 2;
@@ -685,10 +711,15 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
         }
       }
     };
-    auto qk_residual = [&](const uint8_t* rt) __attribute__((always_inline)) {
+    // Operands in an LDS tile.  Pieces are permuted by XOR, and a tile starts at a multiple of a row, so the piece of
+    // the kk-th channels (the c-th output tile) is the first one's address with some bits flipped.  (The addresses are
+    // formed where they are used: held for all of a tile's reads they would take the registers that its loads need.)
+    auto qk_tile = [&](const uint8_t* tile) __attribute__((always_inline)) {
       lds_fence();
+      uint32_t at = (uint32_t)(tile - lds) + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, 0) + (lc & 3), lg);
+      asm("" : "+v"(at));
       qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
-        return *reinterpret_cast<const uint4*>(rt + piece_at<D, TY>(quad_row<D, TY>(lc >> 2, i) + (lc & 3), 4 * kk + lg));
+        return *reinterpret_cast<const uint4*>(lds + (at ^ (uint32_t)(kk << 6)) + i * (quad_row<D, TY>(0, 1) * RB));
       });
       lds_fence();
     };
@@ -696,25 +727,34 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
     uint32_t pb[NQ][4];
     auto pv = [&](const uint8_t* tile) __attribute__((always_inline)) {
       lds_fence();
+      const uint32_t off = (uint32_t)(tile - lds);
+      if constexpr (F32) {
+        uint32_t at[4];
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        if constexpr (F32) {
+        for (int i = 0; i < 4; ++i) {
+          at[i] = off + piece_at<D, TY>(4 * lg + i, lc >> 2) + (lc & 3) * 4;
+          asm("" : "+v"(at[i]));
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int ch = 16 * c + lc;
-            const float a = *reinterpret_cast<const float*>(tile + piece_at<D, TY>(4 * lg + i, ch / 4) + (ch & 3) * 4);
+            const float a = *reinterpret_cast<const float*>(lds + (at[i] ^ (uint32_t)(c << 6)));
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
               acc[q][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, as_f32(pb[q][i]), acc[q][c], 0, 0, 0);
           }
-        } else {
-          // rows quad .. quad + 3 of both operands, channels 16 c ..: lane i of a group names row i / 4, channels 4 (i % 4) ..
+      } else {
+        // rows quad .. quad + 3 of both operands, channels 16 c ..: lane i of a group names row i / 4, channels 4 (i % 4) ..
+        uint32_t at = off + piece_at<D, TY>(quad_row<D, TY>(lg, 0) + (lc >> 2), (lc & 3) >> 1) + (lc & 1) * 8;
+        asm("" : "+v"(at));
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
           i16x4_t h[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint8_t* at = tile + piece_at<D, TY>(quad_row<D, TY>(lg, i) + (lc >> 2), 2 * c + ((lc & 3) >> 1)) + (lc & 1) * 8;
-            h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)at);
-          }
+          for (int i = 0; i < 2; ++i)
+            h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_i16x4_t*)(lds + (at ^ (uint32_t)(c << 5)) + i * (quad_row<D, TY>(0, 1) * RB)));
           const i16x8_t a = {h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]};
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
@@ -728,7 +768,7 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
 
     // ---- what travels ahead of a tile
     struct Ahead {
-      uint4 kv[NLD], vv[VLD];
+      uint4 kv[CG == 1 ? NLD : VLD], vv[VLD];
       Entries ek[NCH], ev[NCH];
       SetRows sk, sv;
       uint32_t mask, rank;
@@ -756,27 +796,12 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
       const bool has = ENT || (SET && mask != 0);
       const bool edge = t0 + TOK > T;  // tokens of the tile past the last one
 
-      // V into LDS (a padding row of an E4M3 block may hold anything: it goes in as zero)
-      if (CG == 1 || v_live) {
-#pragma unroll
-        for (int j = 0; j < VLD; ++j) {
-          const int i = cg * VLD + j;
-          if constexpr (C8) {
-            constexpr int half = kC8Block / D / 2;
-            const int row = i * 2 * half + lane / (D / 8), pc = lane % (D / 8);
-            uint4 x = widen8(b.vv[j].x, b.vv[j].y), y = widen8(b.vv[j].z, b.vv[j].w);
-            if (edge) {
-              if (t0 + row >= T) x = make_uint4(0, 0, 0, 0);
-              if (t0 + row + half >= T) y = make_uint4(0, 0, 0, 0);
-            }
-            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row, pc)) = x;
-            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(row + half, pc)) = y;
-          } else {
-            *reinterpret_cast<uint4*>(vt + piece_at<D, TY>(i * RPL + lane / NP, lane % NP)) = b.vv[j];
-          }
-        }
+      stage(vt, b.vv, t0);
+      load_rowwise(vr, tn, b.vv);
+      if constexpr (CG > 1) {
+        stage(kt, b.kv, t0);
+        load_rowwise(kr, tn, b.kv);
       }
-      load_v(tn, b.vv);
       if constexpr (CG > 1 && RES != 0) {
         if (has && role < roles) {
           const bool rest = CG == 4 && REST && role == 2;
@@ -800,31 +825,32 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int i = 0; i < TI; ++i) s[q][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
-        if constexpr (C8)
-          return i ? widen8(b.kv[kk].z, b.kv[kk].w) : widen8(b.kv[kk].x, b.kv[kk].y);
-        else
-          return b.kv[i * KK + kk];
-      });
-      load_k(tn, k_off, b.kv);
       if constexpr (CG > 1) {
         hand_over();
+        qk_tile(kt);
         if (has) {
-          qk_residual(r_k);
-          if constexpr (REST) qk_residual(r_rest);
+          qk_tile(r_k);
+          if constexpr (REST) qk_tile(r_rest);
         }
       } else {
+        qk([&](int i, int kk) __attribute__((always_inline)) -> uint4 {
+          if constexpr (C8)
+            return i ? widen8(b.kv[kk].z, b.kv[kk].w) : widen8(b.kv[kk].x, b.kv[kk].y);
+          else
+            return b.kv[i * KK + kk];
+        });
+        load_k(tn, k_off, b.kv);
         if (has) {
           if constexpr (ENT) {
             place_all(b.ek, t0);
             scatter(rt, ikr, xkr, t0, false);
           }
           if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, false);
-          qk_residual(rt);
+          qk_tile(rt);
           if constexpr (REST) {
             if constexpr (ENT) scatter(rt, ikr, xkr, t0, true);
             if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, true);
-            qk_residual(rt);
+            qk_tile(rt);
           }
           clear_r(rt);
           lds_fence();
@@ -923,15 +949,21 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
       b.t0 = tile_token(d);
       b.mask = b.rank = 0;
       if constexpr (SET) load_mask(b.t0, b.mask, b.rank);
-      load_v(b.t0, b.vv);
-      load_k(b.t0, k_off, b.kv);
+      load_rowwise(vr, b.t0, b.vv);
+      if constexpr (CG == 1)
+        load_k(b.t0, k_off, b.kv);
+      else
+        load_rowwise(kr, b.t0, b.kv);
       load_res(b);
     }
     settle_queries();
 #pragma unroll 1
     for (int it = 0; it < n; it += DEPTH) {
 #pragma unroll
-      for (int d = 0; d < DEPTH; ++d) step(ahead[d], it + d);  // (one past the last: every token masked)
+      for (int d = 0; d < DEPTH; ++d) {
+        if (d > 0 && it + d >= n) break;
+        step(ahead[d], it + d);
+      }
     }
   };
 
@@ -1009,10 +1041,8 @@ static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
   const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
   if (P.cols == 16)
     hipLaunchKernelGGL((parts_kernel<D, 1, 1, TY, KIND, q4>), grid, block, 0, s, P);
-  else if (P.cols == 32)
-    hipLaunchKernelGGL((parts_kernel<D, 1, 2, TY, KIND, q4>), grid, block, 0, s, P);
   else if (P.cols == 64)
-    hipLaunchKernelGGL((parts_kernel<D, 2, 2, TY, KIND, q4>), grid, block, 0, s, P);
+    hipLaunchKernelGGL((parts_kernel<D, 1, 4, TY, KIND, q4>), grid, block, 0, s, P);
   else
     hipLaunchKernelGGL((parts_kernel<D, 2, 4, TY, KIND, q4>), grid, block, 0, s, P);
   return hipGetLastError();
