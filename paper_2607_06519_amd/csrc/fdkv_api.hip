@@ -986,7 +986,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
   p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 4, 256);
   p.rows = (int)(batch * G);
-  p.cols = p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
+  p.cols = p.n_shared == 0 || p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
   p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (hkv * p.row_groups),
                                  p.cols == 16 ? 4 : 1, 1 << 28);
@@ -1005,8 +1005,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
     p.total_slots = p.own_slots + p.slots[p.n_own];
   }
   // workgroups and record slots are counted in 31 bits
-  if (batch * hkv * std::max<int64_t>(p.total_slots, 1) >= (1ll << 31) ||
-      (hkv * p.total_slots + 8) * p.row_groups >= (1ll << 31))
+  if (batch * hkv * std::max<int64_t>(p.total_slots, 1) >= (1ll << 30) || (hkv * p.total_slots + 8) * p.row_groups >= (1ll << 30))
     return FDKV_E_UNSUPPORTED;
   *out = p;
   return FDKV_OK;
@@ -1102,17 +1101,14 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
     p.tail_v = tail->v;
     p.tail_cap = tail->cap;
   }
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  for (int shared = 0; shared < 2; ++shared) {  // a launch for the parts of single sequences, one for the shared ones
+  for (int shared = 0; shared < 2; ++shared) {
+    PartsSide& side = p.side[shared];
     const int n = shared ? plan.n_shared : plan.n_own;
     const int64_t* slots = plan.slots + (shared ? plan.n_own : 0);
-    p.n_slots = (int)(shared ? plan.shared_wgs : plan.own_slots);
-    if (p.n_slots == 0) continue;
     int base = 0;
     for (int i = 0; i < kMaxParts; ++i) {
-      PartsPart& o = p.part[i];
-      o = PartsPart{};
-      p.part_base[i] = i < n ? base : INT32_MAX;
+      PartsPart& o = side.part[i];
+      side.part_base[i] = i < n ? base : INT32_MAX;
       if (i >= n) continue;
       base += (int)slots[i];
       const int at = shared ? plan.shared[i] : plan.own[i];
@@ -1133,16 +1129,22 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
         o.n_sel = pt.n_sel;
       }
     }
-    p.shared = shared;
-    p.res_cost = shared ? plan.res_cost : 0;
-    p.shared_counts = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + parts_record_bytes(dims, batch, plan));
-    p.cols = shared ? plan.cols : 16;
-    p.rows = shared ? plan.rows : p.G;
-    p.row_groups = shared ? plan.row_groups : 1;
-    p.tiles_per_wg = shared ? plan.shared_tiles_per_wg : plan.own_tiles_per_wg;
-    p.slot0 = shared ? (int)plan.own_slots : 0;
-    p.by_slots.set((uint32_t)p.n_slots);
-    p.by_groups.set((uint32_t)p.row_groups);
+    side.n_slots = (int)(shared ? plan.shared_wgs : plan.own_slots);
+    side.shared = shared;
+    side.res_cost = shared ? plan.res_cost : 0;
+    side.rows = shared ? plan.rows : p.G;
+    side.row_groups = shared ? plan.row_groups : 1;
+    side.tiles_per_wg = shared ? plan.shared_tiles_per_wg : plan.own_tiles_per_wg;
+    side.slot0 = shared ? (int)plan.own_slots : 0;
+    side.by_slots.set((uint32_t)std::max(side.n_slots, 1));
+    side.by_groups.set((uint32_t)side.row_groups);
+  }
+  p.cols = plan.cols;
+  p.shared_counts = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + parts_record_bytes(dims, batch, plan));
+  // (items in eights: parts.h deals them to the XCDs)
+  p.shared_wgs = (uint32_t)((p.hkv * plan.shared_wgs + 7) / 8 * 8 * plan.row_groups);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (plan.total_slots > 0) {
     const hipError_t e = launch_parts(p, s);
     if (e != hipSuccess) return hip_fail(e, "decode_parts");
   }

@@ -157,30 +157,35 @@ struct PartsPart {
   int n_sel, max_len;          // n_sel 0: every token
 };
 
-// One launch: the parts of single sequences, or the shared ones.  What a
-// workgroup needs before it can ask for anything else comes first: it fetches
-// that in one go.
-struct PartsParams {
-  DivU by_slots, by_hkv, by_groups;
-  int hkv, hq, G, g_shift, n_slots, tiles_per_wg, row_groups, rows;  // rows: query rows of a sequence, or of the batch
-  int n_blocks, block, slot0, shared;
+// The parts of single sequences, or the shared ones.  What a workgroup needs
+// before it can ask for anything else comes first: it fetches that in one go.
+struct PartsSide {
+  DivU by_slots, by_groups;
+  int n_slots, tiles_per_wg, row_groups, rows;  // rows: query rows of a sequence, or of the batch
+  int slot0, shared;           // first record slot
   int res_cost;                // a residual head's time per token, a plain one's being 16; 0: every head takes n_slots
                                // workgroups (shared parts only)
-  int* shared_counts;          // [hkv] out: record slots that a head of the shared part fills (res_cost > 0)
+  int part_base[kMaxParts];    // first slot of each part, from 0; INT32_MAX past the last
+  PartsPart part[kMaxParts];
+};
+
+// One launch: workgroups 0 .. shared_wgs - 1 take the shared parts, the others those of single sequences.
+struct PartsParams {
+  uint32_t shared_wgs;
+  DivU by_hkv, by_topk;
+  int hkv, hq, G, g_shift, n_blocks, block, pos, bsize, topk, tail_cap, n_slots_total;
   const void* q;               // [batch][hq][d]
   float* ws;                   // records [batch][hkv][n_slots_total][G][d + 4]
   const void* tail_k;          // [batch][hkv][tail_cap][d]
   const void* tail_v;
-  DivU by_topk;
-  int pos, bsize, topk, tail_cap, n_slots_total;
+  int* shared_counts;          // [hkv] out: record slots that a head of the shared part fills (res_cost > 0)
   float wres[3], scale_log2;
-  int part_base[kMaxParts];    // first slot of each part, from 0; INT32_MAX past the last
-  PartsPart part[kMaxParts];   // this launch's parts
+  PartsSide side[2];           // single sequences, shared
   int batch, d;
   int res_ppm, n_rates;
   int rates_ppm[kMaxRates];
   bool tokres, bf16, coef8;
-  int cols;                    // query rows of a workgroup: 16, 32, 64 or 128
+  int cols;                    // query rows of a workgroup of the shared parts: 16, 64 or 128
 };
 
 struct PartsMergeParams {

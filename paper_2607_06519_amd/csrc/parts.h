@@ -155,39 +155,49 @@ enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
 // walk would wait for every load in flight.
 constexpr int parts_per_cu(int KIND, bool q4) { return KIND == kManyEntries && q4 ? 1 : 2; }
 
+// LDS of a workgroup.  A token group's: the V tile, then R with a row behind it that takes what has no place (CG > 1:
+// the K tile, and R of K, of V and, where K's has one, of K's rest).
+template <int D, int CG, int TY, bool q4>
+struct PartsLds {
+  using S = parts::TileOf<D, TY>;
+  static constexpr bool REST = q4 && !S::F32;  // K's residual has a bf16 rest
+  static constexpr int RT = S::TILE_BYTES + S::RB;
+  static constexpr int GROUP = CG == 1 ? S::TILE_BYTES + RT : 2 * S::TILE_BYTES + (REST ? 3 : 2) * RT;
+  static_assert(GROUP % S::RB == 0 && S::TILE_BYTES % S::RB == 0, "tiles start at a multiple of a row");
+  static constexpr int MP = D + 4;             // floats of a row of the merge (padded against bank conflicts)
+  static constexpr int TILES = 4 / CG * GROUP, MERGE = 4 * 16 * MP * 4;
+  static constexpr int BYTES = TILES > MERGE ? TILES : MERGE;
+};
+
 // CG column groups of 16 NQ columns each, a wave apiece, by TG = 4 / CG token
 // groups.  With CG > 1 the waves of a token group walk the same tiles: each
-// stages its share of V, one places the residual entries of K, one those of V
-// (one the rest of K's), and two barriers a tile hand the tiles over.
+// stages its share of K and V, one places the residual entries of K, one those of
+// V (one the rest of K's), and two barriers a tile hand the tiles over.
 template <int D, int NQ, int CG, int TY, int KIND, bool q4>
-__global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(PartsParams P) {
+__device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide& L, uint32_t w, uint8_t* lds, float (*ml_lds)[16][2]) {
   using namespace parts;
   using S = TileOf<D, TY>;
   constexpr bool F32 = S::F32;
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
   constexpr int TG = 4 / CG, COLS = 16 * NQ * CG;
   constexpr int RS = D + 4;
-  constexpr int MP = D + 4;  // floats of a row of the merge (padded against bank conflicts)
-  // a token group's LDS: the V tile, then R (CG > 1: of K, of V and, where K's has one, of K's rest), each with a row
-  // behind it that takes what has no place
-  constexpr bool REST = q4 && !F32;  // K's residual has a bf16 rest
-  constexpr int kRt = S::TILE_BYTES + RB, kGroupLds = CG == 1 ? S::TILE_BYTES + kRt : 2 * S::TILE_BYTES + (REST ? 3 : 2) * kRt;
-  static_assert(kGroupLds % RB == 0 && S::TILE_BYTES % RB == 0, "tiles start at a multiple of a row");
-  constexpr int kLds = TG * kGroupLds > 4 * 16 * MP * 4 ? TG * kGroupLds : 4 * 16 * MP * 4;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
-  __shared__ float ml_lds[4][16][2];
+  using Lds = PartsLds<D, CG, TY, q4>;
+  constexpr bool REST = Lds::REST;
+  constexpr int kRt = Lds::RT, kGroupLds = Lds::GROUP, MP = Lds::MP;
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4, lane = threadIdx.x & 63;
   const int lc = lane & 15, lg = lane >> 4;  // column (or operand row) and lane group
   const int tg = wave / CG, cg = wave % CG;
   // ---- what the launch says, fetched in one go and kept (left to itself the compiler reads it piece by piece, each
   // piece a trip to memory)
-  DivU by_slots = P.by_slots, by_hkv = P.by_hkv, by_groups = P.by_groups;
-  int hkv = P.hkv, hq = P.hq, G = P.G, g_shift = P.g_shift, n_slots = P.n_slots, tiles_per_wg = P.tiles_per_wg;
-  int res_cost = P.res_cost, row_groups = P.row_groups, rows = P.rows, n_blocks = P.n_blocks, block = P.block, slot0 = P.slot0, shared = P.shared;
-  const void* q_all = P.q;
-  PartsPart pt = P.part[0], pt1 = P.part[1];
-  int base1 = P.part_base[1], base2 = P.part_base[2];
+  DivU by_slots = L.by_slots, by_hkv = P.by_hkv, by_groups = L.by_groups, by_topk = P.by_topk;
+  int hkv = P.hkv, hq = P.hq, G = P.G, g_shift = P.g_shift, n_slots = L.n_slots, tiles_per_wg = L.tiles_per_wg;
+  int res_cost = L.res_cost, row_groups = L.row_groups, rows = L.rows, n_blocks = P.n_blocks, block = P.block, slot0 = L.slot0;
+  int shared = L.shared, pos = P.pos, nb = P.bsize, k = P.topk, tail_cap = P.tail_cap, n_slots_total = P.n_slots_total;
+  const void *q_all = P.q, *tail_k = P.tail_k, *tail_v = P.tail_v;
+  float *ws = P.ws, w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2], scale_log2 = P.scale_log2;
+  PartsPart pt = L.part[0], pt1 = L.part[1];
+  int base1 = L.part_base[1], base2 = L.part_base[2];
   asm volatile("" : "+s"(by_slots.mul), "+s"(by_slots.shift), "+s"(by_hkv.mul), "+s"(by_hkv.shift), "+s"(by_groups.mul),
                "+s"(by_groups.shift), "+s"(hkv), "+s"(hq), "+s"(G), "+s"(g_shift), "+s"(n_slots), "+s"(tiles_per_wg),
                "+s"(row_groups), "+s"(rows), "+s"(res_cost));
@@ -195,17 +205,10 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
                "+s"(pt.cache), "+s"(pt.modes), "+s"(pt.seg_off), "+s"(pt.blocks), "+s"(pt.counts), "+s"(pt.n_sel), "+s"(pt.max_len));
   asm volatile("" : "+s"(pt1.lens), "+s"(pt1.cache), "+s"(pt1.modes), "+s"(pt1.seg_off), "+s"(pt1.blocks), "+s"(pt1.counts),
                "+s"(pt1.n_sel), "+s"(pt1.max_len));
-
-  float* ws = P.ws;
-  const void *tail_k = P.tail_k, *tail_v = P.tail_v;
-  DivU by_topk = P.by_topk;
-  int pos = P.pos, nb = P.bsize, k = P.topk, tail_cap = P.tail_cap, n_slots_total = P.n_slots_total;
-  float w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2], scale_log2 = P.scale_log2;
   asm volatile("" : "+s"(ws), "+s"(tail_k), "+s"(tail_v), "+s"(by_topk.mul), "+s"(by_topk.shift), "+s"(pos), "+s"(nb), "+s"(k),
                "+s"(tail_cap), "+s"(n_slots_total), "+s"(w1), "+s"(w2), "+s"(w3), "+s"(scale_log2));
 
   // ---- which chunk
-  uint32_t w = blockIdx.x;
   int row0 = 0;
   if (shared) {
     // the row groups of one chunk follow each other on one XCD (workgroups go to the XCDs in turn)
@@ -239,9 +242,9 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
     chunk0 = slot - base1;
     if (slot >= base2) {
       int i = 2;
-      while (i + 1 < kMaxParts && slot >= P.part_base[i + 1]) ++i;
-      pt = P.part[i];
-      chunk0 = slot - P.part_base[i];
+      while (i + 1 < kMaxParts && slot >= L.part_base[i + 1]) ++i;
+      pt = L.part[i];
+      chunk0 = slot - L.part_base[i];
     }
   }
   slot += slot0;
@@ -1035,10 +1038,26 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
   }
 }
 
+// NQ, CG: of the shared parts' workgroups; those of single sequences have one column tile and four token groups.  (The
+// two kinds in one launch: the second fills the CUs that the first leaves one by one.)
+template <int D, int NQ, int CG, int TY, int KIND, bool q4>
+__global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(PartsParams P) {
+  constexpr int own = PartsLds<D, 1, TY, q4>::BYTES, both = PartsLds<D, CG, TY, q4>::BYTES;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[own > both ? own : both];
+  __shared__ float ml_lds[4][16][2];
+  const bool shared = blockIdx.x < P.shared_wgs;
+  if constexpr (CG > 1) {
+    if (shared) {
+      parts_body<D, NQ, CG, TY, KIND, q4>(P, P.side[1], blockIdx.x, lds, ml_lds);
+      return;
+    }
+  }
+  parts_body<D, 1, 1, TY, KIND, q4>(P, P.side[shared ? 1 : 0], shared ? blockIdx.x : blockIdx.x - P.shared_wgs, lds, ml_lds);
+}
+
 template <int D, int TY, int KIND, bool q4>
 static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
-  const uint32_t items = (uint32_t)P.hkv * P.n_slots;
-  const dim3 grid(P.shared ? (items + 7) / 8 * 8 * P.row_groups : items * (uint32_t)P.batch), block(256);
+  const dim3 grid(P.shared_wgs + (uint32_t)P.hkv * (uint32_t)P.side[0].n_slots * (uint32_t)P.batch), block(256);
   if (P.cols == 16)
     hipLaunchKernelGGL((parts_kernel<D, 1, 1, TY, KIND, q4>), grid, block, 0, s, P);
   else if (P.cols == 64)

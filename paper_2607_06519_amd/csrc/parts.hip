@@ -18,7 +18,7 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(256) void parts_merge_kernel(PartsMergeParams P) {
   constexpr int RS = D + 4;
   constexpr int LPR = D / 4, NG = 256 / LPR;  // lanes of a record, groups of them
-  constexpr int U = 4;                        // records of a group in flight
+  constexpr int U = 8;                        // records of a group in flight
   __shared__ float m_lds[NG], l_lds[NG];
   __shared__ __attribute__((aligned(16))) float o_lds[NG][D];
   const uint32_t seq = P.by_hq.div(blockIdx.x);
