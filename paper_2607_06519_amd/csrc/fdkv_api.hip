@@ -943,10 +943,10 @@ constexpr int64_t kPartsWorkgroups = 512;
 // dimension 128): one head's share of the workgroups.
 int parts_res_cost(const fdkv_dims* dims) {
   const bool quads = dims->schedule != FDKV_SCHED_PAIRS;
-  if (tokens_mode(dims)) return quads ? 36 : 29;
+  if (tokens_mode(dims)) return quads ? 32 : 24;
   if (dims->topk == 0) return 16;
-  if (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16)) return 48;
-  return quads ? 38 : 26;
+  if (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16)) return 40;
+  return quads ? 28 : 24;
 }
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
@@ -988,8 +988,11 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   p.rows = (int)(batch * G);
   p.cols = p.n_shared == 0 || p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
-  p.shared_tiles_per_wg = per_wg(shared_tiles, kPartsWorkgroups / (hkv * p.row_groups),
-                                 p.cols == 16 ? 4 : 1, 1 << 28);
+  // (Workgroups of 64 rows: three to two CUs, as more of them write more records and leave the own parts to the end.  Per
+  // layer, 32768 tokens, 16 sequences and their tails: 384 workgroups 46.5 us, 256 48.3, 512 49.9.  Of 128 rows, two to
+  // a CU: 131072 tokens 152 us, with 384 164.)
+  const int64_t wgs = p.cols == 64 ? kPartsWorkgroups * 3 / 4 : kPartsWorkgroups;
+  p.shared_tiles_per_wg = per_wg(shared_tiles, wgs / (hkv * p.row_groups), p.cols == 16 ? 4 : 1, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {
@@ -1149,7 +1152,7 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
     if (e != hipSuccess) return hip_fail(e, "decode_parts");
   }
   PartsMergeParams mp{};
-  mp.by_hq.set((uint32_t)p.hq);
+  mp.by_hkv = p.by_hkv;
   mp.ws = p.ws;
   mp.shared_counts = plan.res_cost ? p.shared_counts : nullptr;
   mp.own_slots = (int)plan.own_slots;

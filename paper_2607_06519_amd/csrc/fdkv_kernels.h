@@ -189,7 +189,7 @@ struct PartsParams {
 };
 
 struct PartsMergeParams {
-  DivU by_hq;
+  DivU by_hkv;
   const float* ws;             // records [batch][hkv][n_slots_total][G][d + 4]
   const int* shared_counts;    // [hkv] slots in use after the first own_slots, or null: all of n_slots_total
   int own_slots, n_slots_total, batch, hq, hkv, G, g_shift, d;

@@ -21,8 +21,11 @@ __global__ __launch_bounds__(256) void parts_merge_kernel(PartsMergeParams P) {
   constexpr int U = 8;                        // records of a group in flight
   __shared__ float m_lds[NG], l_lds[NG];
   __shared__ __attribute__((aligned(16))) float o_lds[NG][D];
-  const uint32_t seq = P.by_hq.div(blockIdx.x);
-  const int qh = (int)(blockIdx.x - seq * P.hq), head = qh >> P.g_shift, g = qh & (P.G - 1);
+  // The G rows of a (sequence, KV head), whose records lie side by side, on one XCD (workgroups go to the XCDs in turn).
+  const uint32_t x = blockIdx.x & 7u, y = blockIdx.x >> 3, unit = (y >> P.g_shift) * 8 + x;
+  if (unit >= (uint32_t)(P.batch * P.hkv)) return;
+  const uint32_t seq = P.by_hkv.div(unit);
+  const int head = (int)(unit - seq * P.hkv), g = (int)y & (P.G - 1);
   const int c4 = threadIdx.x % LPR, rg = threadIdx.x / LPR;
   const uint64_t stride = (uint64_t)P.G * RS;
   const float* base = P.ws + ((uint64_t)seq * P.hkv + head) * P.n_slots_total * stride + (uint64_t)g * RS;
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(256) void parts_merge_kernel(PartsMergeParams P) {
       ot = fmaf(w, o_lds[i][threadIdx.x], ot);
     }
     const float res = lt > 0.f ? ot / lt : 0.f;
-    const uint64_t at = (uint64_t)blockIdx.x * D + threadIdx.x;
+    const uint64_t at = ((uint64_t)unit * P.G + g) * D + threadIdx.x;
     if constexpr (BF16)
       static_cast<uint16_t*>(P.out)[at] = (uint16_t)f32_to_bf16_bits(res);
     else
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(256) void parts_merge_kernel(PartsMergeParams P) {
 }  // namespace
 
 hipError_t launch_parts_merge(const PartsMergeParams& P, hipStream_t s) {
-  const dim3 grid((unsigned)(P.batch * P.hq)), block(256);
+  const dim3 grid((unsigned)(P.batch * P.hkv + 7) / 8 * 8 * P.G), block(256);
   if (P.d == 128) {
     if (P.bf16)
       hipLaunchKernelGGL((parts_merge_kernel<128, true>), grid, block, 0, s, P);
