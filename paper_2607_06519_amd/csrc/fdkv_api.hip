@@ -983,8 +983,16 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
     const int64_t n = (tiles + std::max<int64_t>(groups, 1) - 1) / std::max<int64_t>(groups, 1);
     return (int)std::min<int64_t>(most, std::max<int64_t>(1, (n + each - 1) / each) * each);
   };
-  // (a lane of a wave holds the block of one of its tiles: at most 64 a wave)
+  // The fewest tiles a workgroup whose chunks, every part's last one included, are on the card at once.  (A lane of a
+  // wave holds the block of one of its tiles: at most 64 a wave.)
   p.own_tiles_per_wg = per_wg(own_tiles, kPartsWorkgroups / (batch * hkv), 4, 256);
+  auto chunks = [&](int64_t per) {
+    int64_t n = 0;
+    for (int i = 0; i < p.n_own; ++i) n += (tiles[i] + per - 1) / per;
+    return n;
+  };
+  while (p.own_tiles_per_wg < 256 && chunks(p.own_tiles_per_wg) > p.n_own && chunks(p.own_tiles_per_wg) * batch * hkv > kPartsWorkgroups)
+    p.own_tiles_per_wg += 4;
   p.rows = (int)(batch * G);
   p.cols = p.n_shared == 0 || p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
