@@ -358,30 +358,34 @@ def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: boo
     return r
 
 
-def _token_rows(t, heads: int, d: int, what: str) -> int:
+def _token_rows(t, shape: tuple, what: str) -> int:
     """The token stride of ``t [n_tokens][heads][d]`` whose heads are contiguous."""
-    if tuple(t.shape[1:]) != (heads, d) or (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
-        raise ValueError(f"rope_append: {what} is [n_tokens][{heads}][{d}], contiguous but for its token stride")
-    return int(t.stride(0))
+    s = t.stride()
+    if t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"rope_append: {what} is {list(shape)}, contiguous but for its token stride")
+    return s[0]
 
 
 def rope_append(d: Dims, rope: Rope, q, k, v, q_out, seqs, rows, k_out, v_out, q_norm=None, k_norm=None,
                 eps: float = 1e-6, stream=None):
     """Queue fdkv_rope_append: ``q [n][Hq][d]``, ``k`` / ``v [n][Hkv][d]`` (views of one fused projection, say),
     ``k_out`` / ``v_out [batch][Hkv][cap][d]``; ``seqs`` None: token i is of sequence i."""
-    n, hd = int(q.shape[0]), d.head_dim
-    qs = _token_rows(q, d.n_q_heads, hd, "q")
-    ks, vs = _token_rows(k, d.n_kv_heads, hd, "k"), _token_rows(v, d.n_kv_heads, hd, "v")
-    if k.shape[0] != n or v.shape[0] != n or rows.numel() != n or (seqs is not None and seqs.numel() != n) or \
+    n, hkv, hd = q.shape[0], d.n_kv_heads, d.head_dim
+    heads, kv = (n, d.n_q_heads, hd), (n, hkv, hd)
+    qs, ks, vs = _token_rows(q, heads, "q"), _token_rows(k, kv, "k"), _token_rows(v, kv, "v")
+    batch, kh, cap, kd = k_out.shape
+    if rows.shape != (n,) or (seqs is not None and seqs.shape != (n,)) or \
             (rope.rot_dim and rope.tensors[1].shape[-1] != n):
         raise ValueError("rope_append: q, k, v, rows, seqs and the positions hold the same tokens")
-    if q_out.numel() != n * d.n_q_heads * hd or not q_out.is_contiguous() or not k_out.is_contiguous() or \
-            not v_out.is_contiguous() or k_out.shape != v_out.shape or tuple(k_out.shape[1::2]) != (d.n_kv_heads, hd):
+    if q_out.shape != heads or kh != hkv or kd != hd or v_out.shape != k_out.shape or \
+            not (q_out.is_contiguous() and k_out.is_contiguous() and v_out.is_contiguous()):
         raise ValueError("rope_append: q_out is [n][Hq][d], k_out and v_out [batch][Hkv][cap][d], all contiguous")
-    _check(load().fdkv_rope_append(ctypes.byref(d), n, ctypes.byref(rope), _dev(q), qs, _dev(k), ks, _dev(v), vs,
-                                   _dev(q_norm), _dev(k_norm), ctypes.c_float(eps), _dev(q_out), int(k_out.shape[0]),
-                                   _dev(seqs), _dev(rows), int(k_out.shape[2]), _dev(k_out), _dev(v_out),
-                                   _stream(stream)), "fdkv_rope_append")
+    st = (_lib or load()).fdkv_rope_append(
+        ctypes.byref(d), n, ctypes.byref(rope), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _dev(q_norm),
+        _dev(k_norm), eps, q_out.data_ptr(), batch, _dev(seqs), rows.data_ptr(), cap, k_out.data_ptr(),
+        v_out.data_ptr(), _stream(stream))
+    if st:
+        _check(st, "fdkv_rope_append")
 
 
 # ----------------------------------------------------------------- sparse decode: the index and the selection

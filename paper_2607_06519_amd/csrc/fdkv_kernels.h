@@ -208,7 +208,7 @@ struct AppendParams {
 };
 
 // the rows of a step, normed and rotated, on their way into the exact cache
-constexpr int kRopeTokens = 4;      // tokens of a workgroup of a long call ...
+constexpr int kRopeTokens = 2;      // tokens of a workgroup of a long call ...
 constexpr int kRopeMany = 1024;     // ... one of at least this many tokens
 struct RopeParams {
   DivU by_rows, by_pairs;      // division by hq + 2 hkv and rot / 2
@@ -226,7 +226,7 @@ struct RopeParams {
   void* k_out;                 // [batch][hkv][cap][d]
   void* v_out;
   float eps;
-  int n_tokens, hq, hkv, d, rot, batch, cap, tokens_per_wg;
+  int n_tokens, hq, hkv, d, rot, batch, cap;
   bool interleaved, bf16;
   uint8_t axis[64];            // axis of every pair
 };
