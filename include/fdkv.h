@@ -272,6 +272,9 @@ fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, in
  * in fp64.  Selected are the n_first first and the n_last last blocks of the
  * sequence and the best others, ties to the lower block, n_sel in all; a
  * sequence of at most n_sel blocks selects them all.
+ * Bounds and queries are finite numbers: a U that is NaN ranks its block last, an
+ * infinite one ranks none of its head's blocks (what is written are valid block
+ * numbers all the same).
  *   seq_lens    device int32 [batch], 0 <= T_i <= max_seq_len
  *   bounds      device [batch][Hkv][ceil(max_seq_len / 64)][2][d] (fdkv_key_bounds with that blocks_cap)
  *   q           device [batch][Hq][d]

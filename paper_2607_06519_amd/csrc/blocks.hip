@@ -183,10 +183,14 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
 }
 
 // ---------------------------------------------------------------- choice
-constexpr int kChooseThreads = 1024;
+// (Eight waves: 512 blocks of a sequence 5.2 us, 256 4.8; sixteen, with more to exchange and to wait for, 6.1 and 5.9.  At
+// 2048 blocks both take 11.)
+constexpr int kChooseThreads = 512;
 constexpr int kChooseWaves = kChooseThreads / 64;
-constexpr int kChooseBins = 1024;
-constexpr int kChooseList = 1024;
+constexpr int kChooseBins = 512;
+constexpr int kChooseList = 512;
+static_assert(kChooseWaves >= 8, "a wave for every query head of a group");
+static_assert(kChooseList <= kChooseThreads && kChooseThreads >= 256, "a rank of the list, and a digit, a thread");
 
 constexpr int kChooseHeld = 4096;  // ranks that a workgroup keeps in LDS (32 KB)
 
@@ -224,8 +228,8 @@ __global__ __launch_bounds__(kChooseThreads) void block_choose_kernel(SelectPara
   double* sc = P.ws + (uint64_t)sh * G * P.cap;
   double* rank = HELD ? held : sc;
 
-  // Every head's best block: 16 / G waves a head (sixteen waves share four SIMDs, so a reduction of every head in
-  // every wave would cost G times its instructions).
+  // Every head's best block: 8 / G waves a head (a reduction of every head in every wave would cost G times its
+  // instructions).
   constexpr int WPH = kChooseWaves / G;
   double mine[G];  // the thread's first block, requested with the others
 #pragma unroll

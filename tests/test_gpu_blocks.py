@@ -165,3 +165,29 @@ def test_captured_selection(torch_dev):
         call(eager)
         torch.cuda.synchronize()
         assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1]), step
+
+
+@pytest.mark.parametrize("what", ["nan_block", "inf_block", "all_nan", "inf_query"])
+def test_selection_of_what_is_not_a_number(torch_dev, what):
+    """Block numbers stay valid, ascending and distinct, whatever the bounds hold; the ends are among them."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    print(f"[case] not a number: {what}", flush=True)
+    T, n_sel = 6000, 20
+    nb = -(-T // 64)
+    bounds = torch.randn(1, 2, nb, 2, 128, generator=torch.Generator().manual_seed(1)).sort(3)[0].to(torch.bfloat16)
+    q = torch.randn(1, 2, 4, 128, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    if what == "nan_block":
+        bounds[:, :, 7, :, 3] = float("nan")
+    elif what == "inf_block":
+        bounds[:, :, 7, 1, 3] = float("inf")
+    elif what == "all_nan":
+        bounds[:] = float("nan")
+    else:
+        q[:, :, 1, 5] = float("inf")
+    blocks, counts = _select(torch, B, B.dims(2, 2, 8, 128, 0, "bf16"), [T], bounds.cuda(), q.cuda(), 1, 2, n_sel)
+    assert (counts == n_sel).all()
+    for row in blocks:
+        assert (np.diff(row) > 0).all() and row[0] == 0 and row[-2:].tolist() == [nb - 2, nb - 1]
+        if what == "nan_block":
+            assert 7 not in row
