@@ -5,12 +5,15 @@
 // decode calls do.
 //
 // The columns of a wave's matrix products are query rows: the G heads of a
-// sequence's group, or, over a shared span, the rows of the whole batch, 16 NQ of
-// them, so that a shared token is read and rebuilt once for all.  A wave walks
-// tiles of TOK = 32 tokens (16 in fp32) by itself, with no barrier before the
-// final merge of the workgroup's four waves:
+// sequence's group, or, over a shared span, 16 NQ rows of the whole batch, so that
+// a shared token is read and rebuilt once for all of them.  It walks tiles of TOK =
+// 32 tokens (16 in fp32): up to 16 rows every wave has tiles of its own and there is
+// no barrier before the merge of the workgroup's four waves; with more rows the four
+// waves take 16 NQ rows each of the same tile, which they stage together, and two
+// barriers a tile hand it over:
 //   S^T = K~ Q^T   A: 16 tokens x 32 channels straight from memory in the
-//                  operand's layout, B: the queries, kept in registers;
+//                  operand's layout (the four waves' tile: from LDS), B: the
+//                  queries, kept in registers;
 //   softmax        a column lives on the four lanes l, l + 16, l + 32, l + 48, its
 //                  logits in their registers; running max (moved only by more
 //                  than 2^8) and sum in fp32;
@@ -28,13 +31,13 @@
 // as M; no rebuilt value is rounded and no entry is gathered per query row.
 // Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
 //
-// What bounds it: HBM as long as 16 NQ columns are busy with less than the time
-// a tile takes to arrive (a CU gets some 13 bytes a cycle; a tile of 16 KB on one
-// SIMD of it takes 5000 cycles, its products at 64 columns 1100).
+// What bounds it.  Parts of single sequences: HBM where a wave has several tiles (selected blocks of 16 sequences' fp8
+// caches, all heads exact: 32.7 us a layer for 135 MB), else the way to the first one, three trips to memory that need
+// each other (what the launch says; lengths, offsets and blocks; rows): 64 blocks of one sequence take 10 us for 18 MB.
+// Shared spans: HBM for plain heads, and for residual ones the placing of their entries in R.  16 sequences of four
+// heads on 32768 tokens (bf16, pairs of k = 16): 41 us a layer for 161 MB, 3.9 TB/s, tails included; of eight heads on
+// 131072 tokens with token-level sets 140 us for 564 MB, 4.0 TB/s, with all heads plain 116 us, 4.8 TB/s.
 #pragma once
-#ifndef PARTS_DEPTH
-#define PARTS_DEPTH 2
-#endif
 
 #include <type_traits>
 
@@ -155,7 +158,7 @@ enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
 // walk would wait for every load in flight.
 constexpr int parts_per_cu(int KIND, bool q4) { return KIND == kManyEntries && q4 ? 1 : 2; }
 
-// LDS of a workgroup.  A token group's: the V tile, then R with a row behind it that takes what has no place (CG > 1:
+// LDS of a workgroup.  A token group's: the V tile, then R with a row behind it that takes what has no place (CG = 4:
 // the K tile, and R of K, of V and, where K's has one, of K's rest).
 template <int D, int CG, int TY, bool q4>
 struct PartsLds {
@@ -170,12 +173,14 @@ struct PartsLds {
 };
 
 // CG column groups of 16 NQ columns each, a wave apiece, by TG = 4 / CG token
-// groups.  With CG > 1 the waves of a token group walk the same tiles: each
-// stages its share of K and V, one places the residual entries of K, one those of
-// V (one the rest of K's), and two barriers a tile hand the tiles over.
+// groups: CG = 1, four waves with tiles of their own, or CG = 4, four that walk the
+// same tiles.  There each stages its share of K and V, one places the residual
+// entries of K, one those of V (one the rest of K's), and two barriers a tile hand
+// the tiles over.
 template <int D, int NQ, int CG, int TY, int KIND, bool q4>
 __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide& L, uint32_t w, uint8_t* lds, float (*ml_lds)[16][2]) {
   using namespace parts;
+  static_assert(CG == 4 || (CG == 1 && NQ == 1), "the launched forms");
   using S = TileOf<D, TY>;
   constexpr bool F32 = S::F32;
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
@@ -221,8 +226,8 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   int head = (int)(w - sl * hkv), seq = (int)by_slots.div(sl);  // (shared: sequence 0)
   int slot = (int)sl - seq * n_slots, chunk0 = slot, head_slots = 0;
   if (res_cost) {
-    // A residual head's tokens take longer, and one workgroup to a CU is all there is: the workgroups go to the heads
-    // by what their tokens take.  Lane h: head h.
+    // A residual head's tokens take longer and all workgroups run at once, so that the slowest head's would be waited
+    // for: the workgroups go to the heads by what their tokens take.  Lane h: head h.
     const uint32_t b = lane < hkv ? pt.modes[block * hkv + lane] : 0u;
     uint32_t c = lane < hkv ? (mode_of(b) == kResidual ? (uint32_t)res_cost : 16u) : 0u;
 #pragma unroll
@@ -293,7 +298,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   const int n_tiles = picked && T > 0 ? min(max(n_picked, 0), pt.n_sel) * S::TPB : (T + TOK - 1) / TOK;  // of the part
   if (my_block < 0 || my_block >= (T + kBlockTokens - 1) / kBlockTokens) my_block = -1;
   const int end = min(chunk0 + tiles_per_wg, n_tiles);
-  // the wave's tiles: chunk0 + tg + TG i, i < n (CG > 1: the same number for every wave, for the barriers)
+  // the wave's tiles: chunk0 + tg + TG i, i < n (CG = 4: the same number for every wave, for the barriers)
   const int n = CG == 1 ? (chunk0 + tg < end ? (end - chunk0 - tg + TG - 1) / TG : 0) : (end - chunk0 + TG - 1) / TG;
 
   // The scale's sign goes to the queries, so that a column's largest product is its largest logit; a scale of zero
@@ -323,12 +328,12 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   }
 
   uint8_t* vt = lds + tg * kGroupLds;                  // the V tile
-  uint8_t* kt = vt + S::TILE_BYTES;                    // CG > 1: the K tile
+  uint8_t* kt = vt + S::TILE_BYTES;                    // CG = 4: the K tile
   uint8_t* r_k = kt + (CG == 1 ? 0 : S::TILE_BYTES);   // R of K, of V, of K's rest (CG == 1: one after the other)
   uint8_t* r_v = CG == 1 ? r_k : r_k + kRt;
   uint8_t* r_rest = CG == 1 ? r_k : r_k + 2 * kRt;
-  // CG > 1: the wave's tile of R (0: K, 1: V, 2: K's rest; CG == 2: wave 0 has K's rest too)
-  const int role = CG == 1 ? 0 : cg, roles = CG == 4 && REST ? 3 : 2;
+  // CG = 4: the wave's tile of R (0: K, 1: V, 2: K's rest)
+  const int role = CG == 1 ? 0 : cg, roles = REST ? 3 : 2;
   uint8_t* rt = r_k + (CG == 1 ? 0 : role < roles ? role : 0) * kRt;
   // Hands LDS tiles from the waves that wrote them to those that read them.
   auto hand_over = [&]() __attribute__((always_inline)) {
@@ -340,15 +345,16 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
 
   // The walk is compiled for each kind of unit, so that every load of a tile is
   // issued unconditionally (a tile that the wave has not takes the out-of-range
-  // offset) and the compiler can wait for exactly the loads it needs: with the
-  // block size and the entries a lane decided at run time a residual unit's tile
-  // took 11 us instead of TODO.
+  // offset) and the compiler can wait for exactly the loads it needs.  (With the
+  // block size and the entries a lane decided at run time it waits for all of them:
+  // a residual unit's tile took 11 us.)
   auto walk = [&](auto c8_tag, auto res_tag) __attribute__((always_inline)) {
     constexpr bool C8 = decltype(c8_tag)::value;       // shared planes and residual values in E4M3
     constexpr int RES = decltype(res_tag)::value ? KIND : 0;
     constexpr bool ENT = RES == kFewEntries || RES == kManyEntries, SET = RES == kTokenSet;
-    // tiles in flight behind the current one
-    constexpr int DEPTH = CG == 1 || NQ == 2 ? 1 : PARTS_DEPTH;
+    // tiles in flight behind the current one: two where the registers hold them.  (CG = 1 has four tiles of K and V in
+    // flight a workgroup as it is, and 32 columns a wave leave no room for a second.)
+    constexpr int DEPTH = CG == 4 && NQ == 1 ? 2 : 1;
     constexpr int NCH = RES == kManyEntries ? 2 : 1;   // chunks of eight entries a lane that travel ahead
     constexpr int C = C8 ? 1 : S::E;                   // bytes of a stored coefficient
     constexpr int NLD = C8 ? NL / 2 : NL;              // loads of a tile's K (V)
@@ -371,7 +377,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
     // (whole 16-byte pieces: a load whose last word lies half behind the bytes would read 0 for all of it.  The
     // plane's padding may hold anything; entries of tokens behind the last are not used.)
     const uint32_t ibr = (ib + 15) & ~15u, xbr = (xb + 15) & ~15u;
-    // (CG > 1: the wave reads the entries of its role, K's or V's, into what is K's buffer here)
+    // (CG = 4: the wave reads the entries of its role, K's or V's, into what is K's buffer here)
     const uint64_t k_at = CG > 1 && role == 1 ? (uint64_t)ip + xp : 0;
     const uint32_t live = CG > 1 && role >= roles ? 0u : ~0u;
     const auto ikr = rsrc(ent + k_at, ibr & live), xkr = rsrc(ent + k_at + ip, xbr & live);
@@ -807,18 +813,12 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
       }
       if constexpr (CG > 1 && RES != 0) {
         if (has && role < roles) {
-          const bool rest = CG == 4 && REST && role == 2;
+          const bool rest = REST && role == 2;
           if constexpr (ENT) {
             place_all(b.ek, t0);
             scatter(rt, ikr, xkr, t0, rest);
           }
           if constexpr (SET) set_rows(rt, hkr, b.sk, mask, rank, rest);
-          if constexpr (CG == 2 && REST) {
-            if (role == 0) {
-              if constexpr (ENT) scatter(r_rest, ikr, xkr, t0, true);
-              if constexpr (SET) set_rows(r_rest, hkr, b.sk, mask, rank, true);
-            }
-          }
         }
         load_res(b);
       }
@@ -930,20 +930,12 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
       if constexpr (CG > 1) hand_over();
       if (has && role < roles) {
         clear_r(rt);
-        if constexpr (CG == 2 && REST) {
-          if (role == 0) clear_r(r_rest);
-        }
         lds_fence();
       }
     };
 
     if constexpr (RES != 0) {
-      if (role < roles) {
-        clear_r(rt);
-        if constexpr (CG == 2 && REST) {
-          if (role == 0) clear_r(r_rest);
-        }
-      }
+      if (role < roles) clear_r(rt);
     }
     Ahead ahead[DEPTH];
 #pragma unroll
