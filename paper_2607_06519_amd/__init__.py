@@ -5,5 +5,6 @@ hand-written HIP kernels under ``csrc/``; ``binding`` marshals torch tensors
 and numpy arrays into those calls.
 """
 from . import binding  # noqa: F401
-from .binding import (BF16, EXACT, F32, RESIDUAL, SHARED, Dims, FdkvError, compress,  # noqa: F401
-                      decode_attn, decode_workspace, dims, layout, probe, probe_workspace, route)
+from .binding import (BF16, EXACT, F32, RESIDUAL, SHARED, Dims, FdkvError, block_select,  # noqa: F401
+                      block_select_workspace, compress, decode_attn, decode_parts, decode_parts_workspace,
+                      decode_workspace, dims, key_bounds, layout, part, probe, probe_workspace, rope, rope_append, route)

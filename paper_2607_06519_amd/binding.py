@@ -341,6 +341,26 @@ def decode_spans(d: Dims, batch: int, spans: Sequence[Span], tail, layer: int, q
 
 
 # ----------------------------------------------------------------- a step's rows: norm, rotation, cache
+@functools.lru_cache(maxsize=None)
+def _element(dtype: int):
+    """The torch type of inputs, queries and outputs."""
+    import torch
+    return torch.float32 if dtype == F32 else torch.bfloat16
+
+
+def _operands(what: str, element, tensors, numbers=()):
+    """Refuses operands that a kernel would misread: ``tensors`` (each with the values that it holds at least) of another
+    element type, ``numbers`` that are not int32, any that is not contiguous, too short or on another device than the
+    current one."""
+    import torch
+    here = torch.cuda.current_device()
+    for t, n in tensors:
+        if t.dtype is not element or t.get_device() != here or t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{what}: {t.dtype} {list(t.shape)} on {t.device}, not {n} contiguous {element} on cuda:{here}")
+    if numbers:
+        _operands(what, torch.int32, numbers)
+
+
 def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: bool = False) -> Rope:
     """Rotary positions: ``inv_freq`` device float64 ``[rot_dim / 2]``, ``pos`` device int32 ``[n_tokens]``
     or ``[n_axes][n_tokens]``, ``axis`` the axis that each pair follows (default: axis 0).  The descriptor
@@ -355,35 +375,45 @@ def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: boo
         raise ValueError("rope: one axis for each of the rot_dim / 2 pairs")
     r = Rope(int(rot_dim), int(interleaved), n_axes, _dev(inv_freq), _dev(pos), (ctypes.c_uint8 * 64)(*axis))
     r.tensors = (inv_freq, pos)
+    r.n_tokens = int(pos.shape[-1])
     return r
-
-
-def _token_rows(t, shape: tuple, what: str) -> int:
-    """The token stride of ``t [n_tokens][heads][d]`` whose heads are contiguous."""
-    s = t.stride()
-    if t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
-        raise ValueError(f"rope_append: {what} is {list(shape)}, contiguous but for its token stride")
-    return s[0]
 
 
 def rope_append(d: Dims, rope: Rope, q, k, v, q_out, seqs, rows, k_out, v_out, q_norm=None, k_norm=None,
                 eps: float = 1e-6, stream=None):
     """Queue fdkv_rope_append: ``q [n][Hq][d]``, ``k`` / ``v [n][Hkv][d]`` (views of one fused projection, say),
     ``k_out`` / ``v_out [batch][Hkv][cap][d]``; ``seqs`` None: token i is of sequence i."""
-    n, hkv, hd = q.shape[0], d.n_kv_heads, d.head_dim
-    heads, kv = (n, d.n_q_heads, hd), (n, hkv, hd)
-    qs, ks, vs = _token_rows(q, heads, "q"), _token_rows(k, kv, "k"), _token_rows(v, kv, "v")
-    batch, kh, cap, kd = k_out.shape
-    if rows.shape != (n,) or (seqs is not None and seqs.shape != (n,)) or \
-            (rope.rot_dim and rope.tensors[1].shape[-1] != n):
-        raise ValueError("rope_append: q, k, v, rows, seqs and the positions hold the same tokens")
-    if q_out.shape != heads or kh != hkv or kd != hd or v_out.shape != k_out.shape or \
+    # (checks without loops and calls of their own, which would cost a call of 10 us two more)
+    import torch
+    hd, hkv = d.head_dim, d.n_kv_heads
+    n, hq, _ = heads = q.shape
+    kv = k.shape
+    qs, q1, q2 = q.stride()
+    ks, k1, k2 = k.stride()
+    vs, v1, v2 = v.stride()
+    if heads != (n, d.n_q_heads, hd) or kv != (n, hkv, hd) or v.shape != kv or not q2 == k2 == v2 == 1 or \
+            (q1 != hd and hq > 1) or (hkv > 1 and not k1 == v1 == hd):
+        raise ValueError("rope_append: q is [n][Hq][d], k and v [n][Hkv][d], contiguous but for their token strides")
+    batch, kh, cap, kd = cache = k_out.shape
+    if q_out.shape != heads or kh != hkv or kd != hd or v_out.shape != cache or \
             not (q_out.is_contiguous() and k_out.is_contiguous() and v_out.is_contiguous()):
         raise ValueError("rope_append: q_out is [n][Hq][d], k_out and v_out [batch][Hkv][cap][d], all contiguous")
+    e, i32, at = _element(d.dtype), torch.int32, torch.cuda.current_device()
+    if not (e is q.dtype is k.dtype is v.dtype is q_out.dtype is k_out.dtype is v_out.dtype) or \
+            not (at == q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == k_out.get_device() ==
+                 v_out.get_device() == rows.get_device()):
+        raise ValueError(f"rope_append: q, k, v and the outputs are {e}, all on the current device (cuda:{at})")
+    if rows.dtype is not i32 or rows.shape != (n,) or not rows.is_contiguous() or (rope.n_tokens != n and rope.rot_dim) or \
+            (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or
+                                   seqs.get_device() != at)):
+        raise ValueError(f"rope_append: rows and seqs are contiguous int32 [n] on cuda:{at}, the positions of n tokens")
+    if q_norm is not None or k_norm is not None:
+        _operands("rope_append", e, [(t, hd) for t in (q_norm, k_norm) if t is not None])
     st = (_lib or load()).fdkv_rope_append(
-        ctypes.byref(d), n, ctypes.byref(rope), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _dev(q_norm),
-        _dev(k_norm), eps, q_out.data_ptr(), batch, _dev(seqs), rows.data_ptr(), cap, k_out.data_ptr(),
-        v_out.data_ptr(), _stream(stream))
+        ctypes.byref(d), n, ctypes.byref(rope), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+        q_norm.data_ptr() if q_norm is not None else 0, k_norm.data_ptr() if k_norm is not None else 0, eps,
+        q_out.data_ptr(), batch, seqs.data_ptr() if seqs is not None else 0, rows.data_ptr(), cap, k_out.data_ptr(),
+        v_out.data_ptr(), torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
     if st:
         _check(st, "fdkv_rope_append")
 
@@ -393,6 +423,9 @@ def key_bounds(d: Dims, seq_len: int, k_layers: Sequence, bounds_layers: Sequenc
     """Queue fdkv_key_bounds: per layer ``k [Hkv][T][d]`` -> ``bounds [Hkv][blocks_cap][2][d]``."""
     if len(k_layers) != d.n_layers or len(bounds_layers) != d.n_layers:
         raise ValueError("key_bounds: one tensor of keys and one of bounds for every layer")
+    row = d.n_kv_heads * d.head_dim
+    nk, nb = int(seq_len) * row, int(blocks_cap) * 2 * row
+    _operands("key_bounds", _element(d.dtype), [(t, nk) for t in k_layers] + [(t, nb) for t in bounds_layers])
     _check(load().fdkv_key_bounds(ctypes.byref(d), int(seq_len), _ptr_array(k_layers), _ptr_array(bounds_layers),
                                   int(blocks_cap), _stream(stream)), "fdkv_key_bounds")
 
@@ -407,6 +440,10 @@ def block_select_workspace(d: Dims, batch: int, max_seq_len: int) -> int:
 def block_select(d: Dims, batch: int, seq_lens, max_seq_len: int, bounds, q, n_first: int, n_last: int, n_sel: int,
                  blocks_out, counts_out, ws, stream=None):
     """Queue fdkv_block_select for one layer: ``blocks_out [batch][Hkv][n_sel]``, ``counts_out [batch][Hkv]`` int32."""
+    units = int(batch) * d.n_kv_heads
+    _operands("block_select", _element(d.dtype),
+              ((bounds, units * -(-int(max_seq_len) // BLOCK_TOKENS) * 2 * d.head_dim), (q, int(batch) * d.n_q_heads * d.head_dim)),
+              ((seq_lens, int(batch)), (blocks_out, units * int(n_sel)), (counts_out, units)))
     _check(load().fdkv_block_select(ctypes.byref(d), int(batch), _dev(seq_lens), int(max_seq_len), _dev(bounds),
                                     _dev(q), int(n_first), int(n_last), int(n_sel), _dev(blocks_out),
                                     _dev(counts_out), _dev(ws), int(ws.numel() * ws.element_size()),
@@ -434,6 +471,8 @@ def decode_parts_workspace(d: Dims, batch: int, parts: Sequence[Part], tail_cap:
 def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q, out, sm_scale: float, ws,
                  stream=None):
     """Queue fdkv_decode_parts for one layer; ``parts`` are ``Part`` descriptors, ``tail`` a ``Tail`` or None."""
+    n = int(batch) * d.n_q_heads * d.head_dim
+    _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
     arr = _array_type(Part, max(len(parts), 1))(*parts)
     _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),

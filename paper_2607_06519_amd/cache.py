@@ -26,6 +26,10 @@ def torch_dtype(dtype: str):
     return {"bf16": torch.bfloat16, "bf16_e4m3": torch.bfloat16, "f32": torch.float32}[dtype]
 
 
+def _input_dtype(dims: B.Dims):
+    return torch_dtype({B.F32: "f32", B.BF16: "bf16", B.BF16_E4M3: "bf16_e4m3"}[dims.dtype])
+
+
 def to_device(x: np.ndarray, dtype: str, device="cuda"):
     """float32 numpy values (exactly representable in ``dtype``) -> device tensor."""
     torch = _torch()
@@ -52,6 +56,7 @@ class CompressedCache:
         self.seq_lens = torch.tensor(self.seq_lens_host, dtype=torch.int32, device=device)
         self.ws = torch.empty(B.decode_workspace(dims, self.batch, self.max_seq_len) // 4 + 64,
                               dtype=torch.float32, device=device)
+        self.bounds = None                                  # the index of a sparse decode (``index``)
 
     def compress(self, seq: int, k_layers, v_layers, stream=None, token_scores=None, k_select=None):
         """Write sequence ``seq`` from per-layer device tensors ``[Hkv][T][d]`` (``token_scores``
@@ -59,6 +64,17 @@ class CompressedCache:
         selections of the same keys, reused instead of selecting again)."""
         B.compress(self.dims, self.seq_lens_host[seq], k_layers, v_layers, self.modes[seq],
                    self.offsets[seq], self.buf, stream, token_scores, k_select)
+
+    def index(self, seq: int, k_layers, stream=None):
+        """Key bounds of sequence ``seq``, from the keys that ``compress`` takes: what a sparse decode
+        (``Generation`` with ``select``) chooses its blocks by.  ``bounds[l] [batch][Hkv][blocks][2][d]``."""
+        torch = _torch()
+        n = -(-self.max_seq_len // B.BLOCK_TOKENS)
+        if self.bounds is None:
+            shape = (self.batch, self.dims.n_kv_heads, n, 2, self.dims.head_dim)
+            self.bounds = [torch.zeros(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
+                           for _ in range(self.dims.n_layers)]
+        B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds], n, stream)
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         """One decode step of ``layer`` for queries ``q [batch][Hq][d]``; returns ``out``."""
@@ -100,16 +116,38 @@ class Generation:
     A decode step of one token, layer by layer: ``append(layer, k, v)`` puts
     the token's K / V rows at the tail's next row, ``decode(layer, q)``
     attends over every span and the tail including that row; ``advance()``
-    then moves the tail position once for all layers.
+    then moves the tail position once for all layers.  ``append_rotated``
+    stands in for ``append`` where the rows still need their norms and their
+    rotation by position.
+
+    ``shared``, a cache of one sequence, is a prefix that all sequences of the
+    batch continue: it is held and read once for all of them (``prefix`` may
+    then be None, with ``batch`` given).  ``select = (n_first, n_last, n_sel)``
+    makes the decode sparse: of ``prefix``, whose sequences have been indexed
+    (``CompressedCache.index``), a step reads per KV head the first and last
+    blocks of 64 tokens and those that can hold the largest logits, ``n_sel``
+    in all; every other span and the tail are read whole.
     """
 
-    def __init__(self, dims: B.Dims, prefix: "CompressedCache", tail_cap: int, device="cuda"):
+    def __init__(self, dims: B.Dims, prefix: Optional["CompressedCache"], tail_cap: int, device="cuda",
+                 shared: Optional["CompressedCache"] = None, select: Optional[Sequence[int]] = None,
+                 batch: Optional[int] = None):
         torch = _torch()
+        if prefix is None and (shared is None or batch is None or select is not None):
+            raise ValueError("a generation without a prefix of its own takes a shared one and its batch, and selects nothing")
+        if prefix is not None and batch not in (None, prefix.batch):
+            raise ValueError("the batch is the prefix's")
+        if shared is not None and shared.batch != 1:
+            raise ValueError("a shared prefix is a cache of one sequence")
+        if select is not None and prefix.bounds is None:
+            raise ValueError("a sparse decode selects by the prefix's key bounds: index its sequences first")
         self.dims = dims
-        self.batch = prefix.batch
-        self.spans = [prefix]
+        self.batch = prefix.batch if prefix is not None else int(batch)
+        self.spans = [prefix] if prefix is not None else []
+        self.shared = shared
+        self.select = None if select is None else tuple(int(n) for n in select)
         self.cap = int(tail_cap)
-        tdt = torch_dtype({B.F32: "f32", B.BF16: "bf16", B.BF16_E4M3: "bf16_e4m3"}[dims.dtype])
+        tdt = _input_dtype(dims)
         shape = (self.batch, dims.n_kv_heads, self.cap, dims.head_dim)
         self.tail_k = [torch.zeros(shape, dtype=tdt, device=device) for _ in range(dims.n_layers)]
         self.tail_v = [torch.zeros(shape, dtype=tdt, device=device) for _ in range(dims.n_layers)]
@@ -117,11 +155,29 @@ class Generation:
         self.pos = torch.zeros(self.batch, dtype=torch.int32, device=device)      # row the step writes
         self.lens = torch.zeros(self.batch, dtype=torch.int32, device=device)     # rows the step attends
         self._ws = None
+        if self.select is not None:
+            heads = (self.batch, dims.n_kv_heads)
+            self.blocks = torch.empty(heads + (self.select[2],), dtype=torch.int32, device=device)    # of the last decode
+            self.counts = torch.empty(heads, dtype=torch.int32, device=device)
+            n = B.block_select_workspace(dims, self.batch, prefix.max_seq_len)
+            self._select_ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=device)
         self._refresh_ws()
         self._begin_step()
 
     def _refresh_ws(self):
         torch = _torch()
+        if self.shared is not None or self.select is not None:
+            def part(kind, s, **chosen):
+                return B.part(kind, s.seq_lens, s.max_seq_len, s.modes, s.offsets, s.buf, **chosen)
+            self._parts = [] if self.shared is None else [part(B.PART_SHARED, self.shared)]
+            for i, s in enumerate(self.spans):
+                if i == 0 and self.select is not None:
+                    self._parts.append(part(B.PART_BLOCKS, s, blocks=self.blocks, counts=self.counts, n_sel=self.select[2]))
+                else:
+                    self._parts.append(part(B.PART_OWN, s))
+            n = B.decode_parts_workspace(self.dims, self.batch, self._parts, self.cap)
+            self._ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=self.pos.device)
+            return
         n = B.decode_spans_workspace(self.dims, self.batch, [s.max_seq_len for s in self.spans], self.cap)
         self._ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=self.pos.device)
         self._span_desc = [B.Span(int(s.seq_lens.data_ptr()), s.max_seq_len, int(s.modes.data_ptr()),
@@ -142,13 +198,32 @@ class Generation:
         B.append(self.dims, self.batch, self.pos, self.cap, k_new, v_new, self.tail_k[layer], self.tail_v[layer],
                  stream)
 
+    def append_rotated(self, layer: int, rope: B.Rope, q, k_new, v_new, q_norm=None, k_norm=None, eps: float = 1e-6,
+                       stream=None):
+        """``append`` of rows as the projections leave them: queries ``q [batch][Hq][d]`` and keys are
+        normed per head (where weights are given) and turned by ``rope``, keys and values go into the
+        tail.  Heads may lie in one fused projection's rows.  Returns the queries for ``decode``."""
+        if self.full:
+            raise RuntimeError("the tail is full: refresh before appending")
+        out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+        B.rope_append(self.dims, rope, q, k_new, v_new, out, None, self.pos, self.tail_k[layer], self.tail_v[layer],
+                      q_norm, k_norm, eps, stream)
+        return out
+
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         if out is None:
             out = _torch().empty_like(q)
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
         tail = B.Tail(int(self.lens.data_ptr()), self.cap, int(self.tail_k[layer].data_ptr()),
                       int(self.tail_v[layer].data_ptr()))
-        B.decode_spans(self.dims, self.batch, self._span_desc, tail, layer, q, out, scale, self._ws, stream)
+        if self.shared is None and self.select is None:
+            B.decode_spans(self.dims, self.batch, self._span_desc, tail, layer, q, out, scale, self._ws, stream)
+            return out
+        if self.select is not None:
+            s = self.spans[0]
+            B.block_select(self.dims, self.batch, s.seq_lens, s.max_seq_len, s.bounds[layer], q, *self.select,
+                           self.blocks, self.counts, self._select_ws, stream)
+        B.decode_parts(self.dims, self.batch, self._parts, tail, layer, q, out, scale, self._ws, stream)
         return out
 
     def advance(self):
