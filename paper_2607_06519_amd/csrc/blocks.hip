@@ -28,7 +28,7 @@
 // over their bit patterns follow.  Its last pass writes the selected blocks in
 // ascending order.
 #include "fdkv_common.h"
-#include "fdkv_kernels.h"
+#include "serving_kernels.h"
 
 namespace fdkv {
 

@@ -12,6 +12,7 @@
 #include "fdkv.h"
 #include "fdkv_common.h"
 #include "fdkv_kernels.h"
+#include "serving_kernels.h"
 #include "probe_split.h"
 
 using namespace fdkv;

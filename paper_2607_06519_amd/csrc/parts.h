@@ -43,7 +43,7 @@
 
 #include "decode_shape.h"
 #include "fdkv_common.h"
-#include "fdkv_kernels.h"
+#include "serving_kernels.h"
 
 namespace fdkv {
 

@@ -8,7 +8,7 @@
 // Bound by the way to memory and back: the records of one row are some 20 KB.
 #include "decode_shape.h"
 #include "fdkv_common.h"
-#include "fdkv_kernels.h"
+#include "serving_kernels.h"
 
 namespace fdkv {
 

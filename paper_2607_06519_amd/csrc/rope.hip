@@ -18,7 +18,7 @@
 // into LDS (one pair of a token a thread), then walks their rows, the next
 // row's loads requested before the current one is turned.
 #include "fdkv_common.h"
-#include "fdkv_kernels.h"
+#include "serving_kernels.h"
 
 namespace fdkv {
 
