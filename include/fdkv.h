@@ -257,6 +257,7 @@ fdkv_status fdkv_compress(const fdkv_dims* dims, int32_t seq_len, const void* co
  *   bounds_out  host array of L device pointers, out: [Hkv][blocks_cap][2][d] in the element type of the
  *               dims, row 0 the least and row 1 the largest; blocks past ceil(T / 64) are not written
  *   blocks_cap  >= ceil(T / 64)
+ * T <= 2^30 (FDKV_E_UNSUPPORTED otherwise).
  */
 fdkv_status fdkv_key_bounds(const fdkv_dims* dims, int32_t seq_len, const void* const* k_layers,
                             void* const* bounds_out, int32_t blocks_cap, void* stream);
@@ -283,7 +284,7 @@ fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, in
  *   blocks_out  device int32 [batch][Hkv][n_sel], out: block numbers, ascending, then -1
  *   counts_out  device int32 [batch][Hkv], out: min(n_sel, ceil(T_i / 64))
  *   ws          device workspace of fdkv_block_select_workspace() bytes, 8-byte aligned
- * batch x Hkv <= 65535 (FDKV_E_UNSUPPORTED otherwise).
+ * batch x Hkv <= 65535, max_seq_len <= 2^30, n_sel <= 2^24 (FDKV_E_UNSUPPORTED otherwise).
  */
 fdkv_status fdkv_block_select(const fdkv_dims* dims, int32_t batch, const int32_t* seq_lens, int32_t max_seq_len,
                               const void* bounds, const void* q, int32_t n_first, int32_t n_last, int32_t n_sel,
@@ -437,7 +438,7 @@ typedef struct {
  * rotated, query rows written to q_out, key and value rows to the cache.  With a
  * cache of one sequence and rows 0, 1, ... it lays a prompt's keys and values
  * out as fdkv_probe and fdkv_compress take them.
- *   n_tokens       tokens of the call, >= 0
+ *   n_tokens       tokens of the call, 0 .. 2^24 - 1 (FDKV_E_UNSUPPORTED above)
  *   q              device [n_tokens][Hq][d], q_stride elements from token to token
  *   k, v           device [n_tokens][Hkv][d], k_stride / v_stride elements from token to token
  *                  (a fused projection's output is all three, with one stride; a
@@ -521,6 +522,8 @@ fdkv_status fdkv_decode_parts_workspace(const fdkv_dims* dims, int32_t batch, in
  * are those of fdkv_decode_spans.  Rows of the tail at or past its length, and
  * what lies behind a span's tokens, are not used, whatever they hold.
  *   ws   device workspace of fdkv_decode_parts_workspace() bytes (FDKV_E_WORKSPACE if smaller)
+ * At most 2^23 record slots (batch x Hkv x the parts' chunks) and batch x Hq, n_sel <= 2^24
+ * (FDKV_E_UNSUPPORTED otherwise).
  * Probabilities are rounded to the element type for their product with V, their
  * sum is not; the order of fp32 sums depends on the batch and on the bounds.
  */

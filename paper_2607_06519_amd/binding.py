@@ -369,13 +369,15 @@ def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: boo
     n_axes = 1 if pos.dim() == 1 else int(pos.shape[0])
     if inv_freq.dtype != torch.float64 or pos.dtype != torch.int32 or pos.dim() > 2:
         raise ValueError("rope: inv_freq is float64, pos int32 [n_tokens] or [n_axes][n_tokens]")
+    if inv_freq.get_device() != pos.get_device():
+        raise ValueError("rope: inv_freq and pos lie on one device")
     if inv_freq.numel() < rot_dim // 2 or not inv_freq.is_contiguous() or not pos.is_contiguous():
         raise ValueError("rope: inv_freq holds rot_dim / 2 values; both tensors are contiguous")
     if len(axis) not in (0, rot_dim // 2) or rot_dim > 128:
         raise ValueError("rope: one axis for each of the rot_dim / 2 pairs")
     r = Rope(int(rot_dim), int(interleaved), n_axes, _dev(inv_freq), _dev(pos), (ctypes.c_uint8 * 64)(*axis))
     r.tensors = (inv_freq, pos)
-    r.n_tokens = int(pos.shape[-1])
+    r.n_tokens, r.device = int(pos.shape[-1]), pos.get_device()
     return r
 
 
@@ -403,7 +405,7 @@ def rope_append(d: Dims, rope: Rope, q, k, v, q_out, seqs, rows, k_out, v_out, q
             not (at == q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == k_out.get_device() ==
                  v_out.get_device() == rows.get_device()):
         raise ValueError(f"rope_append: q, k, v and the outputs are {e}, all on the current device (cuda:{at})")
-    if rows.dtype is not i32 or rows.shape != (n,) or not rows.is_contiguous() or (rope.n_tokens != n and rope.rot_dim) or \
+    if rows.dtype is not i32 or rows.shape != (n,) or not rows.is_contiguous() or (rope.rot_dim and (rope.n_tokens != n or rope.device != at)) or \
             (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or
                                    seqs.get_device() != at)):
         raise ValueError(f"rope_append: rows and seqs are contiguous int32 [n] on cuda:{at}, the positions of n tokens")
@@ -454,9 +456,15 @@ def block_select(d: Dims, batch: int, seq_lens, max_seq_len: int, bounds, q, n_f
 def part(kind: int, seq_lens, max_seq_len: int, modes, seg_offsets, cache, blocks=None, counts=None,
          n_sel: int = 0) -> Part:
     """A part of a decode step (PART_OWN, PART_BLOCKS or PART_SHARED); the descriptor keeps its tensors."""
+    import torch
+    for t, types in ((seq_lens, (torch.int32,)), (blocks, (torch.int32,)), (counts, (torch.int32,)), (modes, (torch.uint8, torch.int8)),
+                     (seg_offsets, (torch.int64, torch.uint64)), (cache, (cache.dtype,))):
+        if t is not None and (t.dtype not in types or not t.is_contiguous() or t.get_device() != cache.get_device()):
+            raise ValueError(f"part: {t.dtype} {list(t.shape)} on {t.device}, not contiguous {types[0]} on the cache's device")
     p = Part(int(kind), int(max_seq_len), int(n_sel), _dev(seq_lens), _dev(modes), _dev(seg_offsets), _dev(cache),
              _dev(blocks), _dev(counts))
     p.tensors = (seq_lens, modes, seg_offsets, cache, blocks, counts)
+    p.device = cache.get_device()
     return p
 
 
@@ -473,6 +481,9 @@ def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q
     """Queue fdkv_decode_parts for one layer; ``parts`` are ``Part`` descriptors, ``tail`` a ``Tail`` or None."""
     n = int(batch) * d.n_q_heads * d.head_dim
     _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
+    for p in parts:
+        if p.device != q.get_device():
+            raise ValueError("decode_parts: a part lies on another device than the queries")
     arr = _array_type(Part, max(len(parts), 1))(*parts)
     _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),

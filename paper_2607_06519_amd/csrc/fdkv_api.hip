@@ -174,6 +174,10 @@ uint64_t record_bytes(const fdkv_dims* d) { return (uint64_t)(d->n_q_heads / d->
 // blocks of sparse decode in T tokens
 int block_count(int T) { return (int)(((int64_t)T + kBlockTokens - 1) / kBlockTokens); }
 static_assert(kBlockTokens == FDKV_BLOCK_TOKENS, "the header's block");
+// A grid's threads (256 a workgroup) are counted in 32 bits, tokens, tiles and selected
+// blocks in int, with room for the last step of a loop over them.
+constexpr int64_t kMaxGroups = 1 << 23;
+constexpr int kMaxSelectTokens = 1 << 30, kMaxSelected = 1 << 24;
 
 uint64_t decode_chunks(int max_T) { return (uint64_t)(max_T + kDecodeWgTokens - 1) / kDecodeWgTokens; }
 
@@ -618,6 +622,7 @@ fdkv_status fdkv_rope_append(const fdkv_dims* dims, int32_t n_tokens, const fdkv
       (k_norm && !aligned(k_norm, 16)) || (rot > 0 && (!aligned(rope->inv_freq, 8) || !aligned(rope->pos, 4))))
     return FDKV_E_INVALID_ARG;
   if (q_out == q && q_stride != (int64_t)dims->n_q_heads * dims->head_dim && n_tokens > 1) return FDKV_E_INVALID_ARG;
+  if (n_tokens / kRopeTokens >= kMaxGroups) return FDKV_E_UNSUPPORTED;
   RopeParams rp{};
   rp.q = q;
   rp.k = k;
@@ -654,7 +659,9 @@ fdkv_status fdkv_key_bounds(const fdkv_dims* dims, int32_t seq_len, const void* 
                             void* const* bounds_out, int32_t blocks_cap, void* stream) {
   fdkv_status st = check_dims(dims);
   if (st != FDKV_OK) return st;
-  if (seq_len < 0 || !k_layers || !bounds_out || blocks_cap < block_count(seq_len)) return FDKV_E_INVALID_ARG;
+  if (seq_len < 0 || !k_layers || !bounds_out) return FDKV_E_INVALID_ARG;
+  if (seq_len > kMaxSelectTokens) return FDKV_E_UNSUPPORTED;
+  if (blocks_cap < block_count(seq_len)) return FDKV_E_INVALID_ARG;
   if (seq_len == 0) return FDKV_OK;
   for (int l = 0; l < dims->n_layers; ++l)
     if (!aligned(k_layers[l], 16) || !aligned(bounds_out[l], 16)) return FDKV_E_INVALID_ARG;
@@ -679,6 +686,7 @@ fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, in
   fdkv_status st = check_dims(dims);
   if (st != FDKV_OK) return st;
   if (batch < 1 || max_seq_len < 0 || !bytes) return FDKV_E_INVALID_ARG;
+  if (max_seq_len > kMaxSelectTokens) return FDKV_E_UNSUPPORTED;
   *bytes = (size_t)((uint64_t)batch * dims->n_q_heads * std::max(block_count(max_seq_len), 1) * 8);
   return FDKV_OK;
 }
@@ -690,6 +698,7 @@ fdkv_status fdkv_block_select(const fdkv_dims* dims, int32_t batch, const int32_
   fdkv_status st = fdkv_block_select_workspace(dims, batch, max_seq_len, &need);
   if (st != FDKV_OK) return st;
   if (n_sel < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_sel) return FDKV_E_INVALID_ARG;
+  if (n_sel > kMaxSelected) return FDKV_E_UNSUPPORTED;
   if (!aligned(seq_lens, 4) || !aligned(bounds, 16) || !aligned(q, 16) || !aligned(blocks_out, 4) ||
       !aligned(counts_out, 4) || !aligned(ws, 8))
     return FDKV_E_INVALID_ARG;
@@ -956,13 +965,14 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
     return FDKV_E_INVALID_ARG;
   const int tok = dims->dtype == FDKV_F32 ? 16 : 32;  // tokens of a tile
   const int64_t G = dims->n_q_heads / dims->n_kv_heads, hkv = dims->n_kv_heads;
-  if (batch * G * hkv >= (1ll << 30)) return FDKV_E_UNSUPPORTED;
+  if (batch * G * hkv > kMaxGroups) return FDKV_E_UNSUPPORTED;
   PartsPlan p{};
   int64_t tiles[kMaxParts], own_tiles = 0, shared_tiles = 0;
   for (int i = 0; i < n_parts; ++i) {
     const fdkv_part& pt = parts[i];
     if (pt.max_seq_len < 0 || pt.kind < FDKV_PART_OWN || pt.kind > FDKV_PART_SHARED) return FDKV_E_INVALID_ARG;
     if (pt.kind == FDKV_PART_BLOCKS && pt.n_sel < 1) return FDKV_E_INVALID_ARG;
+    if (pt.kind == FDKV_PART_BLOCKS && pt.n_sel > kMaxSelected) return FDKV_E_UNSUPPORTED;
     if (pt.kind == FDKV_PART_SHARED) {
       p.shared[p.n_shared++] = i;
       shared_tiles += ((int64_t)pt.max_seq_len + tok - 1) / tok;
@@ -1016,8 +1026,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
     p.slots[p.n_own] = p.shared_wgs * hkv * p.res_cost / (p.res_cost + 16 * (hkv - 1)) + 1;
     p.total_slots = p.own_slots + p.slots[p.n_own];
   }
-  // workgroups and record slots are counted in 31 bits
-  if (batch * hkv * std::max<int64_t>(p.total_slots, 1) >= (1ll << 30) || (hkv * p.total_slots + 8) * p.row_groups >= (1ll << 30))
+  if (batch * hkv * std::max<int64_t>(p.total_slots, 1) > kMaxGroups || (hkv * p.total_slots + 8) * p.row_groups > kMaxGroups)
     return FDKV_E_UNSUPPORTED;
   *out = p;
   return FDKV_OK;

@@ -191,3 +191,23 @@ def test_selection_of_what_is_not_a_number(torch_dev, what):
         assert (np.diff(row) > 0).all() and row[0] == 0 and row[-2:].tolist() == [nb - 2, nb - 1]
         if what == "nan_block":
             assert 7 not in row
+
+
+def test_more_blocks_than_a_workgroup_holds(torch_dev):
+    """Sequences of more than 4096 blocks keep their ranks in the workspace."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    print("[case] 300000 tokens", flush=True)
+    for dtype, d, G, lens, n_sel in (("bf16", 64, 4, [300000, 100], 100), ("f32", 64, 8, [262145, 262144], 4000), ("bf16", 128, 1, [600001], 1)):
+        dt = torch.float32 if dtype == "f32" else torch.bfloat16
+        g = torch.Generator().manual_seed(lens[0])
+        cap = -(-max(lens) // 64)
+        mid, rad = torch.randn(len(lens), 2, cap, d, generator=g), torch.rand(len(lens), 2, cap, d, generator=g)
+        bounds = torch.stack([mid - rad, mid + rad], 3).to(dt)
+        q = torch.randn(len(lens), 2, G, d, generator=g).to(dt)
+        for first, last in ((0, 0), (0, 1)):
+            want = _want(bounds.double().numpy(), q.double().numpy(), lens, first, last, n_sel)
+            _same(*_select(torch, B, B.dims(2, 2, 2 * G, d, 0, dtype), lens, bounds.cuda(), q.cuda(), first, last, n_sel), want, n_sel)
+    bounds[:] = bounds[:, :, :1]                                 # every rank alike: the lowest blocks
+    want = [[0, 1, 2, 3, 9375]] * 2
+    _same(*_select(torch, B, B.dims(2, 2, 2, d, 0, dtype), lens, bounds.cuda(), q.cuda(), 1, 1, 5), want, 5)

@@ -206,6 +206,12 @@ def test_refusals(torch_dev):
         B.key_bounds(dm, 100, [torch.zeros(2, 99, 128, dtype=st.dt, device="cuda")] * 2, [torch.zeros(2, 2, 2, 128, dtype=st.dt, device="cuda")] * 2, 2)
     with pytest.raises(ValueError):
         B.block_select(dm, st.batch, st.prefix.seq_lens.long(), st.prefix.max_seq_len, st.prefix.bounds[0], good, 0, 0, 4, gen.blocks, gen.counts, gen._select_ws)
+    c = st.shared
+    for bad in (dict(seq_lens=c.seq_lens.long()), dict(modes=c.modes.int()), dict(seg_offsets=c.offsets.int()), dict(seq_lens=c.seq_lens.cpu())):
+        with pytest.raises(ValueError):
+            B.part(B.PART_SHARED, **{**dict(seq_lens=c.seq_lens, max_seq_len=300, modes=c.modes, seg_offsets=c.offsets, cache=c.buf), **bad})
+    with pytest.raises(ValueError):
+        B.rope(128, st.freq, st.pos)
     fresh = make_cache(torch, dm, [100] * st.batch, _modes(dm, st.batch, 1), 5)[0]
     for kw in (dict(prefix=fresh, select=(0, 1, 4)), dict(prefix=None), dict(prefix=None, shared=st.shared), dict(prefix=fresh, shared=fresh),
                dict(prefix=None, shared=st.shared, batch=2, select=(0, 0, 1)), dict(prefix=fresh, batch=7)):

@@ -45,6 +45,7 @@ def test_rope_append_refuses(lib):
         assert call(**{name: -256}) == -1 and call(**{name: 260}) == -1 and call(**{name: 1 << 62}) == -1, name
     assert call(q=P, qo=P, qs=2048) == -1                       # in place only where the rows are contiguous
     assert call(dims=B.dims(2, 2, 6, 128, 0, "bf16")) == -2
+    assert call(n=1 << 24) == -2 and call(n=2147483647) == -2
 
 
 def test_key_bounds_refuses(lib):
@@ -54,6 +55,7 @@ def test_key_bounds_refuses(lib):
     assert call(T=0, cap=0) == 0
     assert call(T=-1) == -1 and call(k=None) == -1 and call(out=None) == -1 and call(cap=1) == -1
     assert call(k=bad) == -1 and call(out=bad) == -1
+    assert call(T=2147483647, cap=1 << 26) == -2
     with pytest.raises(ValueError):
         B.key_bounds(dm, 100, [], [], 2)
 
@@ -71,6 +73,7 @@ def test_block_select_refuses(lib):
     for name, off in (("lens", 2), ("bounds", 8), ("q", 8), ("blocks", 2), ("counts", 1), ("ws", 4)):
         assert call(**{name: None}) == -1 and call(**{name: P + off}) == -1, name
     assert call(batch=32768, n=1 << 62) == -2
+    assert call(T=2147483647, n=1 << 62) == -2 and call(sel=(1 << 24) + 1) == -2 and call(sel=2147483647) == -2
 
 
 def _part(kind=0, T=100, n_sel=0, lens=P, modes=P, offs=P, cache=P, blocks=None, counts=None):
@@ -105,7 +108,10 @@ def test_decode_parts_refuses(lib):
     n = ctypes.c_size_t(0)
     assert lib.fdkv_decode_parts_workspace(ctypes.byref(dm), 2, 0, None, -1, ctypes.byref(n)) == 0 and n.value == 2 * 2 * 4 * 132 * 4
     assert lib.fdkv_decode_parts_workspace(ctypes.byref(dm), 2, 0, None, -1, None) == -1
-    assert lib.fdkv_decode_parts_workspace(ctypes.byref(dm), 1 << 30, 0, None, -1, ctypes.byref(n)) == -2
+    for batch in ((1 << 20) + 1, 1 << 30, 2147483647):
+        assert lib.fdkv_decode_parts_workspace(ctypes.byref(dm), batch, 0, None, -1, ctypes.byref(n)) == -2
+    assert call(parts=[_part(kind=1, n_sel=(1 << 24) + 1, blocks=P, counts=P)]) == -2
+    assert call(parts=[_part(T=1 << 22)], batch=1 << 18) == -2   # more record slots than a launch has workgroups
 
 
 def test_parts_workspace(lib):
