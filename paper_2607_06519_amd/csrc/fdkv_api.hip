@@ -959,6 +959,21 @@ int parts_res_cost(const fdkv_dims* dims) {
   return quads ? 28 : 24;
 }
 
+// Query rows of a workgroup of the shared parts.  A layer of 8 KV heads and 32768 tokens, every width at every number
+// of rows (us):
+//   bf16, pairs of k = 16           16 rows: by 16 40.2, by 64 41.1   32: 45.4, 42.0   64: 62.4, 44.3   96: by 64 62.0, by 128 49.5
+//   bf16, blocks of four            16 rows: by 16 37.3, by 64 45.3   32: 41.6, 46.1   48: 53.1, 46.8
+//   E4M3, pairs                     16 rows: by 16 30.5, by 64 39.2   32: 35.1, 40.0   48: 42.9, 40.7
+//   E4M3, blocks of four            16 rows: by 16 30.1, by 64 44.0   32: 35.1, 44.7   64: 53.2, 46.5   160: by 64 106, by 128 86
+//   fp32, pairs of k = 16           32 rows: by 16 83, by 64 161      64: 134, 163     80: by 16 170, by 128 218   128: 248, 222
+// (fp32 products bound the last: 16 rows a workgroup have no barriers, 128 rows half the reads of LDS a product.)
+int parts_cols(const fdkv_dims* dims, int64_t rows) {
+  if (rows <= 16) return 16;
+  if (dims->dtype == FDKV_F32) return (rows + 15) / 16 > (rows + 127) / 128 * 7 ? 128 : 16;
+  if (rows <= 32 && (dims->schedule != FDKV_SCHED_PAIRS || dims->dtype == FDKV_BF16_E4M3)) return 16;
+  return rows <= 64 ? 64 : 128;
+}
+
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
                        PartsPlan* out) {
   if (batch < 1 || n_parts < 0 || n_parts + (tail_cap >= 0 ? 1 : 0) > kMaxParts || (n_parts > 0 && !parts))
@@ -1005,7 +1020,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   while (p.own_tiles_per_wg < 256 && chunks(p.own_tiles_per_wg) > p.n_own && chunks(p.own_tiles_per_wg) * batch * hkv > kPartsWorkgroups)
     p.own_tiles_per_wg += 4;
   p.rows = (int)(batch * G);
-  p.cols = p.n_shared == 0 || p.rows <= 16 ? 16 : p.rows <= 64 ? 64 : 128;
+  p.cols = p.n_shared == 0 ? 16 : parts_cols(dims, p.rows);
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
   // (Workgroups of 64 rows: three to two CUs, as more of them write more records and leave the own parts to the end.  Per
   // layer, 32768 tokens, 16 sequences and their tails: 384 workgroups 46.5 us, 256 48.3, 512 49.9.  Of 128 rows, two to

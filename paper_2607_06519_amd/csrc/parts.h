@@ -1050,12 +1050,16 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
 template <int D, int TY, int KIND, bool q4>
 static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
   const dim3 grid(P.shared_wgs + (uint32_t)P.hkv * (uint32_t)P.side[0].n_slots * (uint32_t)P.batch), block(256);
-  if (P.cols == 16)
+  if (P.cols == 16) {
     hipLaunchKernelGGL((parts_kernel<D, 1, 1, TY, KIND, q4>), grid, block, 0, s, P);
-  else if (P.cols == 64)
-    hipLaunchKernelGGL((parts_kernel<D, 1, 4, TY, KIND, q4>), grid, block, 0, s, P);
-  else
+  } else if (P.cols == 128) {
     hipLaunchKernelGGL((parts_kernel<D, 2, 4, TY, KIND, q4>), grid, block, 0, s, P);
+  } else {
+    if constexpr (TY != parts::kTyF32)  // (fp32: 16 or 128)
+      hipLaunchKernelGGL((parts_kernel<D, 1, 4, TY, KIND, q4>), grid, block, 0, s, P);
+    else
+      return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 

@@ -14,10 +14,11 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("rows", [64, 128])
 @pytest.mark.parametrize("name", list(KINDS))
 def test_wide_kernels(torch_dev, name, rows):
-    """17 to 64 rows take four column groups of one tile, more than 64 four of two; ragged in their last tile."""
+    """33 to 64 rows take four column groups of one tile, more than 64 four of two (fp32: up to 112 rows groups of 16);
+    ragged in their last tile."""
     dims, dtype, layers = _kind(name)
     G = dims.n_q_heads // dims.n_kv_heads
-    batch = {64: 40, 128: 100}[rows] // G + 1
+    batch = {64: 40, 128: 120}[rows] // G + 1
     log(f"[case] wide {name} {batch} x {G}")
     layer = dims.n_layers - 1
     Case(torch_dev, dims, dtype, batch, 300 + rows, shared=(219,), tail=(9, [s % 10 for s in range(batch)])).check((layer,), name)
