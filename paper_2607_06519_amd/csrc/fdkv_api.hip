@@ -950,13 +950,15 @@ struct PartsPlan {
 constexpr int64_t kPartsWorkgroups = 512;
 
 // A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
-// dimension 128): one head's share of the workgroups.
-int parts_res_cost(const fdkv_dims* dims) {
-  const bool quads = dims->schedule != FDKV_SCHED_PAIRS;
-  if (tokens_mode(dims)) return quads ? 32 : 24;
-  if (dims->topk == 0) return 16;
-  if (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16)) return 40;
-  return quads ? 28 : 24;
+// dimension 128): one head's share of the workgroups.  0: every head takes as many.  A layer of 32768 tokens, four plain
+// heads, three residual and an exact one, by cost and all alike (us): 64 rows of bf16 pairs 41 and 48, 56 of E4M3 blocks
+// of four 46 and 65, 28 of bf16 with k = 24 45 and 58; up to 16 rows, where every workgroup's waves have tiles of their
+// own and memory bounds a residual head too, 40 and 37.
+int parts_res_cost(const fdkv_dims* dims, const PartsPlan& p) {
+  if (p.rows <= 16) return 0;
+  if (!tokens_mode(dims) && dims->topk == 0) return 0;
+  const bool many = !tokens_mode(dims) && (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16));
+  return dims->schedule != FDKV_SCHED_PAIRS || many ? 28 : 24;
 }
 
 // Query rows of a workgroup of the shared parts.  A layer of 8 KV heads and 32768 tokens, every width at every number
@@ -1037,7 +1039,9 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // One shared part: its workgroups are dealt to the heads by cost, so a residual head may take more record slots than
   // the average, at most as many as if it were the only one.  (With few workgroups a head the shares round too far.)
   if (p.n_shared == 1 && hkv <= 64 && p.shared_wgs >= 4 && p.shared_wgs * hkv < (1 << 20)) {
-    p.res_cost = parts_res_cost(dims);
+    p.res_cost = parts_res_cost(dims, p);
+  }
+  if (p.res_cost) {
     p.slots[p.n_own] = p.shared_wgs * hkv * p.res_cost / (p.res_cost + 16 * (hkv - 1)) + 1;
     p.total_slots = p.own_slots + p.slots[p.n_own];
   }
