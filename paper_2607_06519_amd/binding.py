@@ -405,7 +405,8 @@ def rope_append(d: Dims, rope: Rope, q, k, v, q_out, seqs, rows, k_out, v_out, q
             not (at == q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == k_out.get_device() ==
                  v_out.get_device() == rows.get_device()):
         raise ValueError(f"rope_append: q, k, v and the outputs are {e}, all on the current device (cuda:{at})")
-    if rows.dtype is not i32 or rows.shape != (n,) or not rows.is_contiguous() or (rope.rot_dim and (rope.n_tokens != n or rope.device != at)) or \
+    if rows.dtype is not i32 or rows.shape != (n,) or not rows.is_contiguous() or \
+            (rope.rot_dim and (rope.n_tokens != n or rope.device != at)) or \
             (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or
                                    seqs.get_device() != at)):
         raise ValueError(f"rope_append: rows and seqs are contiguous int32 [n] on cuda:{at}, the positions of n tokens")
@@ -425,11 +426,20 @@ def key_bounds(d: Dims, seq_len: int, k_layers: Sequence, bounds_layers: Sequenc
     """Queue fdkv_key_bounds: per layer ``k [Hkv][T][d]`` -> ``bounds [Hkv][blocks_cap][2][d]``."""
     if len(k_layers) != d.n_layers or len(bounds_layers) != d.n_layers:
         raise ValueError("key_bounds: one tensor of keys and one of bounds for every layer")
-    row = d.n_kv_heads * d.head_dim
+    # (a tensor's checks and its address in one pass, as a call takes some 10 us)
+    import torch
+    e, at, row = _element(d.dtype), torch.cuda.current_device(), d.n_kv_heads * d.head_dim
     nk, nb = int(seq_len) * row, int(blocks_cap) * 2 * row
-    _operands("key_bounds", _element(d.dtype), [(t, nk) for t in k_layers] + [(t, nb) for t in bounds_layers])
-    _check(load().fdkv_key_bounds(ctypes.byref(d), int(seq_len), _ptr_array(k_layers), _ptr_array(bounds_layers),
-                                  int(blocks_cap), _stream(stream)), "fdkv_key_bounds")
+    k = [t.data_ptr() for t in k_layers
+         if t.dtype is e and t.get_device() == at and t.is_contiguous() and t.numel() >= nk]
+    b = [t.data_ptr() for t in bounds_layers
+         if t.dtype is e and t.get_device() == at and t.is_contiguous() and t.numel() >= nb]
+    if len(k) != len(k_layers) or len(b) != len(bounds_layers):
+        raise ValueError(f"key_bounds: keys and bounds are contiguous {e} on cuda:{at}, {nk} and {nb} values a layer")
+    pointers = _array_type(ctypes.c_void_p, d.n_layers)
+    _check((_lib or load()).fdkv_key_bounds(ctypes.byref(d), int(seq_len), pointers(*k), pointers(*b), int(blocks_cap),
+                                            torch._C._cuda_getCurrentRawStream(at) if stream is None else
+                                            stream.cuda_stream), "fdkv_key_bounds")
 
 
 def block_select_workspace(d: Dims, batch: int, max_seq_len: int) -> int:

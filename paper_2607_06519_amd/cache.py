@@ -57,6 +57,7 @@ class CompressedCache:
         self.ws = torch.empty(B.decode_workspace(dims, self.batch, self.max_seq_len) // 4 + 64,
                               dtype=torch.float32, device=device)
         self.bounds = None                                  # the index of a sparse decode (``index``)
+        self.indexed = [t == 0 for t in self.seq_lens_host]
 
     def compress(self, seq: int, k_layers, v_layers, stream=None, token_scores=None, k_select=None):
         """Write sequence ``seq`` from per-layer device tensors ``[Hkv][T][d]`` (``token_scores``
@@ -74,7 +75,9 @@ class CompressedCache:
             shape = (self.batch, self.dims.n_kv_heads, n, 2, self.dims.head_dim)
             self.bounds = [torch.zeros(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
                            for _ in range(self.dims.n_layers)]
-        B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds], n, stream)
+        if self.seq_lens_host[seq]:
+            B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds], n, stream)
+        self.indexed[seq] = True
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         """One decode step of ``layer`` for queries ``q [batch][Hq][d]``; returns ``out``."""
@@ -139,7 +142,7 @@ class Generation:
             raise ValueError("the batch is the prefix's")
         if shared is not None and shared.batch != 1:
             raise ValueError("a shared prefix is a cache of one sequence")
-        if select is not None and prefix.bounds is None:
+        if select is not None and (prefix.bounds is None or not all(prefix.indexed)):
             raise ValueError("a sparse decode selects by the prefix's key bounds: index its sequences first")
         self.dims = dims
         self.batch = prefix.batch if prefix is not None else int(batch)
@@ -220,6 +223,8 @@ class Generation:
             B.decode_spans(self.dims, self.batch, self._span_desc, tail, layer, q, out, scale, self._ws, stream)
             return out
         if self.select is not None:
+            if scale < 0:
+                raise ValueError("a sparse decode selects the largest q . k, which a negative scale turns into the least")
             s = self.spans[0]
             B.block_select(self.dims, self.batch, s.seq_lens, s.max_seq_len, s.bounds[layer], q, *self.select,
                            self.blocks, self.counts, self._select_ws, stream)

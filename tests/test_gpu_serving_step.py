@@ -117,10 +117,12 @@ def test_steps(torch_dev, dtype, sched, kw):
         st.gen.advance()
 
 
-def test_refresh_and_the_steps_after(torch_dev):
+@pytest.mark.parametrize("kw", [{}, dict(lens=None, select=None), dict(shared=0)], ids=["both", "shared", "selected"])
+def test_refresh_and_the_steps_after(torch_dev, kw):
     """The tail becomes a span of its own, read whole beside the selected blocks and the shared prefix."""
     torch = torch_dev
-    st = Step(torch, "bf16", cap=5)
+    st = Step(torch, "bf16", cap=5, **kw)
+    spans = len(st.gen.spans)
     for i in range(5):
         st.new_inputs(100 + i)
         st.run()
@@ -131,7 +133,7 @@ def test_refresh_and_the_steps_after(torch_dev):
     dm = st.dims
     probes = [torch.randn(st.batch, dm.n_q_heads, 4, dm.head_dim, generator=st.g).to(st.dt).cuda() for _ in range(dm.n_layers)]
     st.gen.refresh(probes, 4, lam=0.01)
-    assert len(st.gen.spans) == 2
+    assert len(st.gen.spans) == spans + 1
     for i in range(2):
         st.new_inputs(105 + i)
         st.run()
@@ -217,5 +219,10 @@ def test_refusals(torch_dev):
                dict(prefix=None, shared=st.shared, batch=2, select=(0, 0, 1)), dict(prefix=fresh, batch=7)):
         with pytest.raises(ValueError):
             Generation(dm, kw.pop("prefix"), 4, **kw)
+    with pytest.raises(ValueError):
+        gen.decode(0, good, sm_scale=-0.1)
+    fresh.index(0, [torch.zeros(2, 100, 128, dtype=st.dt, device="cuda")] * 2)
+    with pytest.raises(ValueError):                               # the other sequences have no bounds
+        Generation(dm, fresh, 4, select=(0, 1, 4))
     with pytest.raises(B.FdkvError):
         Step(torch, "bf16", select=(3, 3, 4)).run()
