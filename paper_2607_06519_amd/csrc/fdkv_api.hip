@@ -949,31 +949,40 @@ struct PartsPlan {
 // Workgroups that fill the card: two to a CU.
 constexpr int64_t kPartsWorkgroups = 512;
 
-// A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
-// dimension 128): one head's share of the workgroups.  0: every head takes as many.  A layer of 32768 tokens, four plain
-// heads, three residual and an exact one, by cost and all alike (us): 64 rows of bf16 pairs 41 and 48, 56 of E4M3 blocks
-// of four 46 and 65, 28 of bf16 with k = 24 45 and 58; up to 16 rows, where every workgroup's waves have tiles of their
-// own and memory bounds a residual head too, 40 and 37.
-int parts_res_cost(const fdkv_dims* dims, const PartsPlan& p) {
-  if (p.rows <= 16) return 0;
-  if (!tokens_mode(dims) && dims->topk == 0) return 0;
-  const bool many = !tokens_mode(dims) && (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16));
-  return dims->schedule != FDKV_SCHED_PAIRS || many ? 28 : 24;
+// Residual entries of a token by which the kernels differ: parts.h's kManyEntries.
+bool parts_many(const fdkv_dims* dims) {
+  return !tokens_mode(dims) && (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16));
 }
 
-// Query rows of a workgroup of the shared parts.  A layer of 8 KV heads and 32768 tokens, every width at every number
-// of rows (us):
-//   bf16, pairs of k = 16           16 rows: by 16 40.2, by 64 41.1   32: 45.4, 42.0   64: 62.4, 44.3   96: by 64 62.0, by 128 49.5
-//   bf16, blocks of four            16 rows: by 16 37.3, by 64 45.3   32: 41.6, 46.1   48: 53.1, 46.8
-//   E4M3, pairs                     16 rows: by 16 30.5, by 64 39.2   32: 35.1, 40.0   48: 42.9, 40.7
-//   E4M3, blocks of four            16 rows: by 16 30.1, by 64 44.0   32: 35.1, 44.7   64: 53.2, 46.5   160: by 64 106, by 128 86
-//   fp32, pairs of k = 16           32 rows: by 16 83, by 64 161      64: 134, 163     80: by 16 170, by 128 218   128: 248, 222
-// (fp32 products bound the last: 16 rows a workgroup have no barriers, 128 rows half the reads of LDS a product.)
+// A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
+// dimension 128): one head's share of the workgroups.  0: every head takes as many.  A layer of 32768 tokens, four plain
+// heads, three residual and an exact one, by cost and all alike (us): 64 rows of bf16 pairs 41 and 48, 28 of bf16 with
+// k = 24 45 and 58, 64 of fp32 133 and 143; up to 16 rows, where memory bounds a residual head too, 40 and 37.
+int parts_res_cost(const fdkv_dims* dims, const PartsPlan& p) {
+  if (p.rows <= 16 || (!tokens_mode(dims) && dims->topk == 0)) return 0;
+  return dims->schedule != FDKV_SCHED_PAIRS || parts_many(dims) ? 28 : 24;
+}
+
+// Query rows of a workgroup of the shared parts: 16 or 32 by waves with tiles of their own, 64 or 128 by four waves of one
+// tile.  A layer of 8 KV heads and 32768 tokens, times by width (us):
+//                                   32 rows                        64 rows                          128 rows
+//   bf16, pairs of k = 16           16: 45.4  32: 43.0  64: 42.0   16: 62.4  32: 48.2  64: 44.3     32: 65.4  128: 53.0
+//   bf16, blocks of four            16: 41.6  32: 40.1  64: 46.1   16: 61.2  32: 44.3  64: 47.6     32: 65.5  128: 54.0
+//   E4M3, pairs                     16: 35.1  32: 33.5  64: 40.0   16: 48.8  32: 38.3  64: 41.6     32: 53.1  128: 49.1
+//   E4M3, blocks of four            16: 35.1  32: 33.9  64: 44.7   16: 53.2  32: 41.2  64: 46.5     32: 61.1  128: 53.7
+//   bf16, pairs of k = 24           16: 48.7  32: 65.9  64: 44.7   16: 64.9  32: 86.4  64: 46.7     32: 136   128: 55
+//   bf16, blocks of four of k = 24  16: 65.7                       64: 74.3
+//   fp32, pairs of k = 16           16: 83    32: 106   64: 161    16: 134   32: 151   64: 163      16: 248   128: 222
+// (At 16 rows, by 16 and by 64: 37.4 and 41.1, 36.6 and 45.3, 28.4 and 39.2, 28.0 and 44.0; at 160, by 64 and by 128: 85 and
+// 73 bf16 pairs, 106 and 86 E4M3 blocks of four.  32 columns a wave spill with many entries and in fp32, whose products
+// bound it besides: 80 rows by 16 take 170, by 128 218.)
 int parts_cols(const fdkv_dims* dims, int64_t rows) {
+  const bool by_four_or_e4m3 = dims->schedule != FDKV_SCHED_PAIRS || dims->dtype == FDKV_BF16_E4M3;
   if (rows <= 16) return 16;
   if (dims->dtype == FDKV_F32) return (rows + 15) / 16 > (rows + 127) / 128 * 7 ? 128 : 16;
-  if (rows <= 32 && (dims->schedule != FDKV_SCHED_PAIRS || dims->dtype == FDKV_BF16_E4M3)) return 16;
-  return rows <= 64 ? 64 : 128;
+  if (rows > 64) return 128;
+  if (by_four_or_e4m3) return !parts_many(dims) ? 32 : rows <= 32 ? 16 : 64;
+  return 64;
 }
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
@@ -1028,7 +1037,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   // layer, 32768 tokens, 16 sequences and their tails: 384 workgroups 46.5 us, 256 48.3, 512 49.9.  Of 128 rows, two to
   // a CU: 131072 tokens 152 us, with 384 164.)
   const int64_t wgs = p.cols == 64 ? kPartsWorkgroups * 3 / 4 : kPartsWorkgroups;
-  p.shared_tiles_per_wg = per_wg(shared_tiles, wgs / (hkv * p.row_groups), p.cols == 16 ? 4 : 1, 1 << 28);
+  p.shared_tiles_per_wg = per_wg(shared_tiles, wgs / (hkv * p.row_groups), p.cols <= 32 ? 4 : 1, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
   for (int i = 0; i < p.n_shared; ++i) {
@@ -1038,9 +1047,8 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   p.total_slots += p.shared_wgs;
   // One shared part: its workgroups are dealt to the heads by cost, so a residual head may take more record slots than
   // the average, at most as many as if it were the only one.  (With few workgroups a head the shares round too far.)
-  if (p.n_shared == 1 && hkv <= 64 && p.shared_wgs >= 4 && p.shared_wgs * hkv < (1 << 20)) {
+  if (p.n_shared == 1 && hkv <= 64 && p.shared_wgs >= 4 && p.shared_wgs * hkv < (1 << 20))
     p.res_cost = parts_res_cost(dims, p);
-  }
   if (p.res_cost) {
     p.slots[p.n_own] = p.shared_wgs * hkv * p.res_cost / (p.res_cost + 16 * (hkv - 1)) + 1;
     p.total_slots = p.own_slots + p.slots[p.n_own];

@@ -7,10 +7,10 @@
 // The columns of a wave's matrix products are query rows: the G heads of a
 // sequence's group, or, over a shared span, 16 NQ rows of the whole batch, so that
 // a shared token is read and rebuilt once for all of them.  It walks tiles of TOK =
-// 32 tokens (16 in fp32): up to 16 rows every wave has tiles of its own and there is
-// no barrier before the merge of the workgroup's four waves; with more rows the four
-// waves take 16 NQ rows each of the same tile, which they stage together, and two
-// barriers a tile hand it over:
+// 32 tokens (16 in fp32): workgroups of 16 or 32 rows have waves with tiles of their
+// own and no barrier before the merge of their records; in those of 64 or 128 rows
+// the four waves take 16 NQ rows each of the same tile, which they stage together,
+// and two barriers a tile hand it over:
 //   S^T = K~ Q^T   A: 16 tokens x 32 channels straight from memory in the
 //                  operand's layout (the four waves' tile: from LDS), B: the
 //                  queries, kept in registers;
@@ -174,13 +174,13 @@ struct PartsLds {
 
 // CG column groups of 16 NQ columns each, a wave apiece, by TG = 4 / CG token
 // groups: CG = 1, four waves with tiles of their own, or CG = 4, four that walk the
-// same tiles.  There each stages its share of K and V, one places the residual
+// same tiles.  There each wave stages its share of K and V, one places the residual
 // entries of K, one those of V (one the rest of K's), and two barriers a tile hand
 // the tiles over.
 template <int D, int NQ, int CG, int TY, int KIND, bool q4>
 __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide& L, uint32_t w, uint8_t* lds, float (*ml_lds)[16][2]) {
   using namespace parts;
-  static_assert(CG == 4 || (CG == 1 && NQ == 1), "the launched forms");
+  static_assert(CG == 4 || CG == 1, "the launched forms");
   using S = TileOf<D, TY>;
   constexpr bool F32 = S::F32;
   constexpr int TOK = S::TOK, RB = S::RB, NP = S::NP, RPL = S::RPL, NL = S::NL, KK = S::KK, TI = S::TI, CT = S::CT;
@@ -1038,7 +1038,7 @@ __global__ __launch_bounds__(256, parts_per_cu(KIND, q4)) void parts_kernel(Part
   __shared__ __attribute__((aligned(1024))) uint8_t lds[own > both ? own : both];
   __shared__ float ml_lds[4][16][2];
   const bool shared = blockIdx.x < P.shared_wgs;
-  if constexpr (CG > 1) {
+  if constexpr (CG * NQ > 1) {
     if (shared) {
       parts_body<D, NQ, CG, TY, KIND, q4>(P, P.side[1], blockIdx.x, lds, ml_lds);
       return;
@@ -1054,8 +1054,13 @@ static hipError_t launch_parts_kind(const PartsParams& P, hipStream_t s) {
     hipLaunchKernelGGL((parts_kernel<D, 1, 1, TY, KIND, q4>), grid, block, 0, s, P);
   } else if (P.cols == 128) {
     hipLaunchKernelGGL((parts_kernel<D, 2, 4, TY, KIND, q4>), grid, block, 0, s, P);
+  } else if (P.cols == 32) {  // (where parts_cols has it)
+    if constexpr (TY != parts::kTyF32 && KIND != kManyEntries)
+      hipLaunchKernelGGL((parts_kernel<D, 2, 1, TY, KIND, q4>), grid, block, 0, s, P);
+    else
+      return hipErrorInvalidValue;
   } else {
-    if constexpr (TY != parts::kTyF32)  // (fp32: 16 or 128)
+    if constexpr (TY != parts::kTyF32 && (KIND == kManyEntries || (TY == parts::kTyBf16 && !q4)))
       hipLaunchKernelGGL((parts_kernel<D, 1, 4, TY, KIND, q4>), grid, block, 0, s, P);
     else
       return hipErrorInvalidValue;

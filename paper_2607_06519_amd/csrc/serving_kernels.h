@@ -89,7 +89,7 @@ struct PartsParams {
   int res_ppm, n_rates;
   int rates_ppm[kMaxRates];
   bool tokres, bf16, coef8;
-  int cols;                    // query rows of a workgroup of the shared parts: 16, 64 or 128
+  int cols;                    // query rows of a workgroup of the shared parts: 16, 32, 64 or 128
 };
 
 struct PartsMergeParams {

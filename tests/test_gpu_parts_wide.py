@@ -14,8 +14,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("rows", [64, 128])
 @pytest.mark.parametrize("name", list(KINDS))
 def test_wide_kernels(torch_dev, name, rows):
-    """33 to 64 rows take four column groups of one tile, more than 64 four of two (fp32: up to 112 rows groups of 16);
-    ragged in their last tile."""
+    """Up to 64 rows go by 32 or 64, more than 64 by 128 (fp32: up to 112 rows by 16); ragged in their last tile."""
     dims, dtype, layers = _kind(name)
     G = dims.n_q_heads // dims.n_kv_heads
     batch = {64: 40, 128: 120}[rows] // G + 1
