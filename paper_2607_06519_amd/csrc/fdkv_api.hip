@@ -1035,8 +1035,13 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
   // (Workgroups of 64 rows: three to two CUs, as more of them write more records and leave the own parts to the end.  Per
   // layer, 32768 tokens, 16 sequences and their tails: 384 workgroups 46.5 us, 256 48.3, 512 49.9.  Of 128 rows, two to
-  // a CU: 131072 tokens 152 us, with 384 164.)
-  const int64_t wgs = p.cols == 64 ? kPartsWorkgroups * 3 / 4 : kPartsWorkgroups;
+  // a CU: 131072 tokens 152 us, with 384 164.  Up to 32 rows, one to a CU, whose four waves have eight tiles in flight:
+  // 32768 tokens, 12 rows, 256 and 512 workgroups: bf16 pairs 37.6 and 38.5 us, E4M3 pairs 27.1 and 31.2, E4M3 blocks of
+  // four 31.2 and 30.9, fp32 (4096 tokens) 21.6 and 25.2; several groups of rows: 64 by 32, E4M3 39.2 and 38.8, fp32 by
+  // 16 177 and 134.)
+  const int64_t wgs = p.cols == 64                          ? kPartsWorkgroups * 3 / 4
+                      : p.cols <= 32 && p.row_groups == 1 ? kPartsWorkgroups / 2
+                                                          : kPartsWorkgroups;
   p.shared_tiles_per_wg = per_wg(shared_tiles, wgs / (hkv * p.row_groups), p.cols <= 32 ? 4 : 1, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
