@@ -940,7 +940,8 @@ struct PartsPlan {
   int n_own, n_shared;          // parts (the tail among the own ones)
   int own[kMaxParts], shared[kMaxParts];  // their indices in the call; -1: the tail
   int own_tiles_per_wg, shared_tiles_per_wg, cols, rows, row_groups;
-  int res_cost;                 // PartsParams::res_cost
+  int res_cost;                 // PartsSide::res_cost
+  int by_cost;                  // PartsSide::by_cost
   int64_t shared_wgs;           // workgroups of a row group and head of the shared parts, on average
   int64_t slots[kMaxParts];     // record slots of each part, own ones first
   int64_t own_slots, total_slots;
@@ -1045,6 +1046,14 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   p.shared_tiles_per_wg = per_wg(shared_tiles, wgs / (hkv * p.row_groups), p.cols <= 32 ? 4 : 1, 1 << 28);
   for (int i = 0; i < p.n_own; ++i) p.own_slots += p.slots[i] = (tiles[i] + p.own_tiles_per_wg - 1) / p.own_tiles_per_wg;
   p.total_slots = p.own_slots;
+  // Where the own parts' workgroups fill the second place of the CUs, and none waits for one, costly heads are put beside
+  // cheap ones.  It takes another trip to memory (0.3 us), so only for walks of some length.  16 sequences, 32 blocks of
+  // each and a tail, 8 KV heads of every kind, a layer (us, selection included), so and in the order of the heads: E4M3
+  // blocks of four 39.2 and 42.3, E4M3 pairs 37.2 and 39.8, fp32 83.7 and 88.3, bf16 pairs 47.7 and 49.3; 33 sequences
+  // (528 workgroups) 92.2 and 90.9, 83.8 and 78.6, 248 and 248, 110 and 108.
+  const int64_t own_wgs = batch * hkv * p.own_slots;
+  p.by_cost = p.n_shared == 0 && hkv > 1 && hkv <= 64 && p.own_tiles_per_wg >= 16 && own_wgs > kPartsWorkgroups / 2 &&
+              own_wgs <= kPartsWorkgroups;
   for (int i = 0; i < p.n_shared; ++i) {
     const int64_t n = ((int64_t)parts[p.shared[i]].max_seq_len + tok - 1) / tok;
     p.shared_wgs += p.slots[p.n_own + i] = (n + p.shared_tiles_per_wg - 1) / p.shared_tiles_per_wg;
@@ -1185,6 +1194,7 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
     side.n_slots = (int)(shared ? plan.shared_wgs : plan.own_slots);
     side.shared = shared;
     side.res_cost = shared ? plan.res_cost : 0;
+    side.by_cost = shared ? 0 : plan.by_cost;
     side.rows = shared ? plan.rows : p.G;
     side.row_groups = shared ? plan.row_groups : 1;
     side.tiles_per_wg = shared ? plan.shared_tiles_per_wg : plan.own_tiles_per_wg;

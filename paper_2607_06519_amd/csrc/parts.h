@@ -197,7 +197,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   // piece a trip to memory)
   DivU by_slots = L.by_slots, by_hkv = P.by_hkv, by_groups = L.by_groups, by_topk = P.by_topk;
   int hkv = P.hkv, hq = P.hq, G = P.G, g_shift = P.g_shift, n_slots = L.n_slots, tiles_per_wg = L.tiles_per_wg;
-  int res_cost = L.res_cost, row_groups = L.row_groups, rows = L.rows, n_blocks = P.n_blocks, block = P.block, slot0 = L.slot0;
+  int res_cost = L.res_cost, row_groups = L.row_groups, rows = L.rows, by_cost = L.by_cost, n_blocks = P.n_blocks, block = P.block, slot0 = L.slot0;
   int shared = L.shared, pos = P.pos, nb = P.bsize, k = P.topk, tail_cap = P.tail_cap, n_slots_total = P.n_slots_total;
   const void *q_all = P.q, *tail_k = P.tail_k, *tail_v = P.tail_v;
   float *ws = P.ws, w1 = P.wres[0], w2 = P.wres[1], w3 = P.wres[2], scale_log2 = P.scale_log2;
@@ -205,7 +205,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   int base1 = L.part_base[1], base2 = L.part_base[2];
   asm volatile("" : "+s"(by_slots.mul), "+s"(by_slots.shift), "+s"(by_hkv.mul), "+s"(by_hkv.shift), "+s"(by_groups.mul),
                "+s"(by_groups.shift), "+s"(hkv), "+s"(hq), "+s"(G), "+s"(g_shift), "+s"(n_slots), "+s"(tiles_per_wg),
-               "+s"(row_groups), "+s"(rows), "+s"(res_cost));
+               "+s"(row_groups), "+s"(rows), "+s"(res_cost), "+s"(by_cost));
   asm volatile("" : "+s"(n_blocks), "+s"(block), "+s"(slot0), "+s"(shared), "+s"(q_all), "+s"(base1), "+s"(base2), "+s"(pt.lens),
                "+s"(pt.cache), "+s"(pt.modes), "+s"(pt.seg_off), "+s"(pt.blocks), "+s"(pt.counts), "+s"(pt.n_sel), "+s"(pt.max_len));
   asm volatile("" : "+s"(pt1.lens), "+s"(pt1.cache), "+s"(pt1.modes), "+s"(pt1.seg_off), "+s"(pt1.blocks), "+s"(pt1.counts),
@@ -254,6 +254,20 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
   }
   slot += slot0;
   const bool tail = pt.cache == nullptr, picked = pt.n_sel > 0;
+  if (by_cost && !tail) {
+    // Workgroups w and w + 256 share a CU (where every CU has one before any has two): the first 256 take the heads by
+    // rising cost, the next by falling, so that a residual or exact head meets a shared one.  Lane h: head h.
+    const uint32_t md = lane < hkv ? (uint32_t)mode_of(pt.modes[((uint64_t)seq * n_blocks + block) * hkv + lane]) : 4u;
+    int rank = 0, before = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < 4; ++c) {
+      const uint64_t of = __ballot(md == c);
+      rank = md == c ? before + __builtin_popcountll(of & ((1ull << lane) - 1)) : rank;
+      before += __builtin_popcountll(of);
+    }
+    const int place = (sl * hkv >> 8) & 1u ? hkv - 1 - head : head;  // (one order for all heads of the chunk)
+    head = __builtin_ctzll(__ballot(lane < hkv && rank == place));
+  }
 
   // ---- queries, requested first (a column past the rows repeats the last one's and is zeroed)
   auto row_of = [&](int col, int& s, int& g) __attribute__((always_inline)) {  // (sequence, head of the group)

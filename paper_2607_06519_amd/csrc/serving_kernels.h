@@ -69,6 +69,7 @@ struct PartsSide {
   int slot0, shared;           // first record slot
   int res_cost;                // a residual head's time per token, a plain one's being 16; 0: every head takes n_slots
                                // workgroups (shared parts only)
+  int by_cost;                 // the workgroups of a (sequence, chunk) go to the heads in the order of their cost
   int part_base[kMaxParts];    // first slot of each part, from 0; INT32_MAX past the last
   PartsPart part[kMaxParts];
 };

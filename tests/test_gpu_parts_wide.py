@@ -98,3 +98,21 @@ def test_calls_on_two_streams_at_once(torch_dev):
     torch.cuda.synchronize()
     for w, o in zip(want, outs):
         assert all(torch.equal(w, x) for x in o)
+
+
+@pytest.mark.parametrize("kv", [2, 5, 8, 64])
+@pytest.mark.parametrize("dtype,sched", [("bf16_e4m3", 2), ("bf16", 0)])
+def test_heads_in_the_order_of_their_cost(torch_dev, monkeypatch, kv, dtype, sched):
+    """More workgroups than CUs, walks of 16 tiles and more: every head is taken once, whatever the modes are."""
+    def modes(dims, n, seed):
+        from paper_2607_06519_amd import binding as B
+        rng = np.random.default_rng(seed)
+        m = rng.integers(0, 3, (n, len(B.blocks(dims)[0]), dims.n_kv_heads)).astype(np.uint8)
+        m[0], m[-1] = 1, 2                                        # all alike
+        return m
+    monkeypatch.setattr(parts, "_modes", modes)
+    batch = -(-300 // kv)
+    log(f"[case] order {dtype} {kv} heads, {batch} sequences")
+    lens = [300 + (97 * s) % 300 for s in range(batch)]
+    dims = _dims(dtype, kv, 1, 64, 8, sched)
+    Case(torch_dev, dims, dtype, batch, 800 + kv, own=(lens,)).check((1,), f"{dtype} {kv}")
