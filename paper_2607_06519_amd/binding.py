@@ -492,7 +492,7 @@ def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q
     n = int(batch) * d.n_q_heads * d.head_dim
     _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
     for p in parts:
-        if p.device != q.get_device():
+        if getattr(p, "device", q.get_device()) != q.get_device():
             raise ValueError("decode_parts: a part lies on another device than the queries")
     arr = _array_type(Part, max(len(parts), 1))(*parts)
     _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
