@@ -68,13 +68,16 @@ class CompressedCache:
 
     def index(self, seq: int, k_layers, stream=None):
         """Key bounds of sequence ``seq``, from the keys that ``compress`` takes: what a sparse decode
-        (``Generation`` with ``select``) chooses its blocks by.  ``bounds[l] [batch][Hkv][blocks][2][d]``."""
+        (``Generation`` with ``select``) chooses its blocks by.  ``bounds[l] [batch][Hkv][blocks][2][d]``;
+        blocks behind a sequence are left unwritten, as nothing reads them."""
         torch = _torch()
         n = -(-self.max_seq_len // B.BLOCK_TOKENS)
         if self.bounds is None:
             shape = (self.batch, self.dims.n_kv_heads, n, 2, self.dims.head_dim)
-            self.bounds = [torch.zeros(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
+            self.bounds = [torch.empty(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
                            for _ in range(self.dims.n_layers)]
+            if stream is not None:  # the memory is the current stream's, whose work may still use what lay there before
+                stream.wait_stream(torch.cuda.current_stream(self.buf.device))
         if self.seq_lens_host[seq]:
             B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds], n, stream)
         self.indexed[seq] = True
