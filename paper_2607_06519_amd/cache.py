@@ -5,6 +5,7 @@ runs in the library's kernels.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 from typing import Optional, Sequence
 
@@ -35,6 +36,13 @@ def to_device(x: np.ndarray, dtype: str, device="cuda"):
     torch = _torch()
     t = torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32))
     return t.to(device=device).to(torch_dtype(dtype))
+
+
+def _memory_of(stream):
+    """Within it, tensors are allocated from the memory of ``stream`` (None: the current one), for what it writes: a block
+    of the current stream's may still be in use by what is queued there.  A reader on another stream waits for ``stream``
+    as for any tensor of it."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
 
 
 class CompressedCache:
@@ -85,7 +93,8 @@ class CompressedCache:
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         """One decode step of ``layer`` for queries ``q [batch][Hq][d]``; returns ``out``."""
         if out is None:
-            out = _torch().empty_like(q)
+            with _memory_of(stream):
+                out = _torch().empty_like(q)
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
         B.decode_attn(self.dims, self.batch, self.seq_lens, self.max_seq_len, self.modes, self.offsets,
                       self.buf, layer, q, out, scale, self.ws, stream)
@@ -205,20 +214,23 @@ class Generation:
                  stream)
 
     def append_rotated(self, layer: int, rope: B.Rope, q, k_new, v_new, q_norm=None, k_norm=None, eps: float = 1e-6,
-                       stream=None):
+                       stream=None, out=None):
         """``append`` of rows as the projections leave them: queries ``q [batch][Hq][d]`` and keys are
         normed per head (where weights are given) and turned by ``rope``, keys and values go into the
-        tail.  Heads may lie in one fused projection's rows.  Returns the queries for ``decode``."""
+        tail.  Heads may lie in one fused projection's rows.  Returns the queries for ``decode`` (``out``)."""
         if self.full:
             raise RuntimeError("the tail is full: refresh before appending")
-        out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+        if out is None:
+            with _memory_of(stream):
+                out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
         B.rope_append(self.dims, rope, q, k_new, v_new, out, None, self.pos, self.tail_k[layer], self.tail_v[layer],
                       q_norm, k_norm, eps, stream)
         return out
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         if out is None:
-            out = _torch().empty_like(q)
+            with _memory_of(stream):
+                out = _torch().empty_like(q)
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
         tail = B.Tail(int(self.lens.data_ptr()), self.cap, int(self.tail_k[layer].data_ptr()),
                       int(self.tail_v[layer].data_ptr()))
