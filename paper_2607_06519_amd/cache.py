@@ -66,11 +66,16 @@ class CompressedCache:
                               dtype=torch.float32, device=device)
         self.bounds = None                                  # the index of a sparse decode (``index``)
         self.indexed = [t == 0 for t in self.seq_lens_host]
+        self.compressed = [False] * self.batch
 
     def compress(self, seq: int, k_layers, v_layers, stream=None, token_scores=None, k_select=None):
         """Write sequence ``seq`` from per-layer device tensors ``[Hkv][T][d]`` (``token_scores``
         from the probe when residual heads hold a token-level set; ``k_select`` the probe's K
-        selections of the same keys, reused instead of selecting again)."""
+        selections of the same keys, reused instead of selecting again).  A sequence that is written
+        again has to be indexed again, after it, before a sparse decode reads it."""
+        if self.compressed[seq]:
+            self.indexed[seq] = self.seq_lens_host[seq] == 0
+        self.compressed[seq] = True
         B.compress(self.dims, self.seq_lens_host[seq], k_layers, v_layers, self.modes[seq],
                    self.offsets[seq], self.buf, stream, token_scores, k_select)
 
@@ -241,6 +246,8 @@ class Generation:
             if scale < 0:
                 raise ValueError("a sparse decode selects the largest q . k, which a negative scale turns into the least")
             s = self.spans[0]
+            if False in s.indexed:
+                raise RuntimeError("a sequence of the prefix was compressed again: index it before a sparse decode")
             B.block_select(self.dims, self.batch, s.seq_lens, s.max_seq_len, s.bounds[layer], q, *self.select,
                            self.blocks, self.counts, self._select_ws, stream)
         B.decode_parts(self.dims, self.batch, self._parts, tail, layer, q, out, scale, self._ws, stream)

@@ -1,0 +1,64 @@
+"""CompressedCache and Generation around the serving step, on the host: which calls they refuse.  The
+library's device calls are replaced by stubs; everything else is their own code on CPU tensors."""
+import os
+
+import numpy as np
+import pytest
+
+from paper_2607_06519_amd import binding as B
+from paper_2607_06519_amd import cache as C
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    import torch
+    if not os.path.exists(B._LIB_PATH):
+        pytest.skip("libfdkv.so not built")
+    seen = []
+    monkeypatch.setattr(C, "_torch", lambda: torch)
+    for name in ("compress", "key_bounds", "block_select", "decode_parts"):
+        monkeypatch.setattr(C.B, name, lambda *a, _name=name, **k: seen.append(_name))
+    return seen
+
+
+DIMS = B.dims(2, 2, 8, 128, 16, "bf16")
+
+
+def _cache(lens):
+    return C.CompressedCache(DIMS, lens, np.zeros((len(lens), 1, 2), np.uint8), device="cpu")
+
+
+def _sparse(prefix, select=(1, 1, 4)):
+    return C.Generation(DIMS, prefix, 4, device="cpu", select=select)
+
+
+def test_a_sequence_compressed_again_is_indexed_again(calls):
+    import torch
+    q = torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+    c = _cache([200, 100])
+    for s in range(2):
+        c.compress(s, [], [])
+        c.index(s, [])
+    gen = _sparse(c)
+    gen.decode(0, q)
+    c.compress(1, [], [])                                    # other keys
+    calls.clear()
+    with pytest.raises(RuntimeError):
+        gen.decode(0, q)
+    assert not calls
+    with pytest.raises(ValueError):
+        _sparse(c)
+    c.index(1, [])
+    gen.decode(0, q)
+    _sparse(c)
+
+
+def test_indexed_before_or_after_the_first_compression(calls):
+    c = _cache([200, 0, 100])
+    c.index(0, [])
+    c.compress(0, [], [])
+    c.compress(2, [], [])
+    c.index(2, [])
+    c.compress(1, [], [])
+    c.compress(1, [], [])                                    # an empty sequence has no bounds
+    _sparse(c)
