@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void parts_merge_kernel(PartsMergeParams P) {
       lt = fmaf(w, l_lds[i], lt);
       ot = fmaf(w, o_lds[i][threadIdx.x], ot);
     }
-    const float res = lt > 0.f ? ot / lt : 0.f;
+    const float res = lt == 0.f ? 0.f : ot / lt;  // 0: no token at all (a logit that is not a number makes lt NaN)
     const uint64_t at = ((uint64_t)unit * P.G + g) * D + threadIdx.x;
     if constexpr (BF16)
       static_cast<uint16_t*>(P.out)[at] = (uint16_t)f32_to_bf16_bits(res);
