@@ -95,6 +95,9 @@ __device__ __forceinline__ float col_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// What a rounding to `hi` leaves of x; nothing of an infinite one (inf - inf is no number).
+__device__ __forceinline__ float rest_of(float x, float hi) { return fabsf(hi) == INFINITY ? 0.f : x - hi; }
+
 // Orders the compiler's LDS accesses; the hardware runs a wave's in order.
 __device__ __forceinline__ void lds_fence() { asm volatile("" ::: "memory"); }
 
@@ -600,7 +603,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
           *reinterpret_cast<uint16_t*>(rt + p.at[i]) = (uint16_t)((i & 1) ? p.w[i / 2] >> 16 : p.w[i / 2]);
         } else {
           const uint32_t hi = f32_to_bf16_bits(p.x[i]);
-          *reinterpret_cast<uint16_t*>(rt + p.at[i]) = (uint16_t)(rest ? f32_to_bf16_bits(p.x[i] - bf16_to_f32((uint16_t)hi)) : hi);
+          *reinterpret_cast<uint16_t*>(rt + p.at[i]) = (uint16_t)(rest ? f32_to_bf16_bits(rest_of(p.x[i], bf16_to_f32((uint16_t)hi))) : hi);
         }
       }
     };
@@ -685,7 +688,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
             const float y0 = fmaf(w3, bf16_lo(cc), fmaf(w2, bf16_lo(bb), w1 * bf16_lo(a)));
             const float y1 = fmaf(w3, bf16_hi(cc), fmaf(w2, bf16_hi(bb), w1 * bf16_hi(a)));
             const uint32_t hi = cvt_bf16x2(y0, y1);
-            ow[i] = rest ? cvt_bf16x2(y0 - bf16_lo(hi), y1 - bf16_hi(hi)) : hi;
+            ow[i] = rest ? cvt_bf16x2(rest_of(y0, bf16_lo(hi)), rest_of(y1, bf16_hi(hi))) : hi;
           } else {
             ow[i] = a ^ (w1 < 0.f ? 0x80008000u : 0u);
           }
