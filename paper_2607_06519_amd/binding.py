@@ -361,6 +361,20 @@ def _operands(what: str, element, tensors, numbers=()):
         _operands(what, torch.int32, numbers)
 
 
+def _workspace(what: str, ws):
+    """Refuses a workspace that the current device's kernels cannot write (its size is the library's to check)."""
+    import torch
+    here = torch.cuda.current_device()
+    if ws.get_device() != here or not ws.is_contiguous():
+        raise ValueError(f"{what}: a workspace on {ws.device}, strides {ws.stride()}, not contiguous on cuda:{here}")
+
+
+@functools.lru_cache(maxsize=256)
+def _n_blocks(n_layers: int, schedule: int) -> int:
+    """Blocks of layers of a schedule."""
+    return len(blocks(dims(n_layers, 1, 1, 64, 0, "f32", schedule))[0])
+
+
 def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: bool = False) -> Rope:
     """Rotary positions: ``inv_freq`` device float64 ``[rot_dim / 2]``, ``pos`` device int32 ``[n_tokens]``
     or ``[n_axes][n_tokens]``, ``axis`` the axis that each pair follows (default: axis 0).  The descriptor
@@ -456,6 +470,7 @@ def block_select(d: Dims, batch: int, seq_lens, max_seq_len: int, bounds, q, n_f
     _operands("block_select", _element(d.dtype),
               ((bounds, units * -(-int(max_seq_len) // BLOCK_TOKENS) * 2 * d.head_dim), (q, int(batch) * d.n_q_heads * d.head_dim)),
               ((seq_lens, int(batch)), (blocks_out, units * int(n_sel)), (counts_out, units)))
+    _workspace("block_select", ws)
     _check(load().fdkv_block_select(ctypes.byref(d), int(batch), _dev(seq_lens), int(max_seq_len), _dev(bounds),
                                     _dev(q), int(n_first), int(n_last), int(n_sel), _dev(blocks_out),
                                     _dev(counts_out), _dev(ws), int(ws.numel() * ws.element_size()),
@@ -474,6 +489,7 @@ def part(kind: int, seq_lens, max_seq_len: int, modes, seg_offsets, cache, block
     p = Part(int(kind), int(max_seq_len), int(n_sel), _dev(seq_lens), _dev(modes), _dev(seg_offsets), _dev(cache),
              _dev(blocks), _dev(counts))
     p.tensors = (seq_lens, modes, seg_offsets, cache, blocks, counts)
+    p.held = tuple(0 if t is None else t.numel() for t in (seq_lens, modes, seg_offsets, blocks, counts))
     p.device = cache.get_device()
     return p
 
@@ -489,11 +505,22 @@ def decode_parts_workspace(d: Dims, batch: int, parts: Sequence[Part], tail_cap:
 def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q, out, sm_scale: float, ws,
                  stream=None):
     """Queue fdkv_decode_parts for one layer; ``parts`` are ``Part`` descriptors, ``tail`` a ``Tail`` or None."""
-    n = int(batch) * d.n_q_heads * d.head_dim
-    _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
+    n, hkv = int(batch) * d.n_q_heads * d.head_dim, d.n_kv_heads
+    units = hkv * _n_blocks(d.n_layers, d.schedule)
     for p in parts:
-        if getattr(p, "device", q.get_device()) != q.get_device():
+        held = getattr(p, "held", None)    # (a descriptor of plain addresses says nothing of what lies there)
+        if held is None:
+            continue
+        seqs = 1 if p.kind == PART_SHARED else int(batch)
+        chosen = seqs * hkv if p.kind == PART_BLOCKS else 0
+        need = (seqs, seqs * units, seqs * units, chosen * p.n_sel, chosen)
+        if any(h < m for h, m in zip(held, need)):
+            raise ValueError(f"decode_parts: a part of {seqs} sequences takes {need} lengths, modes, offsets, blocks and "
+                             f"counts; it has {held}")
+        if p.device != q.get_device():
             raise ValueError("decode_parts: a part lies on another device than the queries")
+    _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
+    _workspace("decode_parts", ws)
     arr = _array_type(Part, max(len(parts), 1))(*parts)
     _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),
