@@ -389,6 +389,8 @@ def rope(rot_dim: int, inv_freq, pos, axis: Sequence[int] = (), interleaved: boo
         raise ValueError("rope: inv_freq holds rot_dim / 2 values; both tensors are contiguous")
     if len(axis) not in (0, rot_dim // 2) or rot_dim > 128:
         raise ValueError("rope: one axis for each of the rot_dim / 2 pairs")
+    if len(axis) and not (min(axis) >= 0 and max(axis) < n_axes):
+        raise ValueError(f"rope: an axis of a pair is 0 .. {n_axes - 1}, a row of pos")
     r = Rope(int(rot_dim), int(interleaved), n_axes, _dev(inv_freq), _dev(pos), (ctypes.c_uint8 * 64)(*axis))
     r.tensors = (inv_freq, pos)
     r.n_tokens, r.device = int(pos.shape[-1]), pos.get_device()

@@ -81,3 +81,13 @@ def test_workspaces_on_another_device(cpu):
             B.block_select(dims, BATCH, i32(BATCH), 1000, bounds, q, 0, 1, 4, i32(BATCH, 2, 4), i32(BATCH, 2), ws)
     with pytest.raises(torch.Queued):
         B.block_select(dims, BATCH, i32(BATCH), 1000, bounds, q, 0, 1, 4, i32(BATCH, 2, 4), i32(BATCH, 2), torch.zeros(1 << 20))
+
+
+def test_axes_of_pairs():
+    import torch
+    freq = torch.zeros(8, dtype=torch.float64)
+    pos = torch.zeros(2, 3, dtype=torch.int32)
+    assert B.rope(16, freq, pos, [0, 1] * 4).axis[1] == 1
+    for axis in ([0, 2] * 4, [0, 256] * 4, [-1, 0] * 4, [0, 1] * 3):   # (256 is 0 in eight bits)
+        with pytest.raises(ValueError):
+            B.rope(16, freq, pos, axis)
