@@ -161,11 +161,17 @@ class Generation:
             raise ValueError("a shared prefix is a cache of one sequence")
         if select is not None and (prefix.bounds is None or not all(prefix.indexed)):
             raise ValueError("a sparse decode selects by the prefix's key bounds: index its sequences first")
+        if select is not None:
+            n_first, n_last, n_sel = select = tuple(int(n) for n in select)
+            if n_first < 0 or n_last < 0 or n_sel < max(1, n_first + n_last):
+                raise B.FdkvError(-1, f"Generation, select = {select}")
+            if n_sel > B.MAX_SELECTED or prefix.batch * dims.n_kv_heads > B.MAX_SELECT_UNITS:
+                raise B.FdkvError(-2, f"Generation, select = {select}, batch {prefix.batch}")
         self.dims = dims
         self.batch = prefix.batch if prefix is not None else int(batch)
         self.spans = [prefix] if prefix is not None else []
         self.shared = shared
-        self.select = None if select is None else tuple(int(n) for n in select)
+        self.select = select
         self.cap = int(tail_cap)
         tdt = _input_dtype(dims)
         shape = (self.batch, dims.n_kv_heads, self.cap, dims.head_dim)

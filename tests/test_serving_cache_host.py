@@ -62,3 +62,17 @@ def test_indexed_before_or_after_the_first_compression(calls):
     c.compress(1, [], [])
     c.compress(1, [], [])                                    # an empty sequence has no bounds
     _sparse(c)
+
+
+def test_a_selection_that_the_library_refuses_is_refused_at_once(calls):
+    c = _cache([200, 100])
+    for s in range(2):
+        c.index(s, [])
+    for select in ((0, 0, 1), (2, 2, 4), (0, 0, 1 << 12)):
+        assert _sparse(c, select).select == select
+    for select in ((3, 3, 4), (0, 0, 0), (-1, 0, 4), (0, -1, 4), (0, 0, -4), (0, 0, (1 << 24) + 1)):
+        with pytest.raises(B.FdkvError):
+            _sparse(c, select)
+    for select in ((1, 4), (1, 1, 4, 4)):
+        with pytest.raises(ValueError):
+            _sparse(c, select)
