@@ -79,20 +79,26 @@ class CompressedCache:
         B.compress(self.dims, self.seq_lens_host[seq], k_layers, v_layers, self.modes[seq],
                    self.offsets[seq], self.buf, stream, token_scores, k_select)
 
+    def allocate_bounds(self, stream=None):
+        """The memory of ``index`` (its first call asks for it; a cache of empty sequences only needs no call)."""
+        if self.bounds is not None:
+            return
+        torch = _torch()
+        blocks = max(1, -(-self.max_seq_len // B.BLOCK_TOKENS))
+        shape = (self.batch, self.dims.n_kv_heads, blocks, 2, self.dims.head_dim)
+        self.bounds = [torch.empty(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
+                       for _ in range(self.dims.n_layers)]
+        if stream is not None:  # the memory is the current stream's, whose work may still use what lay there before
+            stream.wait_stream(torch.cuda.current_stream(self.buf.device))
+
     def index(self, seq: int, k_layers, stream=None):
         """Key bounds of sequence ``seq``, from the keys that ``compress`` takes: what a sparse decode
         (``Generation`` with ``select``) chooses its blocks by.  ``bounds[l] [batch][Hkv][blocks][2][d]``;
         blocks behind a sequence are left unwritten, as nothing reads them."""
-        torch = _torch()
-        n = -(-self.max_seq_len // B.BLOCK_TOKENS)
-        if self.bounds is None:
-            shape = (self.batch, self.dims.n_kv_heads, n, 2, self.dims.head_dim)
-            self.bounds = [torch.empty(shape, dtype=_input_dtype(self.dims), device=self.buf.device)
-                           for _ in range(self.dims.n_layers)]
-            if stream is not None:  # the memory is the current stream's, whose work may still use what lay there before
-                stream.wait_stream(torch.cuda.current_stream(self.buf.device))
+        self.allocate_bounds(stream)
         if self.seq_lens_host[seq]:
-            B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds], n, stream)
+            B.key_bounds(self.dims, self.seq_lens_host[seq], k_layers, [b[seq] for b in self.bounds],
+                         self.bounds[0].shape[2], stream)
         self.indexed[seq] = True
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
@@ -159,7 +165,7 @@ class Generation:
             raise ValueError("the batch is the prefix's")
         if shared is not None and shared.batch != 1:
             raise ValueError("a shared prefix is a cache of one sequence")
-        if select is not None and (prefix.bounds is None or not all(prefix.indexed)):
+        if select is not None and not all(prefix.indexed):
             raise ValueError("a sparse decode selects by the prefix's key bounds: index its sequences first")
         if select is not None:
             n_first, n_last, n_sel = select = tuple(int(n) for n in select)
@@ -172,6 +178,8 @@ class Generation:
         self.spans = [prefix] if prefix is not None else []
         self.shared = shared
         self.select = select
+        if select is not None:
+            prefix.allocate_bounds()
         self.cap = int(tail_cap)
         tdt = _input_dtype(dims)
         shape = (self.batch, dims.n_kv_heads, self.cap, dims.head_dim)

@@ -76,3 +76,11 @@ def test_a_selection_that_the_library_refuses_is_refused_at_once(calls):
     for select in ((1, 4), (1, 1, 4, 4)):
         with pytest.raises(ValueError):
             _sparse(c, select)
+
+
+def test_a_prefix_of_empty_sequences(calls):
+    """Nothing to index, and nothing to select from: the bounds are there all the same, for their address."""
+    import torch
+    gen = _sparse(_cache([0, 0]))
+    gen.decode(0, torch.zeros(2, 8, 128, dtype=torch.bfloat16))
+    assert calls == ["block_select", "decode_parts"] and all(b.data_ptr() for b in gen.spans[0].bounds)
