@@ -133,6 +133,13 @@ def probe(dims: B.Dims, seq_len: int, k_layers, qp_layers, n_probe: int, stream=
     return err, (scores if scores is not None else ksel)
 
 
+def _same_cache(a: B.Dims, b: B.Dims) -> bool:
+    """Dims of one cache layout (all of it but the query heads)."""
+    here = B.Dims.from_buffer_copy(b)
+    here.n_q_heads = a.n_q_heads
+    return bytes(a) == bytes(here)
+
+
 class Generation:
     """A compressed cache being extended by decoding (the end of Section 3's
     method): compressed spans (prefill first) followed by an exact tail of
@@ -165,6 +172,9 @@ class Generation:
             raise ValueError("the batch is the prefix's")
         if shared is not None and shared.batch != 1:
             raise ValueError("a shared prefix is a cache of one sequence")
+        if shared is not None or select is not None:
+            if not all(_same_cache(c.dims, dims) for c in (shared, prefix) if c is not None):
+                raise ValueError("a prefix of other dimensions, or compressed another way, than the generation")
         if select is not None and not all(prefix.indexed):
             raise ValueError("a sparse decode selects by the prefix's key bounds: index its sequences first")
         if select is not None:

@@ -24,8 +24,8 @@ def calls(monkeypatch):
 DIMS = B.dims(2, 2, 8, 128, 16, "bf16")
 
 
-def _cache(lens):
-    return C.CompressedCache(DIMS, lens, np.zeros((len(lens), 1, 2), np.uint8), device="cpu")
+def _cache(lens, dims=DIMS):
+    return C.CompressedCache(dims, lens, np.zeros((len(lens), len(B.blocks(dims)[0]), dims.n_kv_heads), np.uint8), device="cpu")
 
 
 def _sparse(prefix, select=(1, 1, 4)):
@@ -84,3 +84,20 @@ def test_a_prefix_of_empty_sequences(calls):
     gen = _sparse(_cache([0, 0]))
     gen.decode(0, torch.zeros(2, 8, 128, dtype=torch.bfloat16))
     assert calls == ["block_select", "decode_parts"] and all(b.data_ptr() for b in gen.spans[0].bounds)
+
+
+@pytest.mark.parametrize("which", ["shared", "beside", "sparse"])
+def test_a_prefix_of_another_cache(calls, which):
+    def make(dims):
+        if which == "shared":
+            return C.Generation(DIMS, None, 4, device="cpu", shared=_cache([200], dims), batch=2)
+        if which == "beside":
+            return C.Generation(DIMS, _cache([200, 0], dims), 4, device="cpu", shared=_cache([100]))
+        return C.Generation(DIMS, _cache([0, 0], dims), 4, device="cpu", select=(0, 0, 1))
+    make(DIMS)
+    make(B.dims(2, 2, 4, 128, 16, "bf16"))                   # (the query heads are not the cache's)
+    for dims in (B.dims(4, 2, 8, 128, 16, "bf16"), B.dims(2, 4, 8, 128, 16, "bf16"), B.dims(2, 2, 8, 64, 16, "bf16"),
+                 B.dims(2, 2, 8, 128, 8, "bf16"), B.dims(2, 2, 8, 128, 16, "bf16_e4m3"), B.dims(2, 2, 8, 128, 16, "f32"),
+                 B.dims(2, 2, 8, 128, 16, "bf16", residual=B.RES_TOKENS, res_ppm=10000)):
+        with pytest.raises(ValueError):
+            make(dims)
