@@ -26,9 +26,11 @@
 // R a tile of LDS that is zero but for the residual entries (or the rows of a
 // token-level set) of the tile, each in its place: +-D of a pair is a bf16 value;
 // the sum of a block of four's weighted coefficients goes in as its bf16 rounding
-// and, for K (whose error an exponential would amplify), once more as the rest,
-// so a rebuilt key carries 2^-16 of its residual.  R multiplies the same operands
-// as M; no rebuilt value is rounded and no entry is gathered per query row.
+// and once more as the rest, so a rebuilt row carries 2^-16 of its residual.  (V's
+// rest costs a layer of a shared span of 12345 tokens up to 5% (64 rows: bf16 31.1 and
+// 32.6 us, E4M3 29.4 and 29.5; 256 rows of E4M3 54.0 and 54.8), 8% in bf16 at 32 rows
+// (23.3 and 25.2), and of selected blocks 2 to 4%.)  R multiplies the same operands as
+// M; no rebuilt value is rounded and no entry is gathered per query row.
 // Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
 //
 // What bounds it.  Parts of single sequences: HBM where a wave has several tiles (selected blocks of 16 sequences' fp8
@@ -162,13 +164,13 @@ enum : int { kFewEntries = 1, kManyEntries = 2, kTokenSet = 3 };
 constexpr int parts_per_cu(int KIND, bool q4) { return KIND == kManyEntries && q4 ? 1 : 2; }
 
 // LDS of a workgroup.  A token group's: the V tile, then R with a row behind it that takes what has no place (CG = 4:
-// the K tile, and R of K, of V and, where K's has one, of K's rest).
+// the K tile, and R of K, of V and, of a block of four, of K's and V's rests).
 template <int D, int CG, int TY, bool q4>
 struct PartsLds {
   using S = parts::TileOf<D, TY>;
-  static constexpr bool REST = q4 && !S::F32;  // K's residual has a bf16 rest
+  static constexpr bool REST = q4 && !S::F32;  // a residual has a bf16 rest
   static constexpr int RT = S::TILE_BYTES + S::RB;
-  static constexpr int GROUP = CG == 1 ? S::TILE_BYTES + RT : 2 * S::TILE_BYTES + (REST ? 3 : 2) * RT;
+  static constexpr int GROUP = CG == 1 ? S::TILE_BYTES + RT : 2 * S::TILE_BYTES + (REST ? 4 : 2) * RT;
   static_assert(GROUP % S::RB == 0 && S::TILE_BYTES % S::RB == 0, "tiles start at a multiple of a row");
   static constexpr int MP = D + 4;             // floats of a row of the merge (padded against bank conflicts)
   static constexpr int TILES = 4 / CG * GROUP, MERGE = 4 * 16 * MP * 4;
@@ -178,7 +180,7 @@ struct PartsLds {
 // CG column groups of 16 NQ columns each, a wave apiece, by TG = 4 / CG token
 // groups: CG = 1, four waves with tiles of their own, or CG = 4, four that walk the
 // same tiles.  There each wave stages its share of K and V, one places the residual
-// entries of K, one those of V (one the rest of K's), and two barriers a tile hand
+// entries of K, one those of V (two more the rests), and two barriers a tile hand
 // the tiles over.
 template <int D, int NQ, int CG, int TY, int KIND, bool q4>
 __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide& L, uint32_t w, uint8_t* lds, float (*ml_lds)[16][2]) {
@@ -346,11 +348,12 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
 
   uint8_t* vt = lds + tg * kGroupLds;                  // the V tile
   uint8_t* kt = vt + S::TILE_BYTES;                    // CG = 4: the K tile
-  uint8_t* r_k = kt + (CG == 1 ? 0 : S::TILE_BYTES);   // R of K, of V, of K's rest (CG == 1: one after the other)
+  uint8_t* r_k = kt + (CG == 1 ? 0 : S::TILE_BYTES);   // R of K, of V, of their rests (CG == 1: one after the other)
   uint8_t* r_v = CG == 1 ? r_k : r_k + kRt;
   uint8_t* r_rest = CG == 1 ? r_k : r_k + 2 * kRt;
-  // CG = 4: the wave's tile of R (0: K, 1: V, 2: K's rest)
-  const int role = CG == 1 ? 0 : cg, roles = REST ? 3 : 2;
+  uint8_t* r_vrest = CG == 1 ? r_k : r_k + 3 * kRt;
+  // CG = 4: the wave's tile of R (0: K, 1: V, 2: K's rest, 3: V's)
+  const int role = CG == 1 ? 0 : cg, roles = REST ? 4 : 2;
   uint8_t* rt = r_k + (CG == 1 ? 0 : role < roles ? role : 0) * kRt;
   // Hands LDS tiles from the waves that wrote them to those that read them.
   auto hand_over = [&]() __attribute__((always_inline)) {
@@ -395,7 +398,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
     // plane's padding may hold anything; entries of tokens behind the last are not used.)
     const uint32_t ibr = (ib + 15) & ~15u, xbr = (xb + 15) & ~15u;
     // (CG = 4: the wave reads the entries of its role, K's or V's, into what is K's buffer here)
-    const uint64_t k_at = CG > 1 && role == 1 ? (uint64_t)ip + xp : 0;
+    const uint64_t k_at = CG > 1 && (role & 1) ? (uint64_t)ip + xp : 0;
     const uint32_t live = CG > 1 && role >= roles ? 0u : ~0u;
     const auto ikr = rsrc(ent + k_at, ibr & live), xkr = rsrc(ent + k_at + ip, xbr & live);
     const auto ivr = rsrc(ent + ip + xp, ibr), xvr = rsrc(ent + 2 * (uint64_t)ip + xp, xbr);
@@ -407,7 +410,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
       L = tok_layout(mode, (uint64_t)T, D, ppm, S::E, C, nb);
       set_bytes = residual_token_count((uint64_t)T, ppm) * (uint64_t)(nb - 1) * D * C;
     }
-    const auto hkr = rsrc(seg + (CG > 1 && role == 1 ? L.hv : L.hk), CG > 1 && role >= roles ? 0 : set_bytes);
+    const auto hkr = rsrc(seg + (CG > 1 && (role & 1) ? L.hv : L.hk), CG > 1 && role >= roles ? 0 : set_bytes);
     const auto hvr = rsrc(seg + L.hv, set_bytes);
     const auto* mask_words = as_const(reinterpret_cast<const uint32_t*>(seg + L.mask));
     const auto* counts = as_const(reinterpret_cast<const uint32_t*>(seg + L.count));
@@ -830,7 +833,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
       }
       if constexpr (CG > 1 && RES != 0) {
         if (has && role < roles) {
-          const bool rest = REST && role == 2;
+          const bool rest = REST && role >= 2;
           if constexpr (ENT) {
             place_all(b.ek, t0);
             scatter(rt, ikr, xkr, t0, rest);
@@ -839,6 +842,8 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
         }
         load_res(b);
       }
+
+      SetRows sv;  // V's rows, for their rest
 
       // K
 #pragma unroll
@@ -880,6 +885,7 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
           }
           if constexpr (SET) set_rows(rt, hvr, b.sv, mask, rank, false);
         }
+        if constexpr (SET && REST) sv = b.sv;
         load_res(b);
       }
 
@@ -943,7 +949,16 @@ __device__ __forceinline__ void parts_body(const PartsParams& P, const PartsSide
 
       // V
       pv(vt);
-      if (has) pv(r_v);
+      if (has) {
+        pv(r_v);
+        if constexpr (REST) {
+          if constexpr (CG == 1) {
+            if constexpr (ENT) scatter(rt, ivr, xvr, t0, true);
+            if constexpr (SET) set_rows(rt, hvr, sv, mask, rank, true);
+          }
+          pv(r_vrest);
+        }
+      }
       if constexpr (CG > 1) hand_over();
       if (has && role < roles) {
         clear_r(rt);
