@@ -955,35 +955,55 @@ bool parts_many(const fdkv_dims* dims) {
   return !tokens_mode(dims) && (dims->topk % 8 || dims->topk > (dims->dtype == FDKV_F32 ? 32 : 16));
 }
 
-// A residual head's time per token of a shared span, a plain head's being 16 (measured at 64 query rows, head
-// dimension 128): one head's share of the workgroups.  0: every head takes as many.  A layer of 32768 tokens, four plain
-// heads, three residual and an exact one, by cost and all alike (us): 64 rows of bf16 pairs 41 and 48, 28 of bf16 with
-// k = 24 45 and 58, 64 of fp32 133 and 143; up to 16 rows, where memory bounds a residual head too, 40 and 37.
+// A residual head's time per token of a shared span, a plain head's being 16: one head's share of the workgroups.  0: every
+// head takes as many.  A step's layer of 32768 shared tokens, four plain heads, three residual and an exact one, by a
+// cost of 0, 24 and 28 (us; the workgroups' widths are parts_cols'):
+//   d = 128             16 rows             32 rows             64 rows             128 rows
+//   bf16, pairs         40.0  38.6  39.1    40.8  40.4  41.3    52.8  47.2  47.6    64.5  60.5  59.6
+//   E4M3, pairs         28.7  30.3  31.5    31.7  33.1  34.6    43.9  40.6  40.4    62.1  56.2  56.7
+//   bf16, pairs, k = 24 40.9  39.8  39.8    59.7  47.6  45.6    61.9  50.2  49.4    67.9  59.4  61.3
+//   fp32, pairs         76.4  67.3  67.3    105   85.6  84.9    180   139   138     295   230   232
+//   bf16, fours         37.8  36.5  34.4    43.9  39.6  37.1    58.5  52.9  51.1    77.8  62.6  62.5
+//   E4M3, fours         34.4  31.1  29.2    41.6  37.5  34.1    55.9  45.0  43.9    75.8  62.7  61.4
+// (d = 64 and token sets alike.)  Up to 16 rows memory bounds a residual head of pairs too; blocks of four and fp32 would
+// gain there.  A schedule with blocks of four takes their cost for its pairs.
 int parts_res_cost(const fdkv_dims* dims, const PartsPlan& p) {
   if (p.rows <= 16 || (!tokens_mode(dims) && dims->topk == 0)) return 0;
   return dims->schedule != FDKV_SCHED_PAIRS || parts_many(dims) ? 28 : 24;
 }
 
 // Query rows of a workgroup of the shared parts: 16 or 32 by waves with tiles of their own, 64 or 128 by four waves of one
-// tile.  A layer of 8 KV heads and 32768 tokens, times by width (us):
-//                                   32 rows                        64 rows                          128 rows
-//   bf16, pairs of k = 16           16: 45.4  32: 43.0  64: 42.0   16: 62.4  32: 48.2  64: 44.3     32: 65.4  128: 53.0
-//   bf16, blocks of four            16: 41.6  32: 40.1  64: 46.1   16: 61.2  32: 44.3  64: 47.6     32: 65.5  128: 54.0
-//   E4M3, pairs                     16: 35.1  32: 33.5  64: 40.0   16: 48.8  32: 38.3  64: 41.6     32: 53.1  128: 49.1
-//   E4M3, blocks of four            16: 35.1  32: 33.9  64: 44.7   16: 53.2  32: 41.2  64: 46.5     32: 61.1  128: 53.7
-//   bf16, pairs of k = 24           16: 48.7  32: 65.9  64: 44.7   16: 64.9  32: 86.4  64: 46.7     32: 136   128: 55
-//   bf16, blocks of four of k = 24  16: 65.7                       64: 74.3
-//   fp32, pairs of k = 16           16: 83    32: 106   64: 161    16: 134   32: 151   64: 163      16: 248   128: 222
-// (At 16 rows, by 16 and by 64: 37.4 and 41.1, 36.6 and 45.3, 28.4 and 39.2, 28.0 and 44.0; at 160, by 64 and by 128: 85 and
-// 73 bf16 pairs, 106 and 86 E4M3 blocks of four.  32 columns a wave spill with many entries and in fp32, whose products
-// bound it besides: 80 rows by 16 take 170, by 128 218.)
-int parts_cols(const fdkv_dims* dims, int64_t rows) {
+// tile.  A step's layer of 8 KV heads and 32768 shared tokens, tails of up to 512 and the merge included, by width (us; d = 64:
+// k = 8 and 24):
+//   d = 128                        16 rows           32 rows                    64 rows                             128 rows
+//   bf16, pairs of k = 16          16: 40  32: 39    16: 47  32: 41  64: 44     16: 65  32: 53  64: 48  128: 51     32: 71  64: 66  128: 60
+//   bf16, pairs of token sets      16: 38  32: 38    16: 48  32: 39  64: 43     16: 66  32: 52  64: 46  128: 50     32: 70  64: 63  128: 58
+//   bf16, blocks of four           16: 38  32: 41    16: 46  32: 37  64: 49     16: 68  32: 51  64: 51  128: 57     32: 75  64: 82  128: 65
+//   E4M3, pairs                    16: 29  32: 29    16: 38  32: 33  64: 40     16: 51  32: 41  64: 42  128: 49     32: 55  64: 65  128: 57
+//   E4M3, blocks of four           16: 35  32: 39    16: 39  32: 34  64: 48     16: 58  32: 45  64: 49  128: 56     32: 66  64: 82  128: 62
+//   bf16, pairs of k = 24          16: 41  64: 59    16: 48  32: 77  64: 46     16: 68  32: 89  64: 49  128: 53     64: 74  128: 61
+//   bf16, blocks of four of k = 24 16: 55  64: 161   16: 74  32: 47  64: 74     16: 117 32: 80  64: 80  128: 101    64: 134 128: 104
+//   fp32, pairs of k = 16          16: 76  32: 149   16: 92  32: 130 64: 162    16: 146 32: 152 64: 163 128: 221    16: 252 128: 230
+//   d = 64
+//   bf16, pairs                    16: 23  32: 22    16: 27  32: 23  64: 28     16: 37  32: 30  64: 30  128: 32     32: 39  64: 44  128: 36
+//   bf16, blocks of four           16: 25  32: 26    16: 28  32: 24  64: 33     16: 41  32: 30  64: 34  128: 39     32: 45  64: 56  128: 42
+//   E4M3, pairs                    16: 18  32: 19    16: 21  32: 19  64: 29     16: 29  32: 24  64: 30  128: 32     32: 34  64: 49  128: 35
+//   bf16, pairs of k = 24          16: 28  64: 45    16: 31  32: 26  64: 34     16: 42  32: 34  64: 35  128: 37     64: 54  128: 42
+//   bf16, blocks of four of k = 24 16: 42  64: 83    16: 44  32: 37  64: 53     16: 68  32: 65  64: 54  128: 56     64: 95  128: 59
+//   fp32, pairs                    16: 43  32: 55    16: 53  32: 50  64: 92     16: 83  32: 72  64: 94  128: 119    16: 144 128: 123
+// (bf16 pairs, d = 128: 20, 28 and 48 rows by 32 and by 64 39.4 and 42.5, 40.1 and 43.4, 50.8 and 46.1; 80 rows by 64 and by
+// 128 62.8 and 53.0; 32 rows of 300, 1001, 4096 and 12345 tokens by 32 and by 64 13.0 and 11.4, 14.0 and 14.0, 16.5 and 18.1,
+// 21.9 and 25.4.  fp32: 80 rows by 16 and by 128 170 and 218.  32 columns a wave spill in pairs of many entries and in
+// fp32 at d = 128; where many entries or fp32 would take them all the same there is no such kernel.)  One width serves all
+// layers of a schedule, as the workspace is sized before the layer is known: the pairs of a schedule with blocks of four
+// go by 32 at 33 to 64 rows too.
+int parts_cols(const fdkv_dims* dims, int64_t rows, int64_t tokens) {
   const bool by_four_or_e4m3 = dims->schedule != FDKV_SCHED_PAIRS || dims->dtype == FDKV_BF16_E4M3;
   if (rows <= 16) return 16;
   if (dims->dtype == FDKV_F32) return (rows + 15) / 16 > (rows + 127) / 128 * 7 ? 128 : 16;
   if (rows > 64) return 128;
-  if (by_four_or_e4m3) return !parts_many(dims) ? 32 : rows <= 32 ? 16 : 64;
-  return 64;
+  if (parts_many(dims)) return by_four_or_e4m3 && rows <= 32 ? 16 : 64;
+  return by_four_or_e4m3 || (rows <= 32 && tokens >= 1024) ? 32 : 64;
 }
 
 fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts, int32_t tail_cap,
@@ -1032,7 +1052,7 @@ fdkv_status plan_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, co
   while (p.own_tiles_per_wg < 256 && chunks(p.own_tiles_per_wg) > p.n_own && chunks(p.own_tiles_per_wg) * batch * hkv > kPartsWorkgroups)
     p.own_tiles_per_wg += 4;
   p.rows = (int)(batch * G);
-  p.cols = p.n_shared == 0 ? 16 : parts_cols(dims, p.rows);
+  p.cols = p.n_shared == 0 ? 16 : parts_cols(dims, p.rows, shared_tiles * tok);
   p.row_groups = (p.rows + p.cols - 1) / p.cols;
   // (Workgroups of 64 rows: three to two CUs, as more of them write more records and leave the own parts to the end.  Per
   // layer, 32768 tokens, 16 sequences and their tails: 384 workgroups 46.5 us, 256 48.3, 512 49.9.  Of 128 rows, two to
