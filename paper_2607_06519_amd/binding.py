@@ -349,25 +349,19 @@ def _element(dtype: int):
     return torch.float32 if dtype == F32 else torch.bfloat16
 
 
-def _operands(what: str, element, tensors, numbers=()):
+def _operands(what: str, element, tensors, numbers=(), ws=None):
     """Refuses operands that a kernel would misread: ``tensors`` (each with the values that it holds at least) of another
     element type, ``numbers`` that are not int32, any that is not contiguous, too short or on another device than the
-    current one."""
+    current one, and a workspace ``ws`` with gaps or on another device (its size is the library's to check)."""
     import torch
     here = torch.cuda.current_device()
     for t, n in tensors:
         if t.dtype is not element or t.get_device() != here or t.numel() < n or not t.is_contiguous():
             raise ValueError(f"{what}: {t.dtype} {list(t.shape)} on {t.device}, not {n} contiguous {element} on cuda:{here}")
+    if ws is not None and (ws.get_device() != here or not ws.is_contiguous()):
+        raise ValueError(f"{what}: a workspace on {ws.device}, strides {ws.stride()}, not contiguous on cuda:{here}")
     if numbers:
         _operands(what, torch.int32, numbers)
-
-
-def _workspace(what: str, ws):
-    """Refuses a workspace that the current device's kernels cannot write (its size is the library's to check)."""
-    import torch
-    here = torch.cuda.current_device()
-    if ws.get_device() != here or not ws.is_contiguous():
-        raise ValueError(f"{what}: a workspace on {ws.device}, strides {ws.stride()}, not contiguous on cuda:{here}")
 
 
 @functools.lru_cache(maxsize=256)
@@ -472,8 +466,7 @@ def block_select(d: Dims, batch: int, seq_lens, max_seq_len: int, bounds, q, n_f
     units = int(batch) * d.n_kv_heads
     _operands("block_select", _element(d.dtype),
               ((bounds, units * -(-int(max_seq_len) // BLOCK_TOKENS) * 2 * d.head_dim), (q, int(batch) * d.n_q_heads * d.head_dim)),
-              ((seq_lens, int(batch)), (blocks_out, units * int(n_sel)), (counts_out, units)))
-    _workspace("block_select", ws)
+              ((seq_lens, int(batch)), (blocks_out, units * int(n_sel)), (counts_out, units)), ws)
     _check(load().fdkv_block_select(ctypes.byref(d), int(batch), _dev(seq_lens), int(max_seq_len), _dev(bounds),
                                     _dev(q), int(n_first), int(n_last), int(n_sel), _dev(blocks_out),
                                     _dev(counts_out), _dev(ws), int(ws.numel() * ws.element_size()),
@@ -492,9 +485,22 @@ def part(kind: int, seq_lens, max_seq_len: int, modes, seg_offsets, cache, block
     p = Part(int(kind), int(max_seq_len), int(n_sel), _dev(seq_lens), _dev(modes), _dev(seg_offsets), _dev(cache),
              _dev(blocks), _dev(counts))
     p.tensors = (seq_lens, modes, seg_offsets, cache, blocks, counts)
-    p.held = tuple(0 if t is None else t.numel() for t in (seq_lens, modes, seg_offsets, blocks, counts))
-    p.device = cache.get_device()
+    p.device, p.fits = cache.get_device(), None
     return p
+
+
+def _fits(p: Part, batch: int, hkv: int, n_layers: int, schedule: int, device: int):
+    """Refuses a part whose tensors are shorter than a call would read them, or on another device.  (A descriptor of plain
+    addresses says nothing of what lies there.)"""
+    seqs = 1 if p.kind == PART_SHARED else int(batch)
+    units, chosen = seqs * hkv * _n_blocks(n_layers, schedule), seqs * hkv if p.kind == PART_BLOCKS else 0
+    held = tuple(0 if t is None else t.numel() for i, t in enumerate(p.tensors) if i != 3)
+    need = (seqs, units, units, chosen * p.n_sel, chosen)
+    if any(h < m for h, m in zip(held, need)):
+        raise ValueError(f"decode_parts: a part of {seqs} sequences takes {need} lengths, modes, offsets, blocks and counts; "
+                         f"it has {held}")
+    if p.device != device:
+        raise ValueError("decode_parts: a part lies on another device than the queries")
 
 
 def decode_parts_workspace(d: Dims, batch: int, parts: Sequence[Part], tail_cap: int) -> int:
@@ -508,22 +514,13 @@ def decode_parts_workspace(d: Dims, batch: int, parts: Sequence[Part], tail_cap:
 def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q, out, sm_scale: float, ws,
                  stream=None):
     """Queue fdkv_decode_parts for one layer; ``parts`` are ``Part`` descriptors, ``tail`` a ``Tail`` or None."""
-    n, hkv = int(batch) * d.n_q_heads * d.head_dim, d.n_kv_heads
-    units = hkv * _n_blocks(d.n_layers, d.schedule)
+    n, call = int(batch) * d.n_q_heads * d.head_dim, (batch, d.n_kv_heads, d.n_layers, d.schedule)
     for p in parts:
-        held = getattr(p, "held", None)    # (a descriptor of plain addresses says nothing of what lies there)
-        if held is None:
-            continue
-        seqs = 1 if p.kind == PART_SHARED else int(batch)
-        chosen = seqs * hkv if p.kind == PART_BLOCKS else 0
-        need = (seqs, seqs * units, seqs * units, chosen * p.n_sel, chosen)
-        if any(h < m for h, m in zip(held, need)):
-            raise ValueError(f"decode_parts: a part of {seqs} sequences takes {need} lengths, modes, offsets, blocks and "
-                             f"counts; it has {held}")
-        if p.device != q.get_device():
-            raise ValueError("decode_parts: a part lies on another device than the queries")
-    _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)))
-    _workspace("decode_parts", ws)
+        # (once for a descriptor and a kind of call, which some layers and steps repeat)
+        if getattr(p, "device", None) is not None and p.fits != (call, p.kind, p.n_sel, q.get_device()):
+            _fits(p, *call, q.get_device())
+            p.fits = (call, p.kind, p.n_sel, q.get_device())
+    _operands("decode_parts", _element(d.dtype), ((q, n), (out, n)), (), ws)
     arr = _array_type(Part, max(len(parts), 1))(*parts)
     _check(load().fdkv_decode_parts(ctypes.byref(d), int(batch), len(parts), ctypes.cast(arr, ctypes.c_void_p),
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),

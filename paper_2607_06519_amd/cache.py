@@ -5,7 +5,6 @@ runs in the library's kernels.
 """
 from __future__ import annotations
 
-import contextlib
 import math
 from typing import Optional, Sequence
 
@@ -38,11 +37,14 @@ def to_device(x: np.ndarray, dtype: str, device="cuda"):
     return t.to(device=device).to(torch_dtype(dtype))
 
 
-def _memory_of(stream):
-    """Within it, tensors are allocated from the memory of ``stream`` (None: the current one), for what it writes: a block
-    of the current stream's may still be in use by what is queued there.  A reader on another stream waits for ``stream``
-    as for any tensor of it."""
-    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+def _allocate(stream, make):
+    """``make()``, a tensor that ``stream`` (None: the current one) is to write, from that stream's memory: a block of the
+    current stream's may still be in use by what is queued there.  A reader on another stream waits for ``stream`` as for
+    any tensor of it."""
+    if stream is None:
+        return make()
+    with _torch().cuda.stream(stream):
+        return make()
 
 
 class CompressedCache:
@@ -104,8 +106,7 @@ class CompressedCache:
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         """One decode step of ``layer`` for queries ``q [batch][Hq][d]``; returns ``out``."""
         if out is None:
-            with _memory_of(stream):
-                out = _torch().empty_like(q)
+            out = _allocate(stream, lambda: _torch().empty_like(q))
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
         B.decode_attn(self.dims, self.batch, self.seq_lens, self.max_seq_len, self.modes, self.offsets,
                       self.buf, layer, q, out, scale, self.ws, stream)
@@ -159,7 +160,9 @@ class Generation:
     makes the decode sparse: of ``prefix``, whose sequences have been indexed
     (``CompressedCache.index``), a step reads per KV head the first and last
     blocks of 64 tokens and those that can hold the largest logits, ``n_sel``
-    in all; every other span and the tail are read whole.
+    in all; every other span and the tail are read whole.  With either, a
+    step's last bits depend on the batch and on the lengths that its launch is
+    sized for (fdkv_decode_parts); without, a bf16 sequence's do not.
     """
 
     def __init__(self, dims: B.Dims, prefix: Optional["CompressedCache"], tail_cap: int, device="cuda",
@@ -250,16 +253,14 @@ class Generation:
         if self.full:
             raise RuntimeError("the tail is full: refresh before appending")
         if out is None:
-            with _memory_of(stream):
-                out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+            out = _allocate(stream, lambda: _torch().empty(q.shape, dtype=q.dtype, device=q.device))
         B.rope_append(self.dims, rope, q, k_new, v_new, out, None, self.pos, self.tail_k[layer], self.tail_v[layer],
                       q_norm, k_norm, eps, stream)
         return out
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, stream=None):
         if out is None:
-            with _memory_of(stream):
-                out = _torch().empty_like(q)
+            out = _allocate(stream, lambda: _torch().empty_like(q))
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
         tail = B.Tail(int(self.lens.data_ptr()), self.cap, int(self.tail_k[layer].data_ptr()),
                       int(self.tail_v[layer].data_ptr()))

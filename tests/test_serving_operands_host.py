@@ -59,6 +59,11 @@ def test_parts_shorter_than_the_batch(cpu, schedule, layers):
             with pytest.raises(ValueError):
                 call(_part(torch, kind, dims, BATCH - 1, n_sel))
     grown = _part(torch, B.PART_BLOCKS, dims, BATCH, NSEL)
+    with pytest.raises(torch.Queued):
+        call(grown)
+    more = torch.zeros(BATCH + 1, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):                              # the same descriptor in a call for more
+        B.decode_parts(dims, BATCH + 1, [grown], None, 0, more, torch.zeros_like(more), 0.1, ws)
     grown.n_sel = NSEL + 1
     with pytest.raises(ValueError):
         call(grown)
