@@ -273,9 +273,12 @@ fdkv_status fdkv_block_select_workspace(const fdkv_dims* dims, int32_t batch, in
  * in fp64.  Selected are the n_first first and the n_last last blocks of the
  * sequence and the best others, ties to the lower block, n_sel in all; a
  * sequence of at most n_sel blocks selects them all.
- * Bounds and queries are finite numbers: a U that is NaN ranks its block last, an
- * infinite one ranks none of its head's blocks (what is written are valid block
- * numbers all the same).
+ * Blocks whose bounds agree wherever U reads them have one rank; otherwise a sum
+ * of d products in fp64 may tell apart, or tie, blocks whose U differ by less than
+ * d 2^-52 sum_c |q_gc| max(|lo_jc|, |hi_jc|).
+ * Bounds and queries are finite numbers: a U that is NaN or -inf ranks its block
+ * last, one of +inf ranks none of its head's blocks (what is written are valid
+ * block numbers all the same).
  *   seq_lens    device int32 [batch], 0 <= T_i <= max_seq_len
  *   bounds      device [batch][Hkv][ceil(max_seq_len / 64)][2][d] (fdkv_key_bounds with that blocks_cap)
  *   q           device [batch][Hq][d]
@@ -525,7 +528,11 @@ fdkv_status fdkv_decode_parts_workspace(const fdkv_dims* dims, int32_t batch, in
  * At most 2^23 record slots (batch x Hkv x the parts' chunks) and batch x Hq, n_sel <= 2^24
  * (FDKV_E_UNSUPPORTED otherwise).
  * Probabilities are rounded to the element type for their product with V, their
- * sum is not; the order of fp32 sums depends on the batch and on the bounds.
+ * sum is not; of a bf16 block of four the residual of K~ and V~ is held to 2^-16 of
+ * itself (two bf16 terms).  The order of fp32 sums, and with it the last bits of an
+ * output, depends on the batch, on the parts and on their bounds; the same call gives
+ * the same bits.  A query or a live row that holds a NaN, and a logit of +inf, give NaN
+ * in the rows that read them.
  */
 fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_parts, const fdkv_part* parts,
                               const fdkv_tail* tail, int32_t layer, const void* q, void* out, float sm_scale, void* ws,

@@ -2,7 +2,7 @@
 //   M = max_i m_i,  o = sum_i acc_i 2^(m_i - M) / sum_i l_i 2^(m_i - M)
 // per (sequence, query head), over the records of the sequence's own parts and
 // those of the shared ones, whose number a head's workgroups leave with the
-// records.  One workgroup a query row: a quarter of a wave's lanes (an eighth at
+// records.  One workgroup a query row: half of a wave's lanes (a quarter at
 // d = 64) hold a record's d channels, four each, and every group of them folds
 // every 8th (16th) record into a running (M, l, o); the groups meet in LDS.
 // Bound by the way to memory and back: the records of one row are some 20 KB.

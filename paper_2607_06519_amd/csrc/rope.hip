@@ -55,14 +55,22 @@ struct Piece {  // a 16-byte piece as fp32
   }
 };
 
-// MANY: a long call (kRopeMany tokens or more).  Its workgroups take kRopeTokens
-// tokens each, and its stores pass the caches by: the outputs of a prompt are
-// larger than what the caches hold for the next kernel (8191 tokens of the 8B
-// shape, 201 MB read and written: calls one after the other take 45.9 us with
-// ordinary stores and 41.2 us, 4.9 TB/s, so; replayed from a graph, 4096 tokens
-// take 24.9 and 20.0 us, 1024 8.1 and 6.4, 512 5.3 and 5.9).  A step's few rows
-// stay in the caches, where its attention reads them, and are spread over as many
-// workgroups as they give.
+// MANY: a long call (kRopeMany tokens or more).  Its workgroups take all rows of
+// kRopeTokens tokens, so a token's cosines are formed once, and its stores pass
+// the caches by.  A step's few rows stay in the caches, where its attention reads
+// them, and are spread over as many workgroups as they give, each forming its
+// token's cosines for itself.  Times (us, normed heads, replayed from a graph, as
+// a step's and so), by tokens:
+//                                 512          1024          2048          4096          16384
+//   32 + 16 heads of 128, bf16    6.3   6.6    11.2   7.7    19.4  13.6    34.0  25.1    122   80
+//   32 + 16 heads of 128, fp32    9.2   8.8    15.1  15.1    25.2  22.9    44.2  42.8    161   153
+//   8 + 8 heads of 128, bf16      4.5   4.6     5.6   5.4     8.8   6.6    16.1  10.4    54.6  35.8
+//   8 + 4 heads of 64, bf16       3.7   3.8     4.4   4.4     6.6   5.0    10.4   7.7    40.2  24.2
+//   1 + 2 heads of 64, bf16       4.1   3.7     4.1   3.7     5.7   4.0     9.2   6.0    28.7  16.1
+//   2 + 2 heads of 64, fp32       3.4   3.3     4.0   3.7     4.9   4.3     7.6   5.2    24.3  12.4
+// so the number of tokens decides, whatever their rows; 256 tokens of the first take 4.9 and 6.2.
+// (8191 tokens of the 8B shape, 201 MB read and written, one call after the other:
+// 41.2 us, 4.9 TB/s, and with stores through the caches 45.9.)
 template <int D, bool BF16, bool INTER, bool MANY>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeParams P) {
   using Pc = Piece<BF16>;
