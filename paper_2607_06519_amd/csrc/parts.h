@@ -20,8 +20,8 @@
 //   O^T += V~^T P^T  the probabilities are the B operand where they lie (the
 //                  tokens of a lane's S^T registers are the tokens of its B
 //                  slots), A: transposed reads of the V tile, which goes through
-//                  LDS for that, its 16-byte pieces permuted by the row so that
-//                  the 16 rows of an operand lie in distinct banks.
+//                  LDS for that, its 16-byte pieces permuted by the row
+//                  (piece_at).
 // K~ = M + R and V~ = M + R: M as stored (bf16 or E4M3 widened to bf16, exact),
 // R a tile of LDS that is zero but for the residual entries (or the rows of a
 // token-level set) of the tile, each in its place: +-D of a pair is a bf16 value;
@@ -31,14 +31,16 @@
 // 32.6 us, E4M3 29.4 and 29.5; 256 rows of E4M3 54.0 and 54.8), 8% in bf16 at 32 rows
 // (23.3 and 25.2), and of selected blocks 2 to 4%.)  R multiplies the same operands as
 // M; no rebuilt value is rounded and no entry is gathered per query row.
-// Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
+// Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not: as in the ordinary decode, a
+// second term would double the products with V.  Outputs of bf16 queries are 1.6e-3 to 2.0e-3 of their norm off the
+// exact ones, of which their own rounding is 1.6e-3 to 1.7e-3.
 //
 // What bounds it.  Parts of single sequences: HBM where a wave has several tiles (selected blocks of 16 sequences' fp8
-// caches, all heads exact: 32.7 us a layer for 135 MB), else the way to the first one, three trips to memory that need
+// caches, all heads exact: 33.5 us a layer for 135 MB, 4.0 TB/s), else the way to the first one, three trips to memory that need
 // each other (what the launch says; lengths, offsets and blocks; rows): 64 blocks of one sequence take 10 us for 18 MB.
 // Shared spans: HBM for plain heads, and for residual ones the placing of their entries in R.  16 sequences of four
-// heads on 32768 tokens (bf16, pairs of k = 16): 41 us a layer for 161 MB, 3.9 TB/s, tails included; of eight heads on
-// 131072 tokens with token-level sets 140 us for 564 MB, 4.0 TB/s, with all heads plain 116 us, 4.8 TB/s.
+// heads on 32768 tokens (bf16, pairs of k = 16): 41 us a layer for 161 MB, 3.9 TB/s, tails included (all heads plain 37, residual 50, exact 38); of eight heads
+// on 131072 tokens with token-level sets 149 us for 564 MB, 3.8 TB/s, with all heads plain 125 us.
 #pragma once
 
 #include <type_traits>
@@ -131,8 +133,11 @@ __device__ __forceinline__ int quad_row(int g, int i) {
 }
 
 // Byte of a 16-byte piece of a row in an LDS tile: pieces permuted so that the
-// rows of an operand (one piece, 16 rows) and of a transposed read lie in
-// distinct banks.
+// 16 rows of an operand (one piece of each) lie in distinct banks.  (bf16 rows of
+// 128 channels, by counters: reading operands and staging rows have no conflict,
+// as reads and writes in a line have none; a transposed read, of two pieces of
+// 16 rows, has one for each of its other cycles, 24% of the LDS cycles of a plain
+// head.)
 template <int D, int TY>
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) {
   int f;
