@@ -539,6 +539,113 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
                               size_t ws_bytes, void* stream);
 
 /*
+ * Exact rows before their compression: the attention of a prompt over its own
+ * keys, and pages that hold rows whose number is not known ahead.  A prompt's
+ * rows (fdkv_rope_append) are attended by fdkv_prompt_attn, kept by
+ * fdkv_page_write, attended step by step by fdkv_paged_attn, and read back by
+ * fdkv_page_read where fdkv_probe and fdkv_compress, or the next piece of the
+ * prompt, take them.
+ */
+
+/* Device workspace bytes for fdkv_prompt_attn (0: none is used); `rows` as in the call. */
+fdkv_status fdkv_prompt_attn_workspace(const fdkv_dims* dims, int32_t n_tokens, int32_t batch, int32_t rows,
+                                       size_t* bytes);
+
+/*
+ * fdkv_prompt_attn - device.  One layer's causal attention of packed prompts:
+ * sequence s has N_s query tokens, q_starts[s] .. q_starts[s + 1] - 1 of the call,
+ * and K_s keys, the last N_s of which are the query tokens' own (K_s = N_s: a whole
+ * prompt; K_s > N_s: its next piece).  Token i of the sequence attends over the keys
+ * j <= K_s - N_s + i: o = softmax(q K^T * sm_scale) V; with K_s < N_s the first
+ * tokens see no key, and a token that sees none gets o = 0.
+ *   n_tokens   query tokens of the call, 0 .. 2^24 - 1 (FDKV_E_UNSUPPORTED above)
+ *   q          device [n_tokens][Hq][d], q_stride elements from token to token
+ *   batch      sequences, 1 .. 65535
+ *   q_starts   device int32 [batch + 1], ascending; tokens before the first and from the last on are of no
+ *              sequence, and their rows of out are left as they were
+ *   k, v       device; row j of head h of sequence s is at strides[0] s + strides[1] h + strides[2] (k_starts[s] + j)
+ *              elements (host int64 [3] each, >= 0): a cache [batch][Hkv][cap][d], packed rows [Hkv][n][d] or
+ *              [n][Hkv][d] with k_starts, views of a fused projection
+ *   rows       host: rows that every (sequence, head) has; k_starts[s] + K_s <= rows
+ *   k_starts   device int32 [batch], or NULL: 0
+ *   k_lens     device int32 [batch], K_s
+ *   out        device [n_tokens][Hq][d], apart from every input (q itself where q_stride is Hq * d: in place)
+ *   ws         device workspace of fdkv_prompt_attn_workspace() bytes (FDKV_E_WORKSPACE if smaller; NULL if 0)
+ * Strides are multiples of 16 bytes, rows' below 2^24 bytes (FDKV_E_UNSUPPORTED otherwise).  Numbers
+ * of q_starts, k_starts and k_lens outside of their ranges are taken as the nearest in them.
+ * Rows that no sequence names are not used, whatever they hold; a value row that is
+ * not finite may reach up to 63 tokens before its own.  Probabilities of bf16 calls are rounded
+ * to bf16 for their product with V, their sum is not.  The order of fp32 sums depends on n_tokens,
+ * batch, rows and the place of a token in its sequence; the same call gives the same bits.
+ */
+fdkv_status fdkv_prompt_attn(const fdkv_dims* dims, int32_t n_tokens, const void* q, int64_t q_stride, int32_t batch,
+                             const int32_t* q_starts, const void* k, const int64_t* k_strides, const void* v,
+                             const int64_t* v_strides, int32_t rows, const int32_t* k_starts, const int32_t* k_lens,
+                             void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Pages: row r of sequence s is slot r % page of page table[s][r / page] of a
+ * layer's pool.  A table entry outside [0, n_pages) names no page.  Rows have the
+ * type of the dims; FDKV_BF16_E4M3: a row x is held as E4M3 codes of x 2^-e with the
+ * least e for which max |x_i| <= 448 2^e (at least -126), and the byte e + 127.
+ * A value that is not finite is held as NaN; one of at least 2^128 - 2^123 as 2^128, which reads as infinite.
+ */
+typedef struct {
+  int32_t n_pages;         /* pages of the pool, >= 1 */
+  int32_t page;            /* rows of a page: 16, 32, 64, 128 or 256 */
+  int32_t batch;           /* sequences of the table, >= 1 */
+  int32_t max_pages;       /* pages of a sequence, >= 1 */
+  const int32_t* table;    /* device [batch][max_pages] */
+  void* k;                 /* device [n_pages][Hkv][page][d]; FDKV_BF16_E4M3: codes, one byte each */
+  void* v;
+  uint8_t* k_exp;          /* FDKV_BF16_E4M3: device [n_pages][Hkv][page], 16-byte aligned; else unused */
+  uint8_t* v_exp;
+} fdkv_pages;
+
+/*
+ * fdkv_page_write / fdkv_page_read - device.  One layer's K and V rows into their
+ * pages, and back (exactly what is held; an FP8 row's codes times 2^e).
+ *   n_tokens   rows of the call per head, 0 .. 2^24 - 1 (FDKV_E_UNSUPPORTED above)
+ *   k, v       device; head h of token i is at strides[0] i + strides[1] h elements (host int64 [2] each, >= 0,
+ *              multiples of 16 bytes; rows that are written do not overlap)
+ *   seqs       device int32 [n_tokens], the sequence of each token; NULL: token i is of sequence i
+ *   rows       device int32 [n_tokens], the row of each token in its sequence
+ * A token whose sequence is outside [0, batch), whose row is outside [0, max_pages * page)
+ * or whose page is none is skipped: nothing is written for it.  Two tokens of a
+ * write with the same sequence and row leave a mixture of both.
+ */
+fdkv_status fdkv_page_write(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_tokens, const void* k,
+                            const int64_t* k_strides, const void* v, const int64_t* v_strides, const int32_t* seqs,
+                            const int32_t* rows, void* stream);
+fdkv_status fdkv_page_read(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_tokens, void* k,
+                           const int64_t* k_strides, void* v, const int64_t* v_strides, const int32_t* seqs,
+                           const int32_t* rows, void* stream);
+
+/* Device workspace bytes for fdkv_paged_attn on this batch shape. */
+fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_len, size_t* bytes);
+
+/*
+ * fdkv_paged_attn - device.  One decode step of one layer over paged rows:
+ * o = softmax(q K^T * sm_scale) V over the first T_s rows of each of the pages'
+ * sequences (T_s = 0: o = 0).  Rows of no page are passed over.
+ *   lens       device int32 [batch], 0 <= T_s <= max_len
+ *   max_len    host, sizes the launch; <= max_pages * page and 2^30
+ *   more       NULL, or records of other tokens of the same sequences, which the softmax
+ *              takes in: [batch][Hkv][n_more][G][d + 4] as fdkv_decode_partial writes them with the
+ *              same q and sm_scale (a compressed prefix that the paged rows continue)
+ *   n_more     records of a (sequence, KV head) in more, 0 .. 2^20
+ *   q, out     device [batch][Hq][d]
+ *   ws         device workspace of fdkv_paged_attn_workspace() bytes (FDKV_E_WORKSPACE if smaller)
+ * At most 2^23 workgroups (batch x Hkv x the chunks of max_len) and 2^23 query rows (FDKV_E_UNSUPPORTED
+ * otherwise).  Rows at or past T_s are not used, whatever they hold.  Probabilities are rounded to
+ * the element type for their product with V, their sum is not.  The order of fp32 sums
+ * depends on batch, max_len and n_more; the same call gives the same bits.
+ */
+fdkv_status fdkv_paged_attn(const fdkv_dims* dims, const fdkv_pages* pages, const int32_t* lens, int32_t max_len,
+                            const float* more, int32_t n_more, const void* q, void* out, float sm_scale, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
  * fdkv_check_conversions - diagnostic, synchronous on `stream`.  Runs the
  * device's number encoders over every fp32 bit pattern except NaN and
  * counts where they differ from their integer definitions (0 expected):

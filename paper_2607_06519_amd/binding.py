@@ -29,7 +29,8 @@ SYMBOLS = ("fdkv_status_string", "fdkv_last_error", "fdkv_blocks", "fdkv_layout"
            "fdkv_decode_attn_static", "fdkv_decode_partial", "fdkv_decode_combine", "fdkv_selection_bytes",
            "fdkv_check_conversions", "fdkv_rope_append",
            "fdkv_key_bounds", "fdkv_block_select_workspace", "fdkv_block_select", "fdkv_decode_parts_workspace",
-           "fdkv_decode_parts")
+           "fdkv_decode_parts", "fdkv_prompt_attn_workspace", "fdkv_prompt_attn", "fdkv_page_write", "fdkv_page_read",
+           "fdkv_paged_attn_workspace", "fdkv_paged_attn")
 PAIRS, MIXED, QUADS = 0, 1, 2    # block schedules (fdkv_schedule)
 RES_CHANNELS, RES_TOKENS = 0, 1  # residual kinds (fdkv_residual)
 PART_OWN, PART_BLOCKS, PART_SHARED = 0, 1, 2  # parts of a decode step (fdkv_part_kind)
@@ -72,6 +73,12 @@ class Part(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("n_sel", ctypes.c_int32),
                 ("seq_lens", ctypes.c_void_p), ("modes", ctypes.c_void_p), ("seg_offsets", ctypes.c_void_p),
                 ("cache", ctypes.c_void_p), ("blocks", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p)]
 
 
 class Rope(ctypes.Structure):
@@ -147,6 +154,17 @@ def load():
     lib.fdkv_decode_parts_workspace.argtypes = [DP, I32, I32, P, I32, P]
     lib.fdkv_decode_parts.restype = I32
     lib.fdkv_decode_parts.argtypes = [DP, I32, I32, P, P, I32, P, P, ctypes.c_float, P, SZ, P]
+    lib.fdkv_prompt_attn_workspace.restype = I32
+    lib.fdkv_prompt_attn_workspace.argtypes = [DP, I32, I32, I32, P]
+    lib.fdkv_prompt_attn.restype = I32
+    lib.fdkv_prompt_attn.argtypes = [DP, I32, P, I64, I32, P, P, P, P, P, I32, P, P, P, ctypes.c_float, P, SZ, P]
+    for f in (lib.fdkv_page_write, lib.fdkv_page_read):
+        f.restype = I32
+        f.argtypes = [DP, P, I32, P, P, P, P, P, P, P]
+    lib.fdkv_paged_attn_workspace.restype = I32
+    lib.fdkv_paged_attn_workspace.argtypes = [DP, I32, I32, P]
+    lib.fdkv_paged_attn.restype = I32
+    lib.fdkv_paged_attn.argtypes = [DP, P, P, I32, P, I32, P, P, ctypes.c_float, P, SZ, P]
     _lib = lib
     return lib
 
@@ -526,3 +544,130 @@ def decode_parts(d: Dims, batch: int, parts: Sequence[Part], tail, layer: int, q
                                     None if tail is None else ctypes.byref(tail), int(layer), _dev(q), _dev(out),
                                     ctypes.c_float(sm_scale), _dev(ws), int(ws.numel() * ws.element_size()),
                                     _stream(stream)), "fdkv_decode_parts")
+
+
+# ----------------------------------------------------------------- exact rows: a prompt's attention, pages
+_Strides2, _Strides3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
+def prompt_attn_workspace(d: Dims, n_tokens: int, batch: int, rows: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdkv_prompt_attn_workspace(ctypes.byref(d), int(n_tokens), int(batch), int(rows), ctypes.byref(n)),
+           "fdkv_prompt_attn_workspace")
+    return int(n.value)
+
+
+def prompt_attn(d: Dims, q, k, v, q_starts, k_lens, out, sm_scale: float, ws, k_starts=None, stream=None):
+    """Queue fdkv_prompt_attn for one layer: ``q [n][Hq][d]`` (heads contiguous), ``k`` / ``v [batch or 1][Hkv][rows][d]``
+    (any strides; 1: all sequences' rows in one, from ``k_starts`` on), ``q_starts [batch + 1]``, ``k_lens [batch]``."""
+    import torch
+    e, at, hd = _element(d.dtype), torch.cuda.current_device(), d.head_dim
+    n, batch, (seqs, hkv, rows, _) = q.shape[0], k_lens.shape[0], k.shape
+    if q.shape != (n, d.n_q_heads, hd) or out.shape != q.shape or not out.is_contiguous() or q.stride(2) != 1 or \
+            (q.stride(1) != hd and d.n_q_heads > 1):
+        raise ValueError("prompt_attn: q is [n][Hq][d], contiguous but for its token stride, out contiguous")
+    if k.shape != (seqs, d.n_kv_heads, rows, hd) or v.shape != k.shape or seqs not in (1, batch) or not k.stride(3) == v.stride(3) == 1:
+        raise ValueError("prompt_attn: k and v are [batch or 1][Hkv][rows][d], channels contiguous")
+    if not (e is q.dtype is k.dtype is v.dtype is out.dtype) or \
+            not (at == q.get_device() == k.get_device() == v.get_device() == out.get_device()):
+        raise ValueError(f"prompt_attn: q, k, v and out are {e}, all on the current device (cuda:{at})")
+    numbers = [(q_starts, batch + 1), (k_lens, batch)] + ([] if k_starts is None else [(k_starts, batch)])
+    _operands("prompt_attn", e, (), numbers, ws)
+    ks, vs = (_Strides3(t.stride(0) if seqs > 1 else 0, t.stride(1), t.stride(2)) for t in (k, v))
+    st = (_lib or load()).fdkv_prompt_attn(
+        ctypes.byref(d), n, q.data_ptr(), q.stride(0), batch, q_starts.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, rows,
+        _dev(k_starts), k_lens.data_ptr(), out.data_ptr(), sm_scale, _dev(ws),
+        0 if ws is None else ws.numel() * ws.element_size(),
+        torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "fdkv_prompt_attn")
+
+
+def pages(d: Dims, k, v, table, k_exp=None, v_exp=None) -> Pages:
+    """Pages of one layer: ``k`` / ``v [n_pages][Hkv][page][d]`` in the element type, or E4M3 codes (float8_e4m3fn or
+    uint8) with ``k_exp`` / ``v_exp`` uint8 ``[n_pages][Hkv][page]``; ``table`` int32 ``[batch][max_pages]``.  The
+    descriptor keeps its tensors."""
+    import torch
+    c8 = d.dtype == BF16_E4M3
+    types = (torch.float8_e4m3fn, torch.uint8) if c8 else (_element(d.dtype),)
+    if k.dim() != 4 or k.shape[1] != d.n_kv_heads or k.shape[3] != d.head_dim or v.shape != k.shape or table.dim() != 2:
+        raise ValueError("pages: k and v are [n_pages][Hkv][page][d], table [batch][max_pages]")
+    if c8 != (k_exp is not None) or c8 != (v_exp is not None):
+        raise ValueError("pages: E4M3 pages, and only they, have exponents")
+    if c8 and not (k_exp.shape == v_exp.shape == k.shape[:3] and k_exp.dtype is v_exp.dtype is torch.uint8):
+        raise ValueError("pages: exponents are uint8 [n_pages][Hkv][page]")
+    if k.dtype not in types or v.dtype not in types or table.dtype is not torch.int32:
+        raise ValueError(f"pages: rows are {types[0]}, the table int32")
+    held = [t for t in (k, v, table, k_exp, v_exp) if t is not None]
+    if not all(t.is_contiguous() and t.get_device() == k.get_device() for t in held):
+        raise ValueError("pages: every tensor is contiguous, all on one device")
+    p = Pages(k.shape[0], k.shape[2], table.shape[0], table.shape[1], _dev(table), _dev(k), _dev(v), _dev(k_exp), _dev(v_exp))
+    p.tensors, p.device = held, k.get_device()
+    p.like = (c8, types[-1] if not c8 else None, d.n_kv_heads, d.head_dim)
+    return p
+
+
+def _of_pages(what: str, d: Dims, p: Pages, at: int):
+    """Refuses pages that were made for other dims, or on another device than the current one."""
+    c8 = d.dtype == BF16_E4M3
+    if p.like != (c8, None if c8 else _element(d.dtype), d.n_kv_heads, d.head_dim) or p.device != at:
+        raise ValueError(f"{what}: pages of other dims, or on another device than cuda:{at}")
+
+
+def _page_rows(what: str, d: Dims, p: Pages, k, v, seqs, rows, stream, written: bool):
+    import torch
+    e, at = _element(d.dtype), torch.cuda.current_device()
+    n = rows.shape[0]
+    _of_pages(what, d, p, at)
+    if k.shape != (n, d.n_kv_heads, d.head_dim) or v.shape != k.shape or not k.stride(2) == v.stride(2) == 1:
+        raise ValueError(f"{what}: k and v are [n][Hkv][d], channels contiguous")
+    if not (e is k.dtype is v.dtype) or not (at == k.get_device() == v.get_device()):
+        raise ValueError(f"{what}: k and v are {e} on the current device (cuda:{at})")
+    if written and any(t.shape[i] > 1 and t.stride(i) < d.head_dim for t in (k, v) for i in (0, 1)):
+        raise ValueError(f"{what}: rows that overlap")
+    i32 = torch.int32
+    if rows.dtype is not i32 or rows.dim() != 1 or not rows.is_contiguous() or rows.get_device() != at or \
+            (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or seqs.get_device() != at)):
+        raise ValueError(f"{what}: seqs and rows are contiguous int32 [n] on cuda:{at}")
+    st = getattr(_lib or load(), "fdkv_" + what)(
+        ctypes.byref(d), ctypes.byref(p), n, k.data_ptr(), _Strides2(k.stride(0), k.stride(1)), v.data_ptr(),
+        _Strides2(v.stride(0), v.stride(1)), _dev(seqs), rows.data_ptr(),
+        torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "fdkv_" + what)
+
+
+def page_write(d: Dims, p: Pages, k, v, seqs, rows, stream=None):
+    """Queue fdkv_page_write: ``k`` / ``v [n][Hkv][d]`` (any token and head strides) to rows ``rows [n]`` of the sequences
+    ``seqs [n]`` (None: token i is of sequence i)."""
+    _page_rows("page_write", d, p, k, v, seqs, rows, stream, False)
+
+
+def page_read(d: Dims, p: Pages, k_out, v_out, seqs, rows, stream=None):
+    """Queue fdkv_page_read: rows ``rows [n]`` of the sequences ``seqs [n]`` into ``k_out`` / ``v_out [n][Hkv][d]`` (any
+    token and head strides; rows of no page are left as they were)."""
+    _page_rows("page_read", d, p, k_out, v_out, seqs, rows, stream, True)
+
+
+def paged_attn_workspace(d: Dims, batch: int, max_len: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdkv_paged_attn_workspace(ctypes.byref(d), int(batch), int(max_len), ctypes.byref(n)),
+           "fdkv_paged_attn_workspace")
+    return int(n.value)
+
+
+def paged_attn(d: Dims, p: Pages, lens, max_len: int, q, out, sm_scale: float, ws, more=None, n_more: int = 0, stream=None):
+    """Queue fdkv_paged_attn for one layer: ``q`` / ``out [batch][Hq][d]``, ``lens [batch]``; ``more``: float32 records
+    ``[batch][Hkv][n_more][G][d + 4]`` (decode_partial) that the softmax takes in."""
+    import torch
+    at, n = torch.cuda.current_device(), p.batch * d.n_q_heads * d.head_dim
+    _of_pages("paged_attn", d, p, at)
+    _operands("paged_attn", _element(d.dtype), ((q, n), (out, n)), ((lens, p.batch),), ws)
+    if n_more:
+        _operands("paged_attn", torch.float32, ((more, p.batch * d.n_q_heads * int(n_more) * (d.head_dim + 4)),))
+    st = (_lib or load()).fdkv_paged_attn(
+        ctypes.byref(d), ctypes.byref(p), lens.data_ptr(), int(max_len), _dev(more), int(n_more), q.data_ptr(), out.data_ptr(),
+        sm_scale, ws.data_ptr(), ws.numel() * ws.element_size(),
+        torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "fdkv_paged_attn")

@@ -30,12 +30,13 @@ FLAGS = [
 # Kernels whose matrix products accumulate in ordinary vector registers: a decode over parts rescales its sums,
 # and sums in accumulation registers would be moved over and back for every tile (256 instructions of some 750).
 VGPR_SUMS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+VGPR_SUM_SOURCES = ("parts_", "prompt", "paged")
 
 
 def _compile(src: str) -> str:
     name = os.path.basename(src)
     obj = os.path.join(BUILD, name + ".o")
-    cmd = [HIPCC, *FLAGS, *(VGPR_SUMS if name.startswith("parts_") else []), "-c", src, "-o", obj]
+    cmd = [HIPCC, *FLAGS, *(VGPR_SUMS if name.startswith(VGPR_SUM_SOURCES) else []), "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stderr}")

@@ -12,6 +12,7 @@
 #include "fdkv.h"
 #include "fdkv_common.h"
 #include "fdkv_kernels.h"
+#include "rows_kernels.h"
 #include "serving_kernels.h"
 #include "probe_split.h"
 
@@ -1247,6 +1248,224 @@ fdkv_status fdkv_decode_parts(const fdkv_dims* dims, int32_t batch, int32_t n_pa
   mp.out = out;
   const hipError_t e = launch_parts_merge(mp, s);
   if (e != hipSuccess) return hip_fail(e, "parts_merge");
+  return FDKV_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Workgroups that fill the card: two on each of 256 CUs.
+constexpr int64_t kFillGroups = 512;
+
+int64_t prompt_tiles(const fdkv_dims* d, int64_t n, int batch) {
+  return n * (d->n_q_heads / d->n_kv_heads) / kPromptRows + batch;
+}
+// Workgroups that share the keys of a tile of query rows.
+int prompt_splits(const fdkv_dims* d, int n, int batch, int rows) {
+  const int64_t groups = prompt_tiles(d, n, batch) * d->n_kv_heads;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kFillGroups / groups, (rows + 255) / 256));
+}
+uint64_t prompt_ws_bytes(const fdkv_dims* d, int n, int splits) {
+  return splits == 1 ? 0 : (uint64_t)splits * n * d->n_q_heads * (d->head_dim + 4) * 4;
+}
+fdkv_status check_prompt(const fdkv_dims* dims, int32_t n_tokens, int32_t batch, int32_t rows) {
+  const fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (n_tokens < 0 || batch < 1 || rows < 0) return FDKV_E_INVALID_ARG;
+  if (batch > 65535 || n_tokens >= 1 << 24 || prompt_tiles(dims, n_tokens, batch) * dims->n_kv_heads > kMaxGroups ||
+      (int64_t)n_tokens * dims->n_q_heads > (int64_t)kMaxGroups * 2 * (256 / (dims->head_dim / 4)))
+    return FDKV_E_UNSUPPORTED;
+  return FDKV_OK;
+}
+
+// Tokens of a workgroup of a decode over pages: as many as leave some three workgroups a CU, in whole rounds of its
+// waves' tiles.
+int paged_chunk(const fdkv_dims* d, int batch, int max_len) {
+  const int64_t tokens = (int64_t)batch * d->n_kv_heads * max_len, step = 128;
+  const int64_t c = (tokens / (kFillGroups + kFillGroups / 2) + step - 1) / step * step;
+  return (int)std::min<int64_t>(std::max(c, step), kPagedChunkMost);
+}
+int paged_chunks(const fdkv_dims* d, int batch, int max_len) {
+  const int c = paged_chunk(d, batch, max_len);
+  return std::max(1, (int)(((int64_t)max_len + c - 1) / c));
+}
+
+// A stride in elements as bytes; -1: refused.
+int64_t stride_bytes(int64_t stride, int e) {
+  return stride < 0 || stride > (INT64_MAX >> 34) || stride * e % 16 ? -1 : stride * e;
+}
+
+fdkv_status check_pages(const fdkv_dims* dims, const fdkv_pages* pg, PageParams* out) {
+  const fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (!pg || pg->n_pages < 1 || pg->batch < 1 || pg->max_pages < 1) return FDKV_E_INVALID_ARG;
+  int lp = 4;
+  while (lp < 8 && (1 << lp) != pg->page) ++lp;
+  if ((1 << lp) != pg->page) return FDKV_E_INVALID_ARG;
+  const bool coef8 = dims->dtype == FDKV_BF16_E4M3;
+  if (!aligned(pg->table, 4) || !aligned(pg->k, 16) || !aligned(pg->v, 16) ||
+      (coef8 && (!aligned(pg->k_exp, 16) || !aligned(pg->v_exp, 16))))
+    return FDKV_E_INVALID_ARG;
+  if (dims->n_kv_heads > 32767) return FDKV_E_UNSUPPORTED;
+  out->k = pg->k;
+  out->v = pg->v;
+  out->k_exp = coef8 ? pg->k_exp : nullptr;
+  out->v_exp = coef8 ? pg->v_exp : nullptr;
+  out->table = pg->table;
+  out->n_pages = pg->n_pages;
+  out->log_page = lp;
+  out->batch = pg->batch;
+  out->max_pages = pg->max_pages;
+  out->hkv = dims->n_kv_heads;
+  out->d = dims->head_dim;
+  out->bf16 = dims->dtype != FDKV_F32;
+  out->coef8 = coef8;
+  return FDKV_OK;
+}
+
+fdkv_status page_rows(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_tokens, void* k,
+                      const int64_t* k_strides, void* v, const int64_t* v_strides, const int32_t* seqs,
+                      const int32_t* rows, void* stream, bool write) {
+  PageRowsParams p{};
+  const fdkv_status st = check_pages(dims, pages, &p.pg);
+  if (st != FDKV_OK) return st;
+  if (n_tokens < 0 || !k_strides || !v_strides) return FDKV_E_INVALID_ARG;
+  const int e = elem_bytes(dims);
+  p.k_tok = stride_bytes(k_strides[0], e);
+  p.k_head = stride_bytes(k_strides[1], e);
+  p.v_tok = stride_bytes(v_strides[0], e);
+  p.v_head = stride_bytes(v_strides[1], e);
+  if (p.k_tok < 0 || p.k_head < 0 || p.v_tok < 0 || p.v_head < 0) return FDKV_E_INVALID_ARG;
+  if (n_tokens >= 1 << 24) return FDKV_E_UNSUPPORTED;
+  if (n_tokens == 0) return FDKV_OK;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(rows, 4) || (seqs && !aligned(seqs, 4))) return FDKV_E_INVALID_ARG;
+  p.rows_k = k;
+  p.rows_v = v;
+  p.seqs = seqs;
+  p.rows = rows;
+  p.n_tokens = n_tokens;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t he = write ? launch_page_write(p, s) : launch_page_read(p, s);
+  if (he != hipSuccess) return hip_fail(he, write ? "page_write" : "page_read");
+  return FDKV_OK;
+}
+
+int log2_group(const fdkv_dims* d) {
+  int s = 0;
+  while ((1 << s) < d->n_q_heads / d->n_kv_heads) ++s;
+  return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+fdkv_status fdkv_prompt_attn_workspace(const fdkv_dims* dims, int32_t n_tokens, int32_t batch, int32_t rows,
+                                       size_t* bytes) {
+  const fdkv_status st = check_prompt(dims, n_tokens, batch, rows);
+  if (st != FDKV_OK) return st;
+  if (!bytes) return FDKV_E_INVALID_ARG;
+  *bytes = prompt_ws_bytes(dims, n_tokens, prompt_splits(dims, n_tokens, batch, rows));
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_prompt_attn(const fdkv_dims* dims, int32_t n_tokens, const void* q, int64_t q_stride, int32_t batch,
+                             const int32_t* q_starts, const void* k, const int64_t* k_strides, const void* v,
+                             const int64_t* v_strides, int32_t rows, const int32_t* k_starts, const int32_t* k_lens,
+                             void* out, float sm_scale, void* ws, size_t ws_bytes, void* stream) {
+  const fdkv_status st = check_prompt(dims, n_tokens, batch, rows);
+  if (st != FDKV_OK) return st;
+  if (!k_strides || !v_strides || !isfinite(sm_scale)) return FDKV_E_INVALID_ARG;
+  const int e = elem_bytes(dims);
+  PromptParams p{};
+  int64_t* const to[7] = {&p.q_stride, &p.k_seq, &p.k_head, &p.k_row, &p.v_seq, &p.v_head, &p.v_row};
+  const int64_t from[7] = {q_stride, k_strides[0], k_strides[1], k_strides[2], v_strides[0], v_strides[1], v_strides[2]};
+  for (int i = 0; i < 7; ++i)
+    if ((*to[i] = stride_bytes(from[i], e)) < 0) return FDKV_E_INVALID_ARG;
+  if (p.k_row >= 1 << 24 || p.v_row >= 1 << 24) return FDKV_E_UNSUPPORTED;
+  if (n_tokens == 0) return FDKV_OK;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_starts, 4) || !aligned(k_lens, 4) || (k_starts && !aligned(k_starts, 4)) ||
+      !aligned(k, 16) || !aligned(v, 16))
+    return FDKV_E_INVALID_ARG;
+  if (out == q && q_stride != (int64_t)dims->n_q_heads * dims->head_dim && n_tokens > 1) return FDKV_E_INVALID_ARG;
+  p.splits = prompt_splits(dims, n_tokens, batch, rows);
+  const uint64_t need = prompt_ws_bytes(dims, n_tokens, p.splits);
+  if (need && !aligned(ws, 16)) return FDKV_E_INVALID_ARG;
+  if (ws_bytes < need) return FDKV_E_WORKSPACE;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.q_starts = q_starts;
+  p.k_starts = k_starts;
+  p.k_lens = k_lens;
+  p.out = out;
+  p.ws = static_cast<float*>(ws);
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.n_tokens = n_tokens;
+  p.batch = batch;
+  p.hq = dims->n_q_heads;
+  p.hkv = dims->n_kv_heads;
+  p.g_shift = log2_group(dims);
+  p.rows = rows;
+  p.d = dims->head_dim;
+  p.bf16 = dims->dtype != FDKV_F32;
+  const hipError_t he = launch_prompt_attn(p, static_cast<hipStream_t>(stream));
+  if (he != hipSuccess) return hip_fail(he, "prompt_attn");
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_page_write(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_tokens, const void* k,
+                            const int64_t* k_strides, const void* v, const int64_t* v_strides, const int32_t* seqs,
+                            const int32_t* rows, void* stream) {
+  return page_rows(dims, pages, n_tokens, const_cast<void*>(k), k_strides, const_cast<void*>(v), v_strides, seqs, rows, stream, true);
+}
+
+fdkv_status fdkv_page_read(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_tokens, void* k,
+                           const int64_t* k_strides, void* v, const int64_t* v_strides, const int32_t* seqs,
+                           const int32_t* rows, void* stream) {
+  return page_rows(dims, pages, n_tokens, k, k_strides, v, v_strides, seqs, rows, stream, false);
+}
+
+fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_len, size_t* bytes) {
+  const fdkv_status st = check_dims(dims);
+  if (st != FDKV_OK) return st;
+  if (batch < 1 || max_len < 0 || !bytes) return FDKV_E_INVALID_ARG;
+  if (max_len > kMaxSelectTokens) return FDKV_E_UNSUPPORTED;
+  const int64_t groups = (int64_t)batch * dims->n_kv_heads * paged_chunks(dims, batch, max_len);
+  if (groups > kMaxGroups || (int64_t)batch * dims->n_q_heads > kMaxGroups) return FDKV_E_UNSUPPORTED;
+  *bytes = (uint64_t)groups * record_bytes(dims);
+  return FDKV_OK;
+}
+
+fdkv_status fdkv_paged_attn(const fdkv_dims* dims, const fdkv_pages* pages, const int32_t* lens, int32_t max_len,
+                            const float* more, int32_t n_more, const void* q, void* out, float sm_scale, void* ws,
+                            size_t ws_bytes, void* stream) {
+  PagedParams p{};
+  fdkv_status st = check_pages(dims, pages, &p.pg);
+  if (st != FDKV_OK) return st;
+  if (max_len < 0 || max_len > (int64_t)pages->max_pages * pages->page || n_more < 0 || !isfinite(sm_scale)) return FDKV_E_INVALID_ARG;
+  if (!aligned(lens, 4) || !aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || (n_more && !aligned(more, 16)))
+    return FDKV_E_INVALID_ARG;
+  if (n_more > 1 << 20) return FDKV_E_UNSUPPORTED;
+  size_t need = 0;
+  st = fdkv_paged_attn_workspace(dims, pages->batch, max_len, &need);
+  if (st != FDKV_OK) return st;
+  if (ws_bytes < need) return FDKV_E_WORKSPACE;
+  p.lens = lens;
+  p.q = q;
+  p.out = out;
+  p.ws = static_cast<float*>(ws);
+  p.more = more;
+  p.n_more = n_more;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.max_len = max_len;
+  p.chunk = paged_chunk(dims, pages->batch, max_len);
+  p.n_chunks = paged_chunks(dims, pages->batch, max_len);
+  p.hq = dims->n_q_heads;
+  p.g_shift = log2_group(dims);
+  const hipError_t he = launch_paged_attn(p, static_cast<hipStream_t>(stream));
+  if (he != hipSuccess) return hip_fail(he, "paged_attn");
   return FDKV_OK;
 }
 

@@ -1,0 +1,332 @@
+// Causal attention of packed prompts (fdkv_prompt_attn):
+//   o_i = sum_j softmax_j(q_i . k_j scale) v_j,  j <= K - N + i,
+// for the N query tokens i of a sequence and its K keys (the last N of which
+// are the query tokens' own).
+//
+// A workgroup takes 128 query rows (token, head of the group) of one sequence
+// and KV head, so that a group's heads share every key tile; its four waves
+// take 32 rows each and walk tiles of 64 keys (32 in fp32) that they stage
+// together in LDS, the next tile's loads in flight behind the current one:
+//   S^T = K Q^T    A: 32 keys x 16 channels from LDS, B: the queries, in registers;
+//   softmax        a row lives on lanes l and l + 32; running max (moved only by more
+//                  than 2^8) and sum in fp32;
+//   O^T += V^T P^T the probabilities are the B operand where they lie (the keys of
+//                  a lane's S^T registers are the keys of its B slots), A: transposed
+//                  reads of the V tile.
+// Rows of workgroups with more keys come first.  The workgroups of a KV head are
+// hkv apart, which for eight heads keeps a head's keys in one XCD's L2.
+// Keys behind a sequence's last read as zeros.  Probabilities are rounded to bf16
+// (2^-9 each at most) for the product, their sum is not.
+// Calls of few rows and many keys split the keys over workgroups, whose
+// (acc, m, l) records a second launch joins.
+#include "parts.h"
+#include "rows_kernels.h"
+
+namespace fdkv {
+
+namespace {
+
+using namespace parts;
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+template <int D, bool F32>
+struct Prompt {
+  static constexpr int E = F32 ? 4 : 2, RB = D * E, NP = RB / 16;
+  static constexpr int KEYS = F32 ? 32 : 64;
+  static constexpr int KB = KEYS / 32;                // blocks of 32 keys
+  static constexpr int TILE_BYTES = KEYS * RB;
+  static constexpr int NL = TILE_BYTES / 4096;        // 16-byte loads of a thread, of K or V
+  static constexpr int KS = F32 ? D / 8 : D / 16;     // operand pieces of a row, of a lane
+  static constexpr int CB = D / 32;                   // blocks of 32 channels
+  // Byte of a 16-byte piece of a row of a K tile: eight rows of one piece in distinct banks.
+  static __device__ __forceinline__ uint32_t k_at(int row, int piece) {
+    return (uint32_t)(row * RB + ((piece ^ (row & (NP >= 16 ? 15 : 7))) << 4));
+  }
+  // ... of a V tile: a transposed read takes 64 bytes of four rows at once.  (fp32: 128 bytes of one.)
+  static __device__ __forceinline__ uint32_t v_at(int row, int piece) {
+    const int f = F32 ? 0 : D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+    return (uint32_t)(row * RB + ((piece ^ f) << 4));
+  }
+};
+
+__device__ __forceinline__ float pair_max(float x) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int D, bool F32>
+__global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
+  using S = Prompt<D, F32>;
+  constexpr int RB = S::RB, NP = S::NP, KEYS = S::KEYS, KB = S::KB, NL = S::NL, KS = S::KS, CB = S::CB, RS = D + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * S::TILE_BYTES];  // K, V; K, V of the next tile
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int lr = lane & 31, lh = lane >> 5;
+  const int g_shift = P.g_shift, G = 1 << g_shift;
+
+  // ---- which rows: tile numbers count floor(G q_starts[s] / 128) + s from sequence s on
+  const uint32_t y = P.by_hkv.div(blockIdx.x);
+  const int head = (int)(blockIdx.x - y * P.hkv);
+  const int split = P.splits > 1 ? (int)(y % (uint32_t)P.splits) : 0;
+  const int tile = P.tiles - 1 - (int)(P.splits > 1 ? y / (uint32_t)P.splits : y);
+  auto start_of = [&](int s) { return min(max(as_const(P.q_starts)[s], 0), P.n_tokens); };
+  int seq = -1;
+  for (int s0 = 0; s0 < P.batch; s0 += 64) {
+    const int s = s0 + lane;
+    const int first = s < P.batch ? (int)(((int64_t)start_of(s) << g_shift) / kPromptRows) + s : INT32_MAX;
+    seq += __builtin_popcountll(__ballot(first <= tile));
+  }
+  if (seq < 0) return;
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  const int t0 = start_of(seq), t1 = max(start_of(seq + 1), t0);
+  const int N = t1 - t0;
+  const int64_t row0 = (int64_t)(tile - seq - (int)(((int64_t)t0 << g_shift) / kPromptRows)) * kPromptRows;
+  const int64_t n_rows = (int64_t)N << g_shift;
+  if (row0 < 0 || row0 >= n_rows) return;
+  const int k0 = P.k_starts ? min(max(as_const(P.k_starts)[seq], 0), P.rows) : 0;
+  const int K = min(max(as_const(P.k_lens)[seq], 0), P.rows - k0);
+  const int past = K - N;  // keys before the first query token's own (negative: the first tokens see none)
+
+  const int64_t my_row = row0 + 32 * wave + lr;
+  const bool live = my_row < n_rows;
+  const int64_t row = live ? my_row : n_rows - 1;
+  const int tok = t0 + (int)(row >> g_shift), g = (int)(row & (G - 1));
+  const int lim = min(max(past + (int)(row >> g_shift) + 1, 0), K);  // keys that the row sees
+  const int last_tok = (int)((min(row0 + kPromptRows, n_rows) - 1) >> g_shift);
+  const int kmax = min(max(past + last_tok + 1, 0), K);              // ... that any row sees
+  const int kmin = min(max(past + (int)(row0 >> g_shift) + 1, 0), K);  // ... that every row sees
+  int kb = 0, ke = kmax;
+  if (P.splits > 1) {
+    const int per = ((kmax + KEYS - 1) / KEYS + P.splits - 1) / P.splits * KEYS;
+    kb = min(split * per, kmax);
+    ke = min(kb + per, kmax);
+  }
+
+  // ---- queries
+  uint4 qf[KS];
+  {
+    const uint8_t* src = static_cast<const uint8_t*>(P.q) + (int64_t)tok * P.q_stride + (int64_t)(head * G + g) * RB;
+    const uint32_t keep = P.scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
+    const uint32_t sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;  // the largest product is the largest logit
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      const uint4 v = *reinterpret_cast<const uint4*>(src + 32 * j + 16 * lh);
+      qf[j] = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
+    }
+  }
+  const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
+
+  float m = -INFINITY, l = 0.f;
+  f32x16_t acc[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+
+  const uint8_t* kbase = static_cast<const uint8_t*>(P.k) + seq * P.k_seq + head * P.k_head + k0 * P.k_row;
+  const uint8_t* vbase = static_cast<const uint8_t*>(P.v) + seq * P.v_seq + head * P.v_head + k0 * P.v_row;
+  uint4 kt[NL], vt[NL];
+  const int prow = threadIdx.x / NP, piece = threadIdx.x % NP;  // the thread's first row and piece of a tile
+  constexpr int RPL = 256 / NP;
+  auto load = [&](int k) __attribute__((always_inline)) {
+    const int n = max(min(KEYS, ke - k), 0);
+    const auto kr = rsrc(kbase + (int64_t)k * P.k_row, n ? (uint64_t)(n - 1) * P.k_row + RB : 0);
+    const auto vr = rsrc(vbase + (int64_t)k * P.v_row, n ? (uint64_t)(n - 1) * P.v_row + RB : 0);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = prow + RPL * i;
+      kt[i] = ld128<0>(kr, r < n ? (uint32_t)(r * (int)P.k_row + piece * 16) : kOob);
+      vt[i] = ld128<0>(vr, r < n ? (uint32_t)(r * (int)P.v_row + piece * 16) : kOob);
+    }
+  };
+  auto stage = [&](uint8_t* buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      *reinterpret_cast<uint4*>(buf + S::k_at(prow + RPL * i, piece)) = kt[i];
+      *reinterpret_cast<uint4*>(buf + S::TILE_BYTES + S::v_at(prow + RPL * i, piece)) = vt[i];
+    }
+  };
+
+  auto step = [&](const uint8_t* buf, int k, auto masked) __attribute__((always_inline)) {
+    f32x16_t s[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        const uint4 op = *reinterpret_cast<const uint4*>(buf + S::k_at(32 * b + lr, 2 * j + lh));
+        if constexpr (F32) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(as_f32(word(op, w)), as_f32(word(qf[j], w)), s[b], 0, 0, 0);
+        } else {
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, op), __builtin_bit_cast(bf16x8_t, qf[j]), s[b], 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (k + 32 * b + 8 * (i / 4) + 4 * lh + i % 4 >= lim) s[b][i] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = scale * pair_max(mx);
+    if (__any(mx > m + kSlack)) {
+      const float mn = fmaxf(m, mx);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale, -ref));
+        l += s[b][i];
+      }
+    const uint8_t* vb = buf + S::TILE_BYTES;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            const float v = *reinterpret_cast<const float*>(vb + (8 * (i / 4) + 4 * lh + i % 4) * RB + (32 * c + lr) * 4);
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[b][i], acc[c], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // keys 32 b + 16 h ..
+          const uint4 pb = make_uint4(cvt_bf16x2(s[b][8 * h], s[b][8 * h + 1]), cvt_bf16x2(s[b][8 * h + 2], s[b][8 * h + 3]),
+                                      cvt_bf16x2(s[b][8 * h + 4], s[b][8 * h + 5]), cvt_bf16x2(s[b][8 * h + 6], s[b][8 * h + 7]));
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            i16x4_t x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int r = 32 * b + 16 * h + 8 * u + 4 * lh + ((lane & 15) >> 2);
+              const int p = 4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+              x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(vb + S::v_at(r, p) + (lane & 1) * 8));
+            }
+            const i16x8_t av = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av), __builtin_bit_cast(bf16x8_t, pb), acc[c], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+
+  if (kb < ke) {
+    load(kb);
+    stage(lds);
+    load(kb + KEYS);
+    __syncthreads();
+    int k = kb, b = 0;
+    for (; k < ke; k += KEYS) {
+      uint8_t* buf = lds + b * 2 * S::TILE_BYTES;
+      if (k + KEYS <= kmin)
+        step(buf, k, std::false_type{});
+      else
+        step(buf, k, std::true_type{});
+      if (k + KEYS < ke) {
+        stage(lds + (b ^ 1) * 2 * S::TILE_BYTES);
+        load(k + 2 * KEYS);
+      }
+      __syncthreads();
+      b ^= 1;
+    }
+  }
+  l = pair_sum(l);
+  if (!live) return;
+  if (P.splits > 1) {
+    float* rec = P.ws + (((int64_t)split * P.n_tokens + tok) * P.hq + head * G + g) * RS;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4_t*>(rec + 32 * c + 8 * i + 4 * lh) = f32x4_t{acc[c][4 * i], acc[c][4 * i + 1], acc[c][4 * i + 2], acc[c][4 * i + 3]};
+    if (lh == 0) *reinterpret_cast<float2*>(rec + D) = make_float2(m, l);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: the row sees no key
+  const int64_t at = ((int64_t)tok * P.hq + head * G + g) * D;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4_t o = {acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv, acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv};
+      const int64_t o_at = at + 32 * c + 8 * i + 4 * lh;
+      if constexpr (F32)
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(P.out) + o_at) = o;
+      else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + o_at) = make_uint2(cvt_bf16x2(o[0], o[1]), cvt_bf16x2(o[2], o[3]));
+    }
+}
+
+// Joins the splits' records of a query row: D / 4 lanes a row.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptParams P) {
+  constexpr int RS = D + 4, LPR = D / 4, RPW = 256 / LPR;
+  const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR, rows = (int64_t)P.n_tokens * P.hq;
+  const int c4 = threadIdx.x % LPR;
+  if (row >= rows) return;
+  // tokens of no sequence have no records and keep their outputs
+  const int tok = (int)(row / P.hq);
+  if (tok < as_const(P.q_starts)[0] || tok >= as_const(P.q_starts)[P.batch]) return;
+  float M = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < P.splits; ++i) {
+    const float* r = P.ws + ((int64_t)i * rows + row) * RS;
+    const float2 ml = *reinterpret_cast<const float2*>(r + D);
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(r + 4 * c4);
+    const float mn = fmaxf(M, ml.x), fo = merge_weight(M, mn), fw = merge_weight(ml.x, mn);
+    M = mn;
+    l = l * fo + ml.y * fw;
+    o = o * fo + a * fw;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (BF16)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + row * D + 4 * c4) = make_uint2(cvt_bf16x2(o[0] * inv, o[1] * inv), cvt_bf16x2(o[2] * inv, o[3] * inv));
+  else
+    *reinterpret_cast<f32x4_t*>(static_cast<float*>(P.out) + row * D + 4 * c4) = o * inv;
+}
+
+template <int D, bool F32>
+hipError_t launch(PromptParams P, hipStream_t s) {
+  P.by_hkv.set((uint32_t)P.hkv);
+  P.tiles = (int)(((int64_t)P.n_tokens << P.g_shift) / kPromptRows) + P.batch;
+  hipLaunchKernelGGL((prompt_attn_kernel<D, F32>), dim3((unsigned)((int64_t)P.tiles * P.hkv * P.splits)), dim3(256), 0, s, P);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || P.splits == 1) return e;
+  constexpr int rpw = 256 / (D / 4);
+  hipLaunchKernelGGL((prompt_join_kernel<D, !F32>), dim3((unsigned)(((int64_t)P.n_tokens * P.hq + rpw - 1) / rpw)), dim3(256), 0, s, P);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attn(const PromptParams& P, hipStream_t s) {
+  if (P.n_tokens == 0) return hipSuccess;
+  if (P.d == 128) return P.bf16 ? launch<128, false>(P, s) : launch<128, true>(P, s);
+  return P.bf16 ? launch<64, false>(P, s) : launch<64, true>(P, s);
+}
+
+}  // namespace fdkv
