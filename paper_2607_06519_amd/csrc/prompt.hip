@@ -15,7 +15,7 @@
 //                  reads of the V tile.
 // Rows of workgroups with more keys come first.  The workgroups of a KV head are
 // hkv apart, which for eight heads keeps a head's keys in one XCD's L2.
-// Keys behind a sequence's last read as zeros.  Probabilities are rounded to bf16
+// Probabilities are rounded to bf16
 // (2^-9 each at most) for the product, their sum is not.
 // Calls of few rows and many keys split the keys over workgroups, whose
 // (acc, m, l) records a second launch joins.
@@ -29,6 +29,7 @@ namespace {
 using namespace parts;
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8_t;
 
 template <int D, bool F32>
 struct Prompt {
@@ -37,18 +38,36 @@ struct Prompt {
   static constexpr int KB = KEYS / 32;                // blocks of 32 keys
   static constexpr int TILE_BYTES = KEYS * RB;
   static constexpr int NL = TILE_BYTES / 4096;        // 16-byte loads of a thread, of K or V
+  static constexpr int RPI = 64 / NP;                 // rows of a wave's load
   static constexpr int KS = F32 ? D / 8 : D / 16;     // operand pieces of a row, of a lane
   static constexpr int CB = D / 32;                   // blocks of 32 channels
   // Byte of a 16-byte piece of a row of a K tile: eight rows of one piece in distinct banks.
   static __device__ __forceinline__ uint32_t k_at(int row, int piece) {
-    return (uint32_t)(row * RB + ((piece ^ (row & (NP >= 16 ? 15 : 7))) << 4));
+    return (uint32_t)(row * RB + ((piece ^ k_flip(row)) << 4));
   }
+  static __device__ __forceinline__ int k_flip(int row) { return row & (!F32 && D == 128 ? 15 : 7); }
   // ... of a V tile: a transposed read takes 64 bytes of four rows at once.  (fp32: 128 bytes of one.)
   static __device__ __forceinline__ uint32_t v_at(int row, int piece) {
-    const int f = F32 ? 0 : D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
-    return (uint32_t)(row * RB + ((piece ^ f) << 4));
+    return (uint32_t)(row * RB + ((piece ^ v_flip(row)) << 4));
   }
+  static __device__ __forceinline__ int v_flip(int row) { return F32 ? 0 : D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
 };
+
+// 16 bytes a lane from r + voff + soff to LDS, lane i's at `to` + 16 i.  The compiler does not see the load: its own
+// waits would hold up every LDS read until the loads in flight to the other half of the buffer have landed.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t soff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(soff))
+               : "memory");
+}
+__device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory");
+}
+// A buffer of rows from `base` on (the callers stay within their rows).
+__device__ __forceinline__ u32x4_t buffer_at(const uint8_t* base) {
+  const uint64_t a = (uint64_t)(uintptr_t)base;
+  return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, ~0u, 0x00020000u};
+}
 
 __device__ __forceinline__ float pair_max(float x) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -130,29 +149,47 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
 
   const uint8_t* kbase = static_cast<const uint8_t*>(P.k) + seq * P.k_seq + head * P.k_head + k0 * P.k_row;
   const uint8_t* vbase = static_cast<const uint8_t*>(P.v) + seq * P.v_seq + head * P.v_head + k0 * P.v_row;
-  uint4 kt[NL], vt[NL];
-  const int prow = threadIdx.x / NP, piece = threadIdx.x % NP;  // the thread's first row and piece of a tile
-  constexpr int RPL = 256 / NP;
-  auto load = [&](int k) __attribute__((always_inline)) {
-    const int n = max(min(KEYS, ke - k), 0);
-    const auto kr = rsrc(kbase + (int64_t)k * P.k_row, n ? (uint64_t)(n - 1) * P.k_row + RB : 0);
-    const auto vr = rsrc(vbase + (int64_t)k * P.v_row, n ? (uint64_t)(n - 1) * P.v_row + RB : 0);
+  // the thread's place in a wave's load: rows RPI apart from wave to wave, 4 RPI from load to load (the permutation of
+  // the pieces has that period)
+  constexpr int RPI = S::RPI;
+  const int prow = RPI * wave + lane / NP, piece = lane % NP;
+  const uint32_t kp = (uint32_t)((piece ^ S::k_flip(prow)) * 16), vp = (uint32_t)((piece ^ S::v_flip(prow)) * 16);
+  const int k_row = (int)P.k_row, v_row = (int)P.v_row;
+  const uint32_t k_off = prow * k_row + kp, v_off = prow * v_row + vp;
+  const uint32_t to0 = (uint32_t)(uintptr_t)(lds_u8_t*)lds + wave * 1024;
+  auto load = [&](int k, int b) __attribute__((always_inline)) {
+    const int n = ke - k;
+    const uint32_t to = to0 + b * 2 * S::TILE_BYTES;
+    const auto kr = buffer_at(kbase + (int64_t)k * k_row), vr = buffer_at(vbase + (int64_t)k * v_row);
+    if (n >= KEYS) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = prow + RPL * i;
-      kt[i] = ld128<0>(kr, r < n ? (uint32_t)(r * (int)P.k_row + piece * 16) : kOob);
-      vt[i] = ld128<0>(vr, r < n ? (uint32_t)(r * (int)P.v_row + piece * 16) : kOob);
-    }
-  };
-  auto stage = [&](uint8_t* buf) __attribute__((always_inline)) {
+      for (int i = 0; i < NL; ++i) {
+        if (i == 0) {
+          load_lds(kr, k_off, to);
+          load_lds(vr, v_off, to + S::TILE_BYTES);
+        } else {
+          load_lds(kr, k_off, 4 * RPI * i * k_row, to + 4096 * i);
+          load_lds(vr, v_off, 4 * RPI * i * v_row, to + S::TILE_BYTES + 4096 * i);
+        }
+      }
+    } else {  // the last row stands in for those behind it, whose probabilities are 0
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      *reinterpret_cast<uint4*>(buf + S::k_at(prow + RPL * i, piece)) = kt[i];
-      *reinterpret_cast<uint4*>(buf + S::TILE_BYTES + S::v_at(prow + RPL * i, piece)) = vt[i];
+      for (int i = 0; i < NL; ++i) {
+        const int r = min(prow + 4 * RPI * i, n - 1);
+        load_lds(kr, r * k_row + kp, to + 4096 * i);
+        load_lds(vr, r * v_row + vp, to + S::TILE_BYTES + 4096 * i);
+      }
     }
   };
 
   auto step = [&](const uint8_t* buf, int k, auto masked) __attribute__((always_inline)) {
+    // Pieces are permuted by XOR and tiles start at multiples of a row, so an operand's address is the first one's with
+    // some bits flipped.  (Formed where they are used: held for a whole tile they would take the operands' registers.)
+    uint32_t ka = (uint32_t)(buf - lds) + S::k_at(lr, lh);
+    uint32_t va = (uint32_t)(buf - lds) + S::TILE_BYTES +
+                  (F32 ? S::v_at(4 * lh, 0) + lr * 4
+                       : S::v_at(4 * lh + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8);
+    asm("" : "+v"(ka), "+v"(va));
     f32x16_t s[KB];
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
@@ -160,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        const uint4 op = *reinterpret_cast<const uint4*>(buf + S::k_at(32 * b + lr, 2 * j + lh));
+        const uint4 op = *reinterpret_cast<const uint4*>(lds + (ka ^ (uint32_t)(j << 5)) + 32 * b * RB);
         if constexpr (F32) {
 #pragma unroll
           for (int w = 0; w < 4; ++w)
@@ -169,6 +206,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
           s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, op), __builtin_bit_cast(bf16x8_t, qf[j]), s[b], 0, 0, 0);
         }
       }
+      lds_fence();
     }
     if constexpr (decltype(masked)::value) {
 #pragma unroll
@@ -201,7 +239,6 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
         s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale, -ref));
         l += s[b][i];
       }
-    const uint8_t* vb = buf + S::TILE_BYTES;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       if constexpr (F32) {
@@ -209,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
         for (int i = 0; i < 16; ++i)
 #pragma unroll
           for (int c = 0; c < CB; ++c) {
-            const float v = *reinterpret_cast<const float*>(vb + (8 * (i / 4) + 4 * lh + i % 4) * RB + (32 * c + lr) * 4);
+            const float v = *reinterpret_cast<const float*>(lds + va + (8 * (i / 4) + i % 4) * RB + 128 * c);
             acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[b][i], acc[c], 0, 0, 0);
           }
       } else {
@@ -221,38 +258,30 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
           for (int c = 0; c < CB; ++c) {
             i16x4_t x[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int r = 32 * b + 16 * h + 8 * u + 4 * lh + ((lane & 15) >> 2);
-              const int p = 4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-              x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(vb + S::v_at(r, p) + (lane & 1) * 8));
-            }
+            for (int u = 0; u < 2; ++u)
+              x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(lds + (va ^ (uint32_t)(c << 6)) + (32 * b + 16 * h + 8 * u) * RB));
             const i16x8_t av = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
             acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av), __builtin_bit_cast(bf16x8_t, pb), acc[c], 0, 0, 0);
           }
+          lds_fence();
         }
       }
     }
   };
 
-  if (kb < ke) {
-    load(kb);
-    stage(lds);
-    load(kb + KEYS);
-    __syncthreads();
-    int k = kb, b = 0;
-    for (; k < ke; k += KEYS) {
-      uint8_t* buf = lds + b * 2 * S::TILE_BYTES;
-      if (k + KEYS <= kmin)
-        step(buf, k, std::false_type{});
-      else
-        step(buf, k, std::true_type{});
-      if (k + KEYS < ke) {
-        stage(lds + (b ^ 1) * 2 * S::TILE_BYTES);
-        load(k + 2 * KEYS);
-      }
-      __syncthreads();
-      b ^= 1;
-    }
+#pragma unroll
+  for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(qf[j].x), "+v"(qf[j].y), "+v"(qf[j].z), "+v"(qf[j].w));  // (waited for here, not in the loop)
+  if (kb < ke) load(kb, 0);
+  for (int k = kb, b = 0; k < ke; k += KEYS, b ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    lds_fence();
+    if (k + KEYS < ke) load(k + KEYS, b ^ 1);
+    const uint8_t* buf = lds + b * 2 * S::TILE_BYTES;
+    if (k + KEYS <= kmin)
+      step(buf, k, std::false_type{});
+    else
+      step(buf, k, std::true_type{});
   }
   l = pair_sum(l);
   if (!live) return;
