@@ -272,17 +272,19 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
 #pragma unroll
   for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(qf[j].x), "+v"(qf[j].y), "+v"(qf[j].z), "+v"(qf[j].w));  // (waited for here, not in the loop)
   if (kb < ke) load(kb, 0);
-  for (int k = kb, b = 0; k < ke; k += KEYS, b ^= 1) {
+  int k = kb, b = 0;
+  auto next = [&](auto masked) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     lds_fence();
     if (k + KEYS < ke) load(k + KEYS, b ^ 1);
-    const uint8_t* buf = lds + b * 2 * S::TILE_BYTES;
-    if (k + KEYS <= kmin)
-      step(buf, k, std::false_type{});
-    else
-      step(buf, k, std::true_type{});
-  }
+    step(lds + b * 2 * S::TILE_BYTES, k, masked);
+    k += KEYS;
+    b ^= 1;
+  };
+  const int whole = min(ke, kmin / KEYS * KEYS);  // keys of tiles that every row sees all of (kb is a multiple of KEYS)
+  while (k < whole) next(std::false_type{});
+  while (k < ke) next(std::true_type{});
   l = pair_sum(l);
   if (!live) return;
   if (P.splits > 1) {
