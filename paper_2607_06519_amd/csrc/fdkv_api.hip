@@ -1279,11 +1279,11 @@ fdkv_status check_prompt(const fdkv_dims* dims, int32_t n_tokens, int32_t batch,
   return FDKV_OK;
 }
 
-// Tokens of a workgroup of a decode over pages: as many as leave some three workgroups a CU, in whole rounds of its
-// waves' tiles.
+// Tokens of a workgroup of a decode over pages: as many as leave a workgroup for each CU, in whole rounds of its waves'
+// tiles.
 int paged_chunk(const fdkv_dims* d, int batch, int max_len) {
   const int64_t tokens = (int64_t)batch * d->n_kv_heads * max_len, step = 128;
-  const int64_t c = (tokens / (kFillGroups + kFillGroups / 2) + step - 1) / step * step;
+  const int64_t c = (tokens / (kFillGroups / 2) + step - 1) / step * step;
   return (int)std::min<int64_t>(std::max(c, step), kPagedChunkMost);
 }
 int paged_chunks(const fdkv_dims* d, int batch, int max_len) {

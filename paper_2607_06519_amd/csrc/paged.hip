@@ -68,29 +68,33 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
   const int seq = (int)P.by_chunks.div(y), chunk = (int)(y - seq * P.n_chunks);
   const int hkv = P.pg.hkv, G = 1 << P.g_shift, lp = P.pg.log_page;
   const int c0 = chunk * P.chunk;
+  // a length, the pages of the chunk (two a lane) and the queries, requested in one go
+  const int page0 = c0 >> lp;
+  const int32_t* row = P.pg.table + (int64_t)seq * P.pg.max_pages;
+  const int my_page = row[min(page0 + lane, P.pg.max_pages - 1)], my_page2 = row[min(page0 + 64 + lane, P.pg.max_pages - 1)];
+  uint4 qf[KK];
+  {
+    const uint8_t* src = static_cast<const uint8_t*>(P.q) + ((int64_t)seq * P.hq + (int64_t)head * G + min(lc, G - 1)) * S::RB;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qf[kk] = *reinterpret_cast<const uint4*>(src + (C8 ? 128 * (kk / 2) + 32 * lg + 16 * (kk % 2) : 64 * kk + 16 * lg));
+  }
   const int T = min(max(as_const(P.lens)[seq], 0), P.max_len);
   const bool single = P.n_chunks == 1 && P.n_more == 0;
   if (c0 >= T && !(single && chunk == 0)) return;  // (the join counts the chunks by the length, too)
   const int end = min(c0 + P.chunk, T);
 
-  // the pages of the chunk, one a lane
-  const int page0 = c0 >> lp;
-  const int my_page = as_const(P.pg.table)[(int64_t)seq * P.pg.max_pages + min(page0 + lane, P.pg.max_pages - 1)];
-
   // queries: the operand's channels of piece kk are 32 kk + 8 lg .. (E4M3: 64 (kk / 2) + 16 lg + 8 (kk % 2) ..,
   // fp32: 16 kk + 4 lg ..), columns past the group are zero
-  uint4 qf[KK];
-  {
-    const uint8_t* src = static_cast<const uint8_t*>(P.q) + ((int64_t)seq * P.hq + (int64_t)head * G + min(lc, G - 1)) * S::RB;
+  auto settle_queries = [&]() __attribute__((always_inline)) {  // (once the first rows are requested)
     const uint32_t keep = lc < G && P.scale_log2 != 0.f ? 0xFFFFFFFFu : 0u;
     const uint32_t sign = P.scale_log2 < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;  // the largest product is the largest logit
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      const int off = C8 ? 128 * (kk / 2) + 32 * lg + 16 * (kk % 2) : 64 * kk + 16 * lg;
-      const uint4 v = *reinterpret_cast<const uint4*>(src + off);
+      const uint4 v = qf[kk];
       qf[kk] = make_uint4((v.x ^ sign) & keep, (v.y ^ sign) & keep, (v.z ^ sign) & keep, (v.w ^ sign) & keep);
     }
-  }
+  };
   const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
 
   float m = -INFINITY, l = 0.f;
@@ -108,7 +112,8 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
       const int th = t + 16 * i;  // first token of the half
-      const int id = __builtin_amdgcn_readlane(my_page, min(max((th >> lp) - page0, 0), 63));
+      const int at = min(max((th >> lp) - page0, 0), 127);
+      const int id = at < 64 ? __builtin_amdgcn_readlane(my_page, at) : __builtin_amdgcn_readlane(my_page2, at - 64);
       const bool ok = th < end && (uint32_t)id < (uint32_t)P.pg.n_pages;
       a.live[i] = ok ? min(16, end - th) : 0;
       const int64_t slot = ok ? (((int64_t)id * hkv + head) << lp) + (th & ((1 << lp) - 1)) : 0;
@@ -127,10 +132,9 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
   };
 
   uint8_t* vt = lds + wave * S::TILE_BYTES;
+  // Tile t from its buffer, which then takes the wave's next one.
   Ahead a;
-  int t = c0 + TOK * wave;
-  if (t < end) load(t, a);
-  for (; t < end; t += 4 * TOK) {
+  auto step = [&](int t) __attribute__((always_inline)) {
     int live[TI];
     uint32_t ke[TI], ve[TI];
 #pragma unroll
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
         }
       }
     }
-    load(min(t + 4 * TOK, (1 << 30)), a);  // (behind the end: no rows)
+    load(t + 4 * TOK, a);  // (behind the end: no rows)
 
     bool whole = true;
 #pragma unroll
@@ -253,7 +257,11 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
       }
     }
     lds_fence();
-  }
+  };
+  const int t0 = c0 + TOK * wave;
+  if (t0 < end) load(t0, a);
+  settle_queries();
+  for (int t = t0; t < end; t += 4 * TOK) step(t);
   l = col_sum(l);
 
   // the waves' sums
@@ -295,20 +303,21 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
   }
 }
 
-// Joins the records of a query row: those of the chunks that its length fills, and `more`.  One workgroup a row; a
-// group of D / 4 lanes folds every (1024 / D)-th record, the groups meet in LDS.
-template <int D, bool BF16>
+// Joins the records of a query row: those of the chunks that its length fills, and `more`.  A workgroup takes CH of
+// the D channels; a group of CH / 4 lanes folds every NG-th record, the groups meet in LDS.
+template <int D, int CH, bool BF16>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams P) {
-  constexpr int RS = D + 4, LPR = D / 4, NG = 256 / LPR, U = 4;
+  constexpr int RS = D + 4, LPR = CH / 4, NG = 256 / LPR, U = 4;
   __shared__ float m_lds[NG], l_lds[NG];
-  __shared__ __attribute__((aligned(16))) float o_lds[NG][D];
-  const uint32_t row = blockIdx.x;  // (sequence, query head)
-  const int hkv = P.pg.hkv, G = 1 << P.g_shift;
+  __shared__ __attribute__((aligned(16))) float o_lds[NG][CH];
+  const uint32_t row = blockIdx.x / (D / CH);  // (sequence, query head)
+  const int part = (int)(blockIdx.x % (D / CH)) * CH;
+  const int G = 1 << P.g_shift;
   const uint32_t unit = row >> P.g_shift, seq = P.by_hkv.div(unit);
   const int g = (int)row & (G - 1);
   const int c4 = threadIdx.x % LPR, rg = threadIdx.x / LPR;
   const int T = min(max(as_const(P.lens)[seq], 0), P.max_len);
-  const int own = (T + P.chunk - 1) / P.chunk, n = own + P.n_more;
+  const int own = (int)P.by_chunk.div((uint32_t)(T + P.chunk - 1)), n = own + P.n_more;
   const float* base = P.ws + ((int64_t)unit * P.n_chunks * G + g) * RS;
   const float* more = P.more + ((int64_t)unit * P.n_more * G + g) * RS;
   float M = -INFINITY, l = 0.f;
@@ -321,7 +330,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams P) {
       const int i = min(i0 + u * NG, n - 1);
       const float* r = i < own ? base + (int64_t)i * G * RS : more + (int64_t)(i - own) * G * RS;
       ml[u] = *reinterpret_cast<const float2*>(r + D);
-      a[u] = *reinterpret_cast<const f32x4_t*>(r + 4 * c4);
+      a[u] = *reinterpret_cast<const f32x4_t*>(r + part + 4 * c4);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -338,7 +347,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams P) {
   }
   *reinterpret_cast<f32x4_t*>(&o_lds[rg][4 * c4]) = o;
   __syncthreads();
-  if (threadIdx.x < D) {
+  if (threadIdx.x < CH) {
     float top = -INFINITY, lt = 0.f, ot = 0.f;
 #pragma unroll
     for (int i = 0; i < NG; ++i) top = fmaxf(top, m_lds[i]);
@@ -349,7 +358,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams P) {
       ot = fmaf(w, o_lds[i][threadIdx.x], ot);
     }
     const float res = lt == 0.f ? 0.f : ot / lt;
-    const int64_t at = (int64_t)row * D + threadIdx.x;
+    const int64_t at = (int64_t)row * D + part + threadIdx.x;
     if constexpr (BF16)
       static_cast<uint16_t*>(P.out)[at] = (uint16_t)f32_to_bf16_bits(res);
     else
@@ -366,7 +375,12 @@ hipError_t launch(PagedParams P, hipStream_t s) {
   hipLaunchKernelGGL((paged_attn_kernel<D, TY>), grid, dim3(256), 0, s, P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || (P.n_chunks == 1 && P.n_more == 0)) return e;
-  hipLaunchKernelGGL((paged_join_kernel<D, TY != kTyF32>), dim3((unsigned)(batch * P.hq)), dim3(256), 0, s, P);
+  const unsigned rows = (unsigned)(batch * P.hq);
+  P.by_chunk.set((uint32_t)P.chunk);
+  if (rows <= 256 && P.n_chunks + P.n_more > 24)
+    hipLaunchKernelGGL((paged_join_kernel<D, 32, TY != kTyF32>), dim3(rows * (D / 32)), dim3(256), 0, s, P);
+  else
+    hipLaunchKernelGGL((paged_join_kernel<D, D, TY != kTyF32>), dim3(rows), dim3(256), 0, s, P);
   return hipGetLastError();
 }
 

@@ -79,7 +79,7 @@ __device__ __forceinline__ float pair_sum(float x) {
 }
 
 template <int D, bool F32>
-__global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void prompt_attn_kernel(PromptParams P) {
   using S = Prompt<D, F32>;
   constexpr int RB = S::RB, NP = S::NP, KEYS = S::KEYS, KB = S::KB, NL = S::NL, KS = S::KS, CB = S::CB, RS = D + 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * S::TILE_BYTES];  // K, V; K, V of the next tile
@@ -93,22 +93,28 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
   const int head = (int)(blockIdx.x - y * P.hkv);
   const int split = P.splits > 1 ? (int)(y % (uint32_t)P.splits) : 0;
   const int tile = P.tiles - 1 - (int)(P.splits > 1 ? y / (uint32_t)P.splits : y);
-  auto start_of = [&](int s) { return min(max(as_const(P.q_starts)[s], 0), P.n_tokens); };
-  int seq = -1;
+  // (lane i: the i-th of 64 sequences, everything about it in one trip to memory)
+  int seq = -1, t0 = 0, t1 = 0, k0 = 0, K = 0;
   for (int s0 = 0; s0 < P.batch; s0 += 64) {
-    const int s = s0 + lane;
-    const int first = s < P.batch ? (int)(((int64_t)start_of(s) << g_shift) / kPromptRows) + s : INT32_MAX;
-    seq += __builtin_popcountll(__ballot(first <= tile));
+    const int s = min(s0 + lane, P.batch - 1);
+    const int from = min(max(P.q_starts[s], 0), P.n_tokens), to = max(min(P.q_starts[s + 1], P.n_tokens), from);
+    const int kf = P.k_starts ? min(max(P.k_starts[s], 0), P.rows) : 0;
+    const int kn = min(max(P.k_lens[s], 0), P.rows - kf);
+    const bool before = s0 + lane < P.batch && (int)(((int64_t)from << g_shift) / kPromptRows) + s <= tile;
+    const int n = __builtin_popcountll(__ballot(before));  // (ascending starts: the first n lanes)
+    if (n == 0) break;
+    seq = s0 + n - 1;
+    t0 = __builtin_amdgcn_readlane(from, n - 1);
+    t1 = __builtin_amdgcn_readlane(to, n - 1);
+    k0 = __builtin_amdgcn_readlane(kf, n - 1);
+    K = __builtin_amdgcn_readlane(kn, n - 1);
+    if (n < 64) break;
   }
   if (seq < 0) return;
-  seq = __builtin_amdgcn_readfirstlane(seq);
-  const int t0 = start_of(seq), t1 = max(start_of(seq + 1), t0);
   const int N = t1 - t0;
   const int64_t row0 = (int64_t)(tile - seq - (int)(((int64_t)t0 << g_shift) / kPromptRows)) * kPromptRows;
   const int64_t n_rows = (int64_t)N << g_shift;
   if (row0 < 0 || row0 >= n_rows) return;
-  const int k0 = P.k_starts ? min(max(as_const(P.k_starts)[seq], 0), P.rows) : 0;
-  const int K = min(max(as_const(P.k_lens)[seq], 0), P.rows - k0);
   const int past = K - N;  // keys before the first query token's own (negative: the first tokens see none)
 
   const int64_t my_row = row0 + 32 * wave + lr;
@@ -119,6 +125,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
   const int last_tok = (int)((min(row0 + kPromptRows, n_rows) - 1) >> g_shift);
   const int kmax = min(max(past + last_tok + 1, 0), K);              // ... that any row sees
   const int kmin = min(max(past + (int)(row0 >> g_shift) + 1, 0), K);  // ... that every row sees
+  // ... that any row of the wave sees (0: it has no rows)
+  const int64_t wrow = row0 + 32 * wave;
+  const int wmax = wrow < n_rows ? min(max(past + (int)((min(wrow + 32, n_rows) - 1) >> g_shift) + 1, 0), K) : 0;
   int kb = 0, ke = kmax;
   if (P.splits > 1) {
     const int per = ((kmax + KEYS - 1) / KEYS + P.splits - 1) / P.splits * KEYS;
@@ -182,7 +191,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
     }
   };
 
-  auto step = [&](const uint8_t* buf, int k, auto masked) __attribute__((always_inline)) {
+  auto step = [&](const uint8_t* buf, int k, auto masked, auto blocks) __attribute__((always_inline)) {
+    constexpr int KB = decltype(blocks)::value;  // blocks of 32 keys: the tile's first ones
     // Pieces are permuted by XOR and tiles start at multiples of a row, so an operand's address is the first one's with
     // some bits flipped.  (Formed where they are used: held for a whole tile they would take the operands' registers.)
     uint32_t ka = (uint32_t)(buf - lds) + S::k_at(lr, lh);
@@ -278,7 +288,14 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
     __builtin_amdgcn_s_barrier();
     lds_fence();
     if (k + KEYS < ke) load(k + KEYS, b ^ 1);
-    step(lds + b * 2 * S::TILE_BYTES, k, masked);
+    const uint8_t* buf = lds + b * 2 * S::TILE_BYTES;
+    if constexpr (!decltype(masked)::value)
+      step(buf, k, masked, std::integral_constant<int, KB>{});
+    else if (KB == 1 || k + 32 >= wmax) {
+      if (k < wmax) step(buf, k, masked, std::integral_constant<int, 1>{});
+    } else {
+      step(buf, k, masked, std::integral_constant<int, KB>{});
+    }
     k += KEYS;
     b ^= 1;
   };
@@ -286,8 +303,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
   while (k < whole) next(std::false_type{});
   while (k < ke) next(std::true_type{});
   l = pair_sum(l);
-  if (!live) return;
   if (P.splits > 1) {
+    if (!live) return;
     float* rec = P.ws + (((int64_t)split * P.n_tokens + tok) * P.hq + head * G + g) * RS;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
@@ -298,18 +315,34 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams P) {
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;  // 0: the row sees no key
-  const int64_t at = ((int64_t)tok * P.hq + head * G + g) * D;
+  if constexpr (F32) {
+    if (!live) return;
+    float* out = static_cast<float*>(P.out) + ((int64_t)tok * P.hq + head * G + g) * D;
 #pragma unroll
-  for (int c = 0; c < CB; ++c)
+    for (int c = 0; c < CB; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4_t o = {acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv, acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv};
-      const int64_t o_at = at + 32 * c + 8 * i + 4 * lh;
-      if constexpr (F32)
-        *reinterpret_cast<f32x4_t*>(static_cast<float*>(P.out) + o_at) = o;
-      else
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + o_at) = make_uint2(cvt_bf16x2(o[0], o[1]), cvt_bf16x2(o[2], o[3]));
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4_t*>(out + 32 * c + 8 * i + 4 * lh) =
+            f32x4_t{acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv, acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv};
+  } else {
+    // Through LDS, so that whole rows are written at once: the half that no wave reads any more holds 32 rows a wave.
+    uint8_t* mine = lds + b * 2 * S::TILE_BYTES + wave * 32 * RB;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint2*>(mine + lr * RB + (((4 * c + i) ^ (lr & (NP - 1))) << 4) + 8 * lh) =
+            make_uint2(cvt_bf16x2(acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv), cvt_bf16x2(acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv));
+    lds_fence();
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int r = RPI * i + lane / NP;
+      const int64_t at = row0 + 32 * wave + r;
+      const uint4 w = *reinterpret_cast<const uint4*>(mine + r * RB + ((piece ^ (r & (NP - 1))) << 4));
+      if (at < n_rows)
+        *(reinterpret_cast<uint4*>(static_cast<uint16_t*>(P.out) + ((int64_t)(t0 + (int)(at >> g_shift)) * P.hq + head * G + (int)(at & (G - 1))) * D) + piece) = w;
     }
+  }
 }
 
 // Joins the splits' records of a query row: D / 4 lanes a row.

@@ -49,9 +49,9 @@ struct PageRowsParams {
 };
 
 // decode over pages (paged.hip)
-constexpr int kPagedChunkMost = 1024;  // tokens of a workgroup, at most (64 pages of 16)
+constexpr int kPagedChunkMost = 2048;  // tokens of a workgroup, at most (128 pages of 16)
 struct PagedParams {
-  DivU by_hkv, by_chunks;
+  DivU by_hkv, by_chunks, by_chunk;  // by hkv, n_chunks, chunk
   PageParams pg;
   const int32_t* lens;         // [batch]
   const void* q;               // [batch][hq][d]

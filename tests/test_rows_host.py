@@ -120,7 +120,7 @@ def test_paged_attn_refuses(lib):
         assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 1, -1, ctypes.byref(n)) == -1
         assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 1, 1, None) == -1
         assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 1 << 22, 1, ctypes.byref(n)) == -2
-        assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 1 << 13, 1 << 20, ctypes.byref(n)) == -2
+        assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 1 << 14, 1 << 20, ctypes.byref(n)) == -2
         assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 2147483647, 1 << 30, ctypes.byref(n)) == -2
 
 
