@@ -615,23 +615,27 @@ def _of_pages(what: str, d: Dims, p: Pages, at: int):
 
 
 def _page_rows(what: str, d: Dims, p: Pages, k, v, seqs, rows, stream, written: bool):
+    # (checks without loops and calls of their own, as a call takes some 7 us)
     import torch
-    e, at = _element(d.dtype), torch.cuda.current_device()
-    n = rows.shape[0]
+    e, at, i32, hd = _element(d.dtype), torch.cuda.current_device(), torch.int32, d.head_dim
+    n, = rows.shape
     _of_pages(what, d, p, at)
-    if k.shape != (n, d.n_kv_heads, d.head_dim) or v.shape != k.shape or not k.stride(2) == v.stride(2) == 1:
+    kv = k.shape
+    k0, k1, k2 = k.stride()
+    v0, v1, v2 = v.stride()
+    if kv != (n, d.n_kv_heads, hd) or v.shape != kv or not k2 == v2 == 1:
         raise ValueError(f"{what}: k and v are [n][Hkv][d], channels contiguous")
-    if not (e is k.dtype is v.dtype) or not (at == k.get_device() == v.get_device()):
-        raise ValueError(f"{what}: k and v are {e} on the current device (cuda:{at})")
-    if written and any(t.shape[i] > 1 and t.stride(i) < d.head_dim for t in (k, v) for i in (0, 1)):
+    if not (e is k.dtype is v.dtype) or not (at == k.get_device() == v.get_device() == rows.get_device()):
+        raise ValueError(f"{what}: k and v are {e}, all on the current device (cuda:{at})")
+    if written and ((n > 1 and (k0 < hd or v0 < hd)) or (d.n_kv_heads > 1 and (k1 < hd or v1 < hd))):
         raise ValueError(f"{what}: rows that overlap")
-    i32 = torch.int32
-    if rows.dtype is not i32 or rows.dim() != 1 or not rows.is_contiguous() or rows.get_device() != at or \
+    if rows.dtype is not i32 or not rows.is_contiguous() or \
             (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or seqs.get_device() != at)):
         raise ValueError(f"{what}: seqs and rows are contiguous int32 [n] on cuda:{at}")
-    st = getattr(_lib or load(), "fdkv_" + what)(
-        ctypes.byref(d), ctypes.byref(p), n, k.data_ptr(), _Strides2(k.stride(0), k.stride(1)), v.data_ptr(),
-        _Strides2(v.stride(0), v.stride(1)), _dev(seqs), rows.data_ptr(),
+    lib = _lib or load()
+    st = (lib.fdkv_page_read if written else lib.fdkv_page_write)(
+        ctypes.byref(d), ctypes.byref(p), n, k.data_ptr(), _Strides2(k0, k1), v.data_ptr(), _Strides2(v0, v1),
+        seqs.data_ptr() if seqs is not None else 0, rows.data_ptr(),
         torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
     if st:
         _check(st, "fdkv_" + what)
