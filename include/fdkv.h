@@ -605,7 +605,7 @@ typedef struct {
 /*
  * fdkv_page_write / fdkv_page_read - device.  One layer's K and V rows into their
  * pages, and back (exactly what is held; an FP8 row's codes times 2^e).
- *   n_tokens   rows of the call per head, 0 .. 2^24 - 1 (FDKV_E_UNSUPPORTED above)
+ *   n_tokens   rows of the call per head, >= 0; ceil(n_tokens / 8) x Hkv <= 2^22 (FDKV_E_UNSUPPORTED otherwise)
  *   k, v       device; head h of token i is at strides[0] i + strides[1] h elements (host int64 [2] each, >= 0,
  *              multiples of 16 bytes; rows that are written do not overlap)
  *   seqs       device int32 [n_tokens], the sequence of each token; NULL: token i is of sequence i

@@ -1311,7 +1311,6 @@ fdkv_status check_pages(const fdkv_dims* dims, const fdkv_pages* pg, PageParams*
   if (!aligned(pg->table, 4) || !aligned(pg->k, 16) || !aligned(pg->v, 16) ||
       (coef8 && (!aligned(pg->k_exp, 16) || !aligned(pg->v_exp, 16))))
     return FDKV_E_INVALID_ARG;
-  if (dims->n_kv_heads > 32767) return FDKV_E_UNSUPPORTED;
   out->k = pg->k;
   out->v = pg->v;
   out->k_exp = coef8 ? pg->k_exp : nullptr;
@@ -1341,7 +1340,7 @@ fdkv_status page_rows(const fdkv_dims* dims, const fdkv_pages* pages, int32_t n_
   p.v_tok = stride_bytes(v_strides[0], e);
   p.v_head = stride_bytes(v_strides[1], e);
   if (p.k_tok < 0 || p.k_head < 0 || p.v_tok < 0 || p.v_head < 0) return FDKV_E_INVALID_ARG;
-  if (n_tokens >= 1 << 24) return FDKV_E_UNSUPPORTED;
+  if (((int64_t)n_tokens + 7) / 8 * 2 * dims->n_kv_heads > kMaxGroups) return FDKV_E_UNSUPPORTED;
   if (n_tokens == 0) return FDKV_OK;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(rows, 4) || (seqs && !aligned(seqs, 4))) return FDKV_E_INVALID_ARG;
   p.rows_k = k;

@@ -9,11 +9,11 @@
 // binades) and the way back, c_i 2^e, is exact in bf16.  With 448 = 7/8 2^9 and
 // max |x| = m 2^k, 1 <= m < 2: e = k - 8 + (m > 7/4).  The byte kept is e + 127.
 //
-// HBM bound: every row is read once and written once, by d / 8 (bf16) or d / 4
-// lanes of 16 bytes of it each; a workgroup takes 16 consecutive tokens of one head (d = 128, bf16),
-// which of a prompt lie side by side in their page.  8191 tokens of 8 heads of 128
-// in E4M3: 13.0 us written (3.9 TB/s, read plus written), 10.7 us read (4.7 TB/s).  Two, four
-// and eight rows a lane, all requested before the first is used, took as long in E4M3
+// HBM bound: every row is read once and written once, in pieces of 16 bytes a
+// lane (32 of a row on its way into E4M3); a workgroup takes some 16 consecutive tokens of one
+// head, which of a prompt lie side by side in their page.  8191 tokens of 8 heads of 128
+// in E4M3: 11.7 us written (4.3 TB/s, read plus written), 10.8 us read (4.7 TB/s).  A head's tokens before the next head's took
+// 15.4 us written; two, four and eight rows a lane, all requested before the first is used, as long as one in E4M3
 // (93, 93 and 96 us for 32768 tokens written and read, one row 92) and longer in bf16.
 #include <type_traits>
 
@@ -51,16 +51,21 @@ __device__ __forceinline__ int64_t slot_of(const PageParams& pg, const int32_t* 
 template <int D, int TY, bool WRITE>
 __global__ __launch_bounds__(kThreads) void page_rows_kernel(PageRowsParams P) {
   constexpr int E = TY == kF32 ? 4 : 2;
-  constexpr int LPR = D * E / 16, RPW = kThreads / LPR;  // lanes of a row, rows of a workgroup
+  constexpr int N = WRITE && TY == kC8 ? 2 : 1;              // 16-byte pieces of a lane
+  constexpr int LPR = D * E / 16 / N, RPW = kThreads / LPR;  // lanes of a row, rows of a workgroup
   const int r = threadIdx.x / LPR, j = threadIdx.x % LPR;
-  const int64_t tok = (int64_t)blockIdx.x * RPW + r;
-  const bool is_v = (int)blockIdx.y >= P.pg.hkv;
-  const int head = is_v ? blockIdx.y - P.pg.hkv : blockIdx.y;
+  // the heads of 16 tokens follow each other, so that the workgroups at work together read a projection's rows whole
+  const uint32_t tile = P.by_heads.div(blockIdx.x);
+  const int h = (int)(blockIdx.x - tile * 2 * P.pg.hkv);
+  const int64_t tok = (int64_t)tile * RPW + r;
+  const bool is_v = h >= P.pg.hkv;
+  const int head = is_v ? h - P.pg.hkv : h;
   if (tok >= P.n_tokens) return;  // (the lanes of a row leave together)
   uint4* mine = reinterpret_cast<uint4*>(static_cast<uint8_t*>(is_v ? P.rows_v : P.rows_k) + tok * (is_v ? P.v_tok : P.k_tok) +
-                                         head * (is_v ? P.v_head : P.k_head)) + j;
-  uint4 w{};
+                                         head * (is_v ? P.v_head : P.k_head)) + j * N;
+  uint4 w{}, w2{};
   if constexpr (WRITE) w = *mine;  // (on its way while the row's place is looked up)
+  if constexpr (N == 2) w2 = mine[1];
   const int64_t slot = slot_of(P.pg, P.seqs, P.rows, (int)tok, head);
   uint8_t* pool = static_cast<uint8_t*>(is_v ? P.pg.v : P.pg.k);
   if constexpr (TY != kC8) {
@@ -72,13 +77,12 @@ __global__ __launch_bounds__(kThreads) void page_rows_kernel(PageRowsParams P) {
       *mine = *held;
   } else {
     uint8_t* exps = is_v ? P.pg.v_exp : P.pg.k_exp;
-    uint2* held = reinterpret_cast<uint2*>(pool) + slot * LPR + j;
     if constexpr (WRITE) {
-      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+      const uint32_t x[8] = {w.x, w.y, w.z, w.w, w2.x, w2.y, w2.z, w2.w};
       // bf16 magnitudes compare as their bits; what is not a number is left out (and stored as such)
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 8; ++i) {
         const uint32_t lo = x[i] & 0x7FFFu, hi = (x[i] >> 16) & 0x7FFFu;
         top = max(top, max(lo > 0x7F80u ? 0u : lo, hi > 0x7F80u ? 0u : hi));
       }
@@ -86,18 +90,18 @@ __global__ __launch_bounds__(kThreads) void page_rows_kernel(PageRowsParams P) {
       // top = m 2^k, k + 127 its exponent bits; m > 7/4: fraction bits above 1100000
       const int b = max((int)(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0), 1);  // 1 .. 248
       const float f = as_f32((uint32_t)(254 - b) << 23);                            // 2^-(b - 127)
-      uint32_t c[2];
+      uint32_t c[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 4; ++i) {
         const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(bf16_lo(x[2 * i]) * f, bf16_hi(x[2 * i]) * f, 0, false);
         c[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(bf16_lo(x[2 * i + 1]) * f, bf16_hi(x[2 * i + 1]) * f, lo, true);
       }
       if (slot < 0) return;
-      *held = make_uint2(c[0], c[1]);
+      reinterpret_cast<uint4*>(pool)[slot * LPR + j] = make_uint4(c[0], c[1], c[2], c[3]);
       if (j == 0) exps[slot] = (uint8_t)b;
     } else {
       if (slot < 0) return;
-      const uint2 c = *held;
+      const uint2 c = reinterpret_cast<const uint2*>(pool)[slot * LPR + j];
       const float f = as_f32((uint32_t)exps[slot] << 23);
       auto two = [&](uint32_t y, auto hi) {
         typedef float f32x2v __attribute__((ext_vector_type(2)));
@@ -110,9 +114,10 @@ __global__ __launch_bounds__(kThreads) void page_rows_kernel(PageRowsParams P) {
 }
 
 template <int D, int TY, bool WRITE>
-hipError_t launch(const PageRowsParams& P, hipStream_t s) {
-  constexpr int rpw = kThreads / (D * (TY == kF32 ? 4 : 2) / 16);
-  const dim3 grid((unsigned)(((int64_t)P.n_tokens + rpw - 1) / rpw), (unsigned)(2 * P.pg.hkv));
+hipError_t launch(PageRowsParams P, hipStream_t s) {
+  constexpr int rpw = kThreads / (D * (TY == kF32 ? 4 : 2) / 16) * (WRITE && TY == kC8 ? 2 : 1);
+  P.by_heads.set((uint32_t)(2 * P.pg.hkv));
+  const dim3 grid((unsigned)(((int64_t)P.n_tokens + rpw - 1) / rpw * (2 * P.pg.hkv)));
   hipLaunchKernelGGL((page_rows_kernel<D, TY, WRITE>), grid, dim3(kThreads), 0, s, P);
   return hipGetLastError();
 }

@@ -39,6 +39,7 @@ struct PageParams {
   bool bf16, coef8;
 };
 struct PageRowsParams {
+  DivU by_heads;               // by 2 hkv
   PageParams pg;
   void* rows_k;                // [n_tokens][hkv][d]: read by a write, written by a read
   void* rows_v;

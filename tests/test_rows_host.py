@@ -84,7 +84,7 @@ def test_page_rows_refuse(lib):
             def call(pg=_pages(), n=4, k=P, ks=(256, 128), v=P, vs=(256, 128), seqs=None, rows=P, dims=dm):
                 s2 = lambda s: (ctypes.c_int64 * 2)(*s) if s else None
                 return f(ctypes.byref(dims), ctypes.byref(pg) if pg else None, n, k, s2(ks), v, s2(vs), seqs, rows, None)
-            assert call(n=0) == 0 and call(pg=None) == -1 and call(n=-1) == -1 and call(n=1 << 24) == -2
+            assert call(n=0) == 0 and call(pg=None) == -1 and call(n=-1) == -1 and call(n=(1 << 24) + 1) == -2 and call(n=2147483647) == -2
             for pg in BAD + (BAD8 if dtype == "bf16_e4m3" else []):
                 assert call(pg=pg) == -1
             for name, off in (("k", 8), ("v", 8), ("rows", 2)):
@@ -94,7 +94,7 @@ def test_page_rows_refuse(lib):
                 assert call(**{name: None}) == -1
                 for bad in ((-128, 128), (256, -8), (257, 128), (256, 1 << 62)):
                     assert call(**{name: bad}) == -1, bad
-            assert call(dims=B.dims(2, 40000, 40000, 128, 0, dtype)) == -2
+            assert call(dims=B.dims(2, 1 << 22, 1 << 22, 128, 0, dtype), n=9) == -2
 
 
 def test_paged_attn_refuses(lib):
