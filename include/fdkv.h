@@ -621,7 +621,7 @@ fdkv_status fdkv_page_read(const fdkv_dims* dims, const fdkv_pages* pages, int32
                            const int64_t* k_strides, void* v, const int64_t* v_strides, const int32_t* seqs,
                            const int32_t* rows, void* stream);
 
-/* Device workspace bytes for fdkv_paged_attn on this batch shape. */
+/* Device workspace bytes for fdkv_paged_attn on this batch shape, enough for every shorter max_len too. */
 fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int32_t max_len, size_t* bytes);
 
 /*
@@ -635,7 +635,8 @@ fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int3
  *              same q and sm_scale (a compressed prefix that the paged rows continue)
  *   n_more     records of a (sequence, KV head) in more, 0 .. 2^20
  *   q, out     device [batch][Hq][d]
- *   ws         device workspace of fdkv_paged_attn_workspace() bytes (FDKV_E_WORKSPACE if smaller)
+ *   ws         device workspace of fdkv_paged_attn_workspace() bytes (a call needs batch x Hkv x its chunks x G x (d + 4) x 4:
+ *              FDKV_E_WORKSPACE otherwise)
  * At most 2^23 workgroups (batch x Hkv x the chunks of max_len) and 2^23 query rows (FDKV_E_UNSUPPORTED
  * otherwise).  Rows at or past T_s are not used, whatever they hold.  Probabilities are rounded to
  * the element type for their product with V, their sum is not.  The order of fp32 sums

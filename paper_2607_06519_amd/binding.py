@@ -35,6 +35,7 @@ PAIRS, MIXED, QUADS = 0, 1, 2    # block schedules (fdkv_schedule)
 RES_CHANNELS, RES_TOKENS = 0, 1  # residual kinds (fdkv_residual)
 PART_OWN, PART_BLOCKS, PART_SHARED = 0, 1, 2  # parts of a decode step (fdkv_part_kind)
 BLOCK_TOKENS = 64                # tokens of a block of sparse decode (FDKV_BLOCK_TOKENS)
+DECODE_CHUNK = 512               # tokens of a record of fdkv_decode_partial
 MAX_SELECTED, MAX_SELECT_UNITS = 1 << 24, 65535  # of fdkv_block_select: n_sel, and batch x Hkv
 
 

@@ -316,3 +316,206 @@ class Generation:
         self._refresh_ws()
         self._begin_step()
         return modes
+
+
+class PagedCache:
+    """Exact rows of up to ``batch`` sequences in pages, before (or instead of)
+    their compression: prompts as they come in, in pieces of any length, and
+    the tokens decoded after them, in one pool of ``n_pages`` pages of ``page``
+    rows a layer.  The rows of dims of ``bf16_e4m3`` are held in FP8 with an exponent a
+    row.
+
+    A prompt, or its next piece: ``rows = begin(counts)`` takes pages for
+    ``counts[s]`` new tokens of every sequence s, ``prompt(rows, layer, q, k, v)``
+    stores a layer's rows and attends (causally, over the sequence's earlier
+    rows too), and ``end(rows)`` makes them part of the sequences.  A decode step:
+    ``begin_step()`` takes a row for each active sequence, ``append(layer, k, v)``
+    and ``decode(layer, q)`` store and attend layer by layer, ``advance()`` ends
+    it.  ``read`` gives a sequence's rows back as ``probe`` and
+    ``CompressedCache.compress`` take them, and ``release`` its pages to others.
+    ``decode(..., prefix=cache)`` also attends over a compressed prefix that the
+    paged rows continue.
+
+    ``append`` and ``decode`` of one step can be captured in a graph once and
+    replayed every step between ``begin_step`` and ``advance``, which change the
+    positions, lengths and tables that the graph reads: captured calls are sized
+    for ``max_len`` rows, others for the longest sequence.  All calls go to the
+    current stream.
+    """
+
+    def __init__(self, dims: B.Dims, batch: int, max_len: int, n_pages: Optional[int] = None, page: int = 64, device="cuda"):
+        torch = _torch()
+        self.dims, self.batch, self.page = dims, int(batch), int(page)
+        self.max_len = int(max_len)
+        most = max(1, -(-self.max_len // self.page))
+        self.n_pages = self.batch * most if n_pages is None else int(n_pages)
+        shape = (self.n_pages, dims.n_kv_heads, self.page, dims.head_dim)
+        c8 = dims.dtype == B.BF16_E4M3
+        tdt = torch.uint8 if c8 else _input_dtype(dims)
+        self.table = torch.full((self.batch, most), -1, dtype=torch.int32, device=device)
+        self.pools = []
+        for _ in range(dims.n_layers):
+            kv = [torch.zeros(shape, dtype=tdt, device=device) for _ in range(2)]
+            exps = [torch.zeros(shape[:3], dtype=torch.uint8, device=device) if c8 else None for _ in range(2)]
+            self.pools.append(B.pages(dims, *kv, self.table, *exps))
+        self.free = list(range(self.n_pages - 1, -1, -1))
+        self.held = [[] for _ in range(self.batch)]         # pages of each sequence
+        self.lens_host = [0] * self.batch                   # rows held before the current step
+        self.active = [False] * self.batch
+        self._open = None                                   # rows of begin (or True: a step) that have not ended
+        self.pos = torch.full((self.batch,), -1, dtype=torch.int32, device=device)  # row that a step writes
+        self.lens = torch.zeros(self.batch, dtype=torch.int32, device=device)       # rows that a step attends
+        self._ws = torch.empty(B.paged_attn_workspace(dims, self.batch, self.max_len) // 4 + 64, dtype=torch.float32,
+                               device=device)
+
+    def _take(self, counts):
+        """Pages for ``counts[s]`` more rows of each sequence; none are taken where not all fit."""
+        torch = _torch()
+        if self._open is not None:
+            raise RuntimeError("end the rows, or advance the step, that have begun")
+        if len(counts) != self.batch or min(counts) < 0:
+            raise ValueError("a number of new rows for each sequence")
+        want = [-(-(n + c) // self.page) for n, c in zip(self.lens_host, counts)]
+        if any(n + c > self.max_len for n, c in zip(self.lens_host, counts)):
+            raise RuntimeError(f"a sequence holds {self.max_len} rows at most")
+        if sum(max(0, w - len(h)) for w, h in zip(want, self.held)) > len(self.free):
+            raise RuntimeError("the pool has no pages left: release sequences, or compress them")
+        for s, w in enumerate(want):
+            first = len(self.held[s])
+            if w > first:
+                new = [self.free.pop() for _ in range(w - first)]
+                self.held[s] += new
+                self.table[s, first:w] = torch.tensor(new, dtype=torch.int32).to(self.table.device)
+
+    def release(self, seq: int):
+        """Sequence ``seq`` ends: its pages are free, it holds no rows."""
+        if self._open is not None:
+            raise RuntimeError("end the rows, or advance the step, that have begun")
+        self.free += reversed(self.held[seq])
+        self.held[seq] = []
+        self.lens_host[seq] = 0
+        self.active[seq] = False
+        self.table[seq].fill_(-1)
+        self.pos[seq].fill_(-1)
+        self.lens[seq].fill_(0)
+
+    # ------------------------------------------------------------ prompts
+    def begin(self, counts: Sequence[int]):
+        """Takes pages for ``counts[s]`` new tokens of every sequence (packed in the order of the sequences in the calls
+        that follow) and returns what ``prompt`` needs to know of them."""
+        torch = _torch()
+        counts = [int(c) for c in counts]
+        self._take(counts)
+
+        class Rows:
+            pass
+        r, dev = Rows(), self.table.device
+        part = [s for s in range(self.batch) if counts[s]]
+        past = [self.lens_host[s] for s in part]
+        new = [counts[s] for s in part]
+        starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        k_lens = np.array([a + b for a, b in zip(past, new)], dtype=np.int32)
+        firsts = np.concatenate([[0], np.cumsum(k_lens)]).astype(np.int32)
+
+        def put(x):
+            return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)
+
+        def spans(first, count):
+            return np.concatenate([np.arange(a, a + n) for a, n in zip(first, count)]) if len(count) else np.zeros(0)
+        r.counts, r.n, r.total, r.earlier = counts, int(starts[-1]), int(firsts[-1]), sum(past)
+        r.starts, r.k_lens, r.k_starts = put(starts), put(k_lens), put(firsts[:-1])
+        r.seqs, r.rows = put(np.repeat(part, new)), put(spans(past, new))
+        if r.earlier:                                       # where earlier and new rows lie among all of the call's keys
+            r.old_seqs, r.old_rows = put(np.repeat(part, past)), put(spans([0] * len(past), past))
+            r.old_at, r.new_at = (torch.from_numpy(x.astype(np.int64)).to(dev) for x in (spans(firsts[:-1], past), spans(firsts[:-1] + past, new)))
+        n = B.prompt_attn_workspace(self.dims, r.n, len(part), r.total) if r.n else 0
+        r.ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=dev)
+        self._open = r
+        return r
+
+    def prompt(self, rows, layer: int, q, k, v, out=None, sm_scale: Optional[float] = None):
+        """Stores the new rows ``k`` / ``v [n][Hkv][d]`` of ``layer`` and returns the attention of ``q [n][Hq][d]`` over them
+        and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held.)"""
+        torch = _torch()
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if rows.n == 0:
+            return out
+        pages, scale = self.pools[layer], 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
+        B.page_write(self.dims, pages, k, v, rows.seqs, rows.rows)
+        keys = k.transpose(0, 1)[None], v.transpose(0, 1)[None]
+        if rows.earlier:
+            shape = (rows.earlier, self.dims.n_kv_heads, self.dims.head_dim)
+            old = [torch.empty(shape, dtype=k.dtype, device=k.device) for _ in range(2)]
+            B.page_read(self.dims, pages, *old, rows.old_seqs, rows.old_rows)
+            keys = [torch.empty((rows.total, *shape[1:]), dtype=k.dtype, device=k.device) for _ in range(2)]
+            for both, a, b in zip(keys, old, (k, v)):
+                both[rows.old_at], both[rows.new_at] = a, b
+            keys = [x.transpose(0, 1)[None] for x in keys]
+        B.prompt_attn(self.dims, q, *keys, rows.starts, rows.k_lens, out, scale, rows.ws, k_starts=rows.k_starts)
+        return out
+
+    def end(self, rows):
+        """The rows of ``begin`` become part of their sequences."""
+        if rows is not self._open:
+            raise RuntimeError("not the rows that have begun")
+        self._open = None
+        for s, c in enumerate(rows.counts):
+            self.lens_host[s] += c
+
+    # ------------------------------------------------------------ steps
+    def begin_step(self, active: Optional[Sequence[bool]] = None):
+        """A step of the ``active`` sequences (default: those that hold rows) begins: each takes a row."""
+        torch = _torch()
+        active = [n > 0 for n in self.lens_host] if active is None else [bool(a) for a in active]
+        self._take([int(a) for a in active])
+        self._open, self.active = True, active
+        now = torch.tensor([[n if a else -1 for n, a in zip(self.lens_host, active)],
+                            [n + 1 if a else 0 for n, a in zip(self.lens_host, active)]], dtype=torch.int32).to(self.pos.device)
+        self.pos.copy_(now[0])
+        self.lens.copy_(now[1])
+
+    def append(self, layer: int, k_new, v_new):
+        """This step's K / V rows ``[batch][Hkv][d]`` of ``layer`` (those of sequences that are not active are passed over)."""
+        B.page_write(self.dims, self.pools[layer], k_new, v_new, None, self.pos)
+
+    def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, prefix: Optional[CompressedCache] = None):
+        """The step's attention ``[batch][Hq][d]`` of ``layer``: over every active sequence's paged rows, and the tokens of
+        ``prefix``, a compressed cache of the same batch (of sequences that are not active: over the prefix alone)."""
+        torch = _torch()
+        if out is None:
+            out = torch.empty_like(q)
+        scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
+        most = self.max_len
+        if not torch.cuda.is_current_stream_capturing():
+            most = min(most, -(-max(n + a for n, a in zip(self.lens_host, self.active)) // 256) * 256)
+        more, n_more = None, 0
+        if prefix is not None:
+            if prefix.batch != self.batch or not _same_cache(prefix.dims, self.dims) or prefix.dims.n_q_heads != self.dims.n_q_heads:
+                raise ValueError("a prefix of another batch, other dimensions, or compressed another way")
+            if prefix.max_seq_len:
+                B.decode_partial(prefix.dims, self.batch, prefix.seq_lens, prefix.max_seq_len, prefix.modes, prefix.offsets,
+                                 prefix.buf, layer, q, scale, prefix.ws)
+                more, n_more = prefix.ws, -(-prefix.max_seq_len // B.DECODE_CHUNK)
+        B.paged_attn(self.dims, self.pools[layer], self.lens, most, q, out, scale, self._ws, more=more, n_more=n_more)
+        return out
+
+    def advance(self):
+        """End of a decode step: the appended rows become part of their sequences."""
+        if self._open is not True:
+            raise RuntimeError("no step has begun")
+        self._open = None
+        for s, a in enumerate(self.active):
+            self.lens_host[s] += int(a)
+        self.active = [False] * self.batch
+
+    # ------------------------------------------------------------ rows back
+    def read(self, layer: int, seq: int):
+        """K and V rows ``[Hkv][T][d]`` of a sequence, as held."""
+        torch = _torch()
+        T, dev = self.lens_host[seq], self.table.device
+        k, v = (torch.empty((self.dims.n_kv_heads, T, self.dims.head_dim), dtype=_input_dtype(self.dims), device=dev) for _ in range(2))
+        if T:
+            rows = torch.arange(T, dtype=torch.int32, device=dev)
+            B.page_read(self.dims, self.pools[layer], k.transpose(0, 1), v.transpose(0, 1), torch.full_like(rows, seq), rows)
+        return k, v

@@ -1286,13 +1286,17 @@ fdkv_status check_prompt(const fdkv_dims* dims, int32_t n_tokens, int32_t batch,
 // 116; 64 sequences of 100 to 8000 tokens 229, 228, 240, 16 of 1000 to 16000 in E4M3 63, 61, 62, 32 of 100 to 32000
 // 224, 219, 224, and 8 alike of 16384 99, 100, 96).
 int paged_chunk(const fdkv_dims* d, int batch, int max_len) {
-  const int64_t tokens = (int64_t)batch * d->n_kv_heads * max_len, step = 128;
-  const int64_t c = (tokens / (kFillGroups / 2) + step - 1) / step * step;
+  const int64_t tokens = (int64_t)batch * d->n_kv_heads * max_len, fill = kFillGroups / 2, step = 128;
+  const int64_t c = ((tokens + fill - 1) / fill + step - 1) / step * step;
   return (int)std::min<int64_t>(std::max(c, step), batch == 1 ? kPagedChunkMost : kPagedChunkMost * 3 / 4);
 }
 int paged_chunks(const fdkv_dims* d, int batch, int max_len) {
   const int c = paged_chunk(d, batch, max_len);
   return std::max(1, (int)(((int64_t)max_len + c - 1) / c));
+}
+
+int64_t paged_groups(const fdkv_dims* d, int batch, int max_len) {
+  return (int64_t)batch * d->n_kv_heads * paged_chunks(d, batch, max_len);
 }
 
 // A stride in elements as bytes; -1: refused.
@@ -1435,9 +1439,13 @@ fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int3
   if (st != FDKV_OK) return st;
   if (batch < 1 || max_len < 0 || !bytes) return FDKV_E_INVALID_ARG;
   if (max_len > kMaxSelectTokens) return FDKV_E_UNSUPPORTED;
-  const int64_t groups = (int64_t)batch * dims->n_kv_heads * paged_chunks(dims, batch, max_len);
+  const int64_t groups = paged_groups(dims, batch, max_len);
   if (groups > kMaxGroups || (int64_t)batch * dims->n_q_heads > kMaxGroups) return FDKV_E_UNSUPPORTED;
-  *bytes = (uint64_t)groups * record_bytes(dims);
+  // a shorter call may take more workgroups: up to one for each CU and one more a unit (chunks below the most), of 128
+  // tokens at least
+  const int64_t units = (int64_t)batch * dims->n_kv_heads;
+  const int64_t fill = std::min<int64_t>(kFillGroups / 2 + units, units * std::max<int64_t>(1, ((int64_t)max_len + 127) / 128));
+  *bytes = (uint64_t)std::max(groups, fill) * record_bytes(dims);
   return FDKV_OK;
 }
 
@@ -1451,10 +1459,9 @@ fdkv_status fdkv_paged_attn(const fdkv_dims* dims, const fdkv_pages* pages, cons
   if (!aligned(lens, 4) || !aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || (n_more && !aligned(more, 16)))
     return FDKV_E_INVALID_ARG;
   if (n_more > 1 << 20) return FDKV_E_UNSUPPORTED;
-  size_t need = 0;
-  st = fdkv_paged_attn_workspace(dims, pages->batch, max_len, &need);
-  if (st != FDKV_OK) return st;
-  if (ws_bytes < need) return FDKV_E_WORKSPACE;
+  const int64_t groups = max_len > kMaxSelectTokens ? 0 : paged_groups(dims, pages->batch, max_len);
+  if (max_len > kMaxSelectTokens || groups > kMaxGroups || (int64_t)pages->batch * dims->n_q_heads > kMaxGroups) return FDKV_E_UNSUPPORTED;
+  if (ws_bytes < (uint64_t)groups * record_bytes(dims)) return FDKV_E_WORKSPACE;
   p.lens = lens;
   p.q = q;
   p.out = out;

@@ -1,0 +1,232 @@
+"""PagedCache: prompts in pieces, steps, pages that go from one sequence to another, a captured step, a compressed prefix,
+and the way into compression, against attention in 64 bits over the rows as given and as held."""
+import math
+
+import numpy as np
+import pytest
+
+from rows_cases import attend, check, random_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch_dev():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    from paper_2607_06519_amd import binding
+    binding.load()
+    return torch
+
+
+num = lambda t: t.double().cpu().numpy()
+
+
+def _piece(torch, cache, g, dtype, counts):
+    """The next tokens of a prompt through every layer, checked."""
+    dims = cache.dims
+    kv, hq, d, n = dims.n_kv_heads, dims.n_q_heads, dims.head_dim, sum(counts)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    before = [[[num(x) for x in cache.read(l, s)] for s in range(cache.batch)] for l in range(dims.n_layers)]
+    rows = cache.begin(counts)
+    for l in range(dims.n_layers):
+        fused = random_rows(torch, g, dtype, n, 2 * kv, d).cuda()
+        q = torch.randn(n, hq, d, generator=g).to(dt).cuda()
+        k, v = fused[:, :kv], fused[:, kv:]
+        got = num(cache.prompt(rows, l, q, k, v))
+        at = 0
+        for s, c in enumerate(counts):
+            K, V = (np.concatenate([before[l][s][i], num(x[at:at + c]).transpose(1, 0, 2)], 1) for i, x in enumerate((k, v)))
+            past = K.shape[1] - c
+            for h in range(hq):
+                want, bound = attend(num(q[at:at + c, h]), K[h * kv // hq], V[h * kv // hq], 1 / math.sqrt(d), dtype == "f32", past + 1 + np.arange(c))
+                check(got[at:at + c, h], want, bound, (l, s, h))
+            at += c
+    cache.end(rows)
+    for l in range(dims.n_layers):                               # what was there is there
+        for s in range(cache.batch):
+            for x, old in zip(cache.read(l, s), before[l][s]):
+                assert np.array_equal(num(x)[:, :old.shape[1]], old)
+
+
+def _step(torch, cache, g, dtype, active=None):
+    dims = cache.dims
+    kv, hq, d = dims.n_kv_heads, dims.n_q_heads, dims.head_dim
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    cache.begin_step(active)
+    was = list(cache.active)
+    outs = []
+    for l in range(dims.n_layers):
+        k, v = (random_rows(torch, g, dtype, cache.batch, kv, d).cuda() for _ in range(2))
+        q = torch.randn(cache.batch, hq, d, generator=g).to(dt).cuda()
+        cache.append(l, k, v)
+        outs.append((q, k, v, cache.decode(l, q)))
+    cache.advance()
+    for l, (q, k, v, out) in enumerate(outs):
+        for s in range(cache.batch):
+            if not was[s]:
+                assert (out[s] == 0).all()
+                continue
+            K, V = (num(x) for x in cache.read(l, s))
+            if dtype != "bf16_e4m3":
+                assert np.array_equal(K[:, -1], num(k[s])) and np.array_equal(V[:, -1], num(v[s]))
+            for h in range(kv):
+                G = hq // kv
+                want, bound = attend(num(q[s, h * G:(h + 1) * G]), K[h], V[h], 1 / math.sqrt(d), dtype == "f32")
+                check(num(out[s, h * G:(h + 1) * G]), want, bound, (l, s, h))
+
+
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 16), ("bf16_e4m3", 128, 64), ("bf16_e4m3", 64, 16), ("f32", 64, 32)])
+def test_prompts_and_steps(torch_dev, dtype, d, page):
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    from paper_2607_06519_amd.cache import PagedCache
+    g = torch.Generator().manual_seed(d + page)
+    dims = B.dims(2, 2, 8, d, 0, dtype)
+    cache = PagedCache(dims, 3, 400, n_pages=-(-720 // page), page=page)
+    _piece(torch, cache, g, dtype, [100, 0, 37])
+    _piece(torch, cache, g, dtype, [50, 200, 1])
+    for active in (None, [True, False, True], None):
+        _step(torch, cache, g, dtype, active)
+    held = [num(x) for x in cache.read(1, 2)]
+    free = len(cache.free)
+    with pytest.raises(RuntimeError, match="no pages"):
+        cache.begin([240, 190, 200])
+    with pytest.raises(RuntimeError, match="at most"):
+        cache.begin([0, 0, 400])
+    assert len(cache.free) == free and cache.lens_host == [153, 202, 41]
+    cache.release(1)
+    _piece(torch, cache, g, dtype, [0, 3, 0])                    # pages that another sequence held
+    _piece(torch, cache, g, dtype, [0, 130, 200])
+    _step(torch, cache, g, dtype)
+    assert all(np.array_equal(num(x)[:, :41], h) for x, h in zip(cache.read(1, 2), held))
+    for s in range(3):
+        cache.release(s)
+    assert sorted(cache.free) == list(range(cache.n_pages))
+    cache.begin_step()                                           # no sequence holds a row
+    q = torch.ones(3, 8, d, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
+    assert (cache.decode(0, q) == 0).all()
+    cache.advance()
+
+
+def test_order_of_calls(torch_dev):
+    from paper_2607_06519_amd import binding as B
+    from paper_2607_06519_amd.cache import PagedCache
+    cache = PagedCache(B.dims(2, 1, 1, 64, 0, "bf16"), 2, 64)
+    for bad in (lambda: cache.advance(), lambda: cache.end(None) if cache._open is not None else cache.end(object())):
+        with pytest.raises(RuntimeError):
+            bad()
+    rows = cache.begin([3, 0])
+    for bad in (lambda: cache.begin([1, 0]), lambda: cache.begin_step(), lambda: cache.advance(), lambda: cache.release(0)):
+        with pytest.raises(RuntimeError):
+            bad()
+    cache.end(rows)
+    cache.begin_step()
+    for bad in (lambda: cache.begin([1, 0]), lambda: cache.begin_step(), lambda: cache.end(rows), lambda: cache.release(0)):
+        with pytest.raises(RuntimeError):
+            bad()
+    cache.advance()
+    assert cache.lens_host == [4, 0]
+    for counts in ([1], [1, -1], [1, 1, 1]):
+        with pytest.raises(ValueError):
+            cache.begin(counts)
+
+
+def test_captured_step(torch_dev):
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    from paper_2607_06519_amd.cache import PagedCache
+    dims = B.dims(2, 2, 8, 128, 0, "bf16_e4m3")
+    g = torch.Generator().manual_seed(2)
+    caches = [PagedCache(dims, 2, 300, page=16) for _ in range(2)]
+    n = 120
+    q, k, v = (torch.randn(n, h, 128, generator=g).to(torch.bfloat16).cuda() for h in (8, 2, 2))
+    for c in caches:
+        rows = c.begin([100, 20])
+        for l in range(2):
+            c.prompt(rows, l, q, k, v)
+        c.end(rows)
+    qs, ks, vs = q[:2].clone(), k[:2].clone(), v[:2].clone()
+    out = [torch.empty_like(qs) for _ in range(2)]
+
+    def layers(c, out):
+        for l in range(2):
+            c.append(l, ks, vs)
+            c.decode(l, qs, out=out[l])
+    one, other = caches
+    graph = torch.cuda.CUDAGraph()
+    for step in range(40):                                       # (past the ends of pages)
+        qs.add_(0.125)
+        ks.mul_(-1.0625)
+        one.begin_step()
+        if step == 0:
+            layers(one, out)
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                layers(one, out)
+        else:
+            graph.replay()
+        one.advance()
+        other.begin_step()
+        eager = [torch.empty_like(qs) for _ in range(2)]
+        layers(other, eager)
+        other.advance()
+        torch.cuda.synchronize()
+        for l in range(2):                                       # (a captured call is sized for more rows: sums in another order)
+            far = (out[l].double() - eager[l].double()).norm() / eager[l].double().norm()
+            assert far < 2.0 ** -8, (step, l, float(far))
+    for l in range(2):
+        for s in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(one.read(l, s), other.read(l, s)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_behind_a_prefix_and_into_compression(torch_dev, dtype):
+    """A compressed prefix and paged rows behind it give what a generation with a tail of the same rows gives within the
+    bound of either; the rows read back compress to the same bytes as the rows that went in."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    from paper_2607_06519_amd.cache import CompressedCache, PagedCache
+    from serving_cases import attend as attend_parts, make_cache, unit_rows
+    dims = B.dims(2, 2, 8, 128, 16, dtype)
+    prefix, _ = make_cache(torch, dims, [300, 600], np.array([[[0, 1]], [[2, 1]]], np.uint8), 3)
+    raw = prefix.host_bytes()
+    cache = PagedCache(dims, 2, 256, page=32)
+    g = torch.Generator().manual_seed(5)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    given = [[], []]
+    for step in range(40):
+        cache.begin_step([True, step < 33])
+        k, v = (random_rows(torch, g, dtype, 2, 2, 128).cuda() for _ in range(2))
+        for l in range(2):
+            cache.append(l, k * (l + 1), v)
+        given[0].append(k), given[1].append(v)
+        if step < 39:
+            cache.advance()
+    q = torch.randn(2, 8, 128, generator=g).to(dt).cuda()
+    outs = [num(cache.decode(l, q, prefix=prefix)) for l in range(2)]
+    cache.advance()
+    for l in range(2):
+        for s in range(2):
+            K, V = (num(x) for x in cache.read(l, s))
+            if s == 1:
+                K = V = np.zeros((2, 0, 128))                    # not active in this step: the prefix alone
+            for h in range(2):
+                parts = [unit_rows(prefix, raw, s, l, h, dtype), (K[h], V[h], np.zeros_like(K[h]), np.zeros_like(K[h]))]
+                want, bound = attend_parts(num(q[s, 4 * h:4 * h + 4]), parts, 1 / math.sqrt(128), dtype == "f32", False)
+                check(outs[l][s, 4 * h:4 * h + 4], want, bound, (l, s, h))
+    with pytest.raises(ValueError):
+        PagedCache(dims, 3, 64).decode(0, torch.zeros(3, 8, 128, dtype=dt, device="cuda"), prefix=prefix)
+    # into compression
+    T = cache.lens_host[0]
+    back = [cache.read(l, 0) for l in range(2)]
+    straight = [tuple((torch.stack([x[0] for x in given[i]], 1) * (l + 1 if i == 0 else 1)).contiguous() for i in range(2)) for l in range(2)]
+    bufs = []
+    for layers in (back, straight):
+        c = CompressedCache(dims, [T], np.array([[[1, 0]]], np.uint8))
+        c.buf.zero_()
+        c.compress(0, [x[0] for x in layers], [x[1] for x in layers])
+        torch.cuda.synchronize()
+        bufs.append(c.host_bytes())
+    assert np.array_equal(*bufs)

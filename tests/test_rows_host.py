@@ -124,6 +124,17 @@ def test_paged_attn_refuses(lib):
         assert lib.fdkv_paged_attn_workspace(ctypes.byref(dm), 2147483647, 1 << 30, ctypes.byref(n)) == -2
 
 
+def test_paged_workspace_serves_shorter_calls(lib):
+    """The query never gives less for more tokens, nor less than a call's chunks of at least 128 tokens need."""
+    for batch, kv in ((1, 1), (1, 8), (3, 2), (64, 8), (300, 1)):
+        dm = B.dims(2, kv, 4 * kv, 128, 0, "bf16")
+        last, unit = 0, batch * kv * 4 * 132 * 4
+        for m in sorted({*range(0, 3000, 97), *range(32500, 33100), *(1 << i for i in range(21)), *((1 << i) + 1 for i in range(21))}):
+            n = B.paged_attn_workspace(dm, batch, m)
+            assert n >= last and unit <= n <= unit * max(1, -(-m // 128)), (batch, kv, m)
+            last = n
+
+
 @pytest.fixture
 def cpu(monkeypatch, lib):
     """CPU tensors pass for the current device's; a call that is not refused ends in Queued."""
