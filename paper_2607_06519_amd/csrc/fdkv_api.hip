@@ -1261,10 +1261,12 @@ constexpr int64_t kFillGroups = 512;
 int64_t prompt_tiles(const fdkv_dims* d, int64_t n, int batch) {
   return n * (d->n_q_heads / d->n_kv_heads) / kPromptRows + batch;
 }
-// Workgroups that share the keys of a tile of query rows.
+// Workgroups that share the keys of a tile of query rows: as many as fill the card, of 256 keys at least (fp32, whose
+// tiles of 32 keys take longer than bf16's of 64: 64).
 int prompt_splits(const fdkv_dims* d, int n, int batch, int rows) {
   const int64_t groups = prompt_tiles(d, n, batch) * d->n_kv_heads;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kFillGroups / groups, (rows + 255) / 256));
+  const int64_t least = d->dtype == FDKV_F32 ? 64 : 256;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kFillGroups / groups, (rows + least - 1) / least));
 }
 uint64_t prompt_ws_bytes(const fdkv_dims* d, int n, int splits) {
   return splits == 1 ? 0 : (uint64_t)splits * n * d->n_q_heads * (d->head_dim + 4) * 4;

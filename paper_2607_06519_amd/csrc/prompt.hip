@@ -345,26 +345,51 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void prompt_attn_kernel(Promp
   }
 }
 
-// Joins the splits' records of a query row: D / 4 lanes a row.
-template <int D, bool BF16>
+// Joins the splits' records of a query row: D / 4 lanes fold one record after another (four in flight), or, of many
+// splits (WIDE), the D / 4-lane groups of a workgroup take turns and meet in LDS.
+template <int D, bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptParams P) {
-  constexpr int RS = D + 4, LPR = D / 4, RPW = 256 / LPR;
-  const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR, rows = (int64_t)P.n_tokens * P.hq;
-  const int c4 = threadIdx.x % LPR;
+  constexpr int RS = D + 4, LPR = D / 4, NG = 256 / LPR, STEP = WIDE ? NG : 1, U = 4;
+  __shared__ float ml_lds[NG][2];
+  __shared__ __attribute__((aligned(16))) float o_lds[NG][D];
+  const int rg = threadIdx.x / LPR, c4 = threadIdx.x % LPR;
+  const int64_t rows = (int64_t)P.n_tokens * P.hq, row = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * NG + rg;
   if (row >= rows) return;
   // tokens of no sequence have no records and keep their outputs
   const int tok = (int)(row / P.hq);
   if (tok < as_const(P.q_starts)[0] || tok >= as_const(P.q_starts)[P.batch]) return;
+  const float* base = P.ws + row * RS;
   float M = -INFINITY, l = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < P.splits; ++i) {
-    const float* r = P.ws + ((int64_t)i * rows + row) * RS;
-    const float2 ml = *reinterpret_cast<const float2*>(r + D);
-    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(r + 4 * c4);
-    const float mn = fmaxf(M, ml.x), fo = merge_weight(M, mn), fw = merge_weight(ml.x, mn);
+  auto fold = [&](float mi, float li, const f32x4_t& a) __attribute__((always_inline)) {
+    const float mn = fmaxf(M, mi), fo = merge_weight(M, mn), fw = merge_weight(mi, mn);
     M = mn;
-    l = l * fo + ml.y * fw;
+    l = l * fo + li * fw;
     o = o * fo + a * fw;
+  };
+  for (int i0 = WIDE ? rg : 0; i0 < P.splits; i0 += STEP * U) {
+    float2 ml[U];
+    f32x4_t a[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* r = base + (int64_t)min(i0 + STEP * u, P.splits - 1) * rows * RS;
+      ml[u] = *reinterpret_cast<const float2*>(r + D);
+      a[u] = *reinterpret_cast<const f32x4_t*>(r + 4 * c4);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + STEP * u < P.splits) fold(ml[u].x, ml[u].y, a[u]);
+  }
+  if constexpr (WIDE) {
+    if (c4 == 0) {
+      ml_lds[rg][0] = M;
+      ml_lds[rg][1] = l;
+    }
+    *reinterpret_cast<f32x4_t*>(&o_lds[rg][4 * c4]) = o;
+    __syncthreads();
+    if (rg) return;
+#pragma unroll
+    for (int i = 1; i < NG; ++i) fold(ml_lds[i][0], ml_lds[i][1], *reinterpret_cast<const f32x4_t*>(&o_lds[i][4 * c4]));
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if constexpr (BF16)
@@ -380,8 +405,12 @@ hipError_t launch(PromptParams P, hipStream_t s) {
   hipLaunchKernelGGL((prompt_attn_kernel<D, F32>), dim3((unsigned)((int64_t)P.tiles * P.hkv * P.splits)), dim3(256), 0, s, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || P.splits == 1) return e;
+  const int64_t rows = (int64_t)P.n_tokens * P.hq;
   constexpr int rpw = 256 / (D / 4);
-  hipLaunchKernelGGL((prompt_join_kernel<D, !F32>), dim3((unsigned)(((int64_t)P.n_tokens * P.hq + rpw - 1) / rpw)), dim3(256), 0, s, P);
+  if (P.splits > 8)
+    hipLaunchKernelGGL((prompt_join_kernel<D, !F32, true>), dim3((unsigned)rows), dim3(256), 0, s, P);
+  else
+    hipLaunchKernelGGL((prompt_join_kernel<D, !F32, false>), dim3((unsigned)((rows + rpw - 1) / rpw)), dim3(256), 0, s, P);
   return hipGetLastError();
 }
 
