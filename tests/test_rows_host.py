@@ -58,7 +58,7 @@ def test_prompt_workspace(lib):
     for dtype in ("bf16", "f32"):
         for d, G in ((64, 1), (128, 4), (128, 8)):
             dm = B.dims(2, 8, 8 * G, d, 0, dtype)
-            least = 64 if dtype == "f32" else 256
+            least = 64 if dtype == "f32" else 1024
             for n in (1, 7, 250, 3000):
                 for batch in (1, 5):
                     for rows in (0, 1, 256, 257, 5000, 1 << 20, 2147483647):
