@@ -1304,9 +1304,9 @@ int64_t paged_groups(const fdkv_dims* d, int batch, int max_len) {
   return (int64_t)batch * d->n_kv_heads * paged_chunks(d, batch, max_len);
 }
 
-// A stride in elements as bytes; -1: refused.
+// A stride in elements (2^35 at most: times 2^25 tokens it stays in 64 bits) as bytes; -1: refused.
 int64_t stride_bytes(int64_t stride, int e) {
-  return stride < 0 || stride > (INT64_MAX >> 34) || stride * e % 16 ? -1 : stride * e;
+  return stride < 0 || stride > (int64_t)1 << 35 || stride * e % 16 ? -1 : stride * e;
 }
 
 fdkv_status check_pages(const fdkv_dims* dims, const fdkv_pages* pg, PageParams* out) {
@@ -1398,7 +1398,7 @@ fdkv_status fdkv_prompt_attn(const fdkv_dims* dims, int32_t n_tokens, const void
   if (p.k_row >= 1 << 24 || p.v_row >= 1 << 24) return FDKV_E_UNSUPPORTED;
   if (n_tokens == 0) return FDKV_OK;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_starts, 4) || !aligned(k_lens, 4) || (k_starts && !aligned(k_starts, 4)) ||
-      !aligned(k, 16) || !aligned(v, 16))
+      (rows && (!aligned(k, 16) || !aligned(v, 16))))
     return FDKV_E_INVALID_ARG;
   if (out == q && q_stride != (int64_t)dims->n_q_heads * dims->head_dim && n_tokens > 1) return FDKV_E_INVALID_ARG;
   p.splits = prompt_splits(dims, n_tokens, batch, rows);

@@ -117,6 +117,19 @@ def test_one_long_prompt(torch_dev):
     _run(torch_dev, "bf16", 128, 1, 2, [(1500, 1500)], "packed")
 
 
+def test_no_keys_at_all(torch_dev):
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    dims = B.dims(2, 2, 8, 128, 0, "bf16")
+    q = torch.ones(5, 8, 128, dtype=torch.bfloat16, device="cuda")
+    k = torch.empty(1, 2, 0, 128, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 3.0)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()
+    B.prompt_attn(dims, q, k, k, i32(0, 4), i32(7), out, 0.1, None)
+    torch.cuda.synchronize()
+    assert (out[:4] == 0).all() and (out[4] == 3).all()
+
+
 def test_in_place(torch_dev):
     torch = torch_dev
     from paper_2607_06519_amd import binding as B

@@ -34,6 +34,7 @@ def test_prompt_attn_refuses(lib):
     assert call(dims=None) == -1 and call(n=-1) == -1 and call(batch=0) == -1 and call(rows=-1) == -1
     for name, off in (("q", 8), ("starts", 2), ("k", 8), ("v", 8), ("lens", 2), ("out", 8)):
         assert call(**{name: None}) == -1 and call(**{name: P + off}) == -1, name
+    assert call(rows=0, k=P + 8, n=0) == 0
     assert call(first=P + 2) == -1 and call(scale=NAN) == -1 and call(scale=INF) == -1
     assert call(qs=-128) == -1 and call(qs=129) == -1 and call(qs=1 << 62) == -1
     for name in ("ks", "vs"):
