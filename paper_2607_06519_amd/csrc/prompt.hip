@@ -31,10 +31,9 @@ using namespace parts;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) uint8_t lds_u8_t;
 
-template <int D, bool F32>
+template <int D, bool F32, int KEYS>
 struct Prompt {
   static constexpr int E = F32 ? 4 : 2, RB = D * E, NP = RB / 16;
-  static constexpr int KEYS = F32 ? 32 : 64;
   static constexpr int KB = KEYS / 32;                // blocks of 32 keys
   static constexpr int TILE_BYTES = KEYS * RB;
   static constexpr int NL = TILE_BYTES / 4096;        // 16-byte loads of a thread, of K or V
@@ -78,10 +77,17 @@ __device__ __forceinline__ float pair_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-template <int D, bool F32>
-__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void prompt_attn_kernel(PromptParams P) {
-  using S = Prompt<D, F32>;
-  constexpr int RB = S::RB, NP = S::NP, KEYS = S::KEYS, KB = S::KB, NL = S::NL, KS = S::KS, CB = S::CB, RS = D + 4;
+// KEYS of a tile, workgroups to a CU.  (bf16 of 128 channels: tiles of 64 keys for calls of few workgroups, 32 for those of
+// many, of which a CU then holds three.  us, tiles of 64 and 32: a prompt of 1000 tokens 26.7 and 28.9, 2048 tokens 53.5 and
+// 57.3, 8191 tokens 515 and 512, 24 prompts of up to 2000 tokens 360 and 341, 32768 tokens 7770 and 7600.)
+constexpr int keys_of(int D, bool F32, bool many) { return F32 || (many && D == 128) ? 32 : 64; }
+constexpr int per_cu(int D, bool F32, int keys) { return D == 64 ? 4 : F32 || keys == 64 ? 2 : 3; }
+constexpr int kManyGroups = 1024;
+
+template <int D, bool F32, int KEYS>
+__global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(PromptParams P) {
+  using S = Prompt<D, F32, KEYS>;
+  constexpr int RB = S::RB, NP = S::NP, KB = S::KB, NL = S::NL, KS = S::KS, CB = S::CB, RS = D + 4;
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * S::TILE_BYTES];  // K, V; K, V of the next tile
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -325,8 +331,12 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void prompt_attn_kernel(Promp
         *reinterpret_cast<f32x4_t*>(out + 32 * c + 8 * i + 4 * lh) =
             f32x4_t{acc[c][4 * i] * inv, acc[c][4 * i + 1] * inv, acc[c][4 * i + 2] * inv, acc[c][4 * i + 3] * inv};
   } else {
-    // Through LDS, so that whole rows are written at once: the half that no wave reads any more holds 32 rows a wave.
-    uint8_t* mine = lds + b * 2 * S::TILE_BYTES + wave * 32 * RB;
+    // Through LDS, so that whole rows are written at once, 32 of a wave: in the half that no wave reads any more, or, where
+    // that is too small, in all of it once every wave is done.
+    constexpr bool HALF = 2 * S::TILE_BYTES >= 4 * 32 * RB;
+    static_assert(4 * S::TILE_BYTES >= 4 * 32 * RB, "LDS for the rows of four waves");
+    if constexpr (!HALF) __syncthreads();
+    uint8_t* mine = lds + (HALF ? b * 2 * S::TILE_BYTES : 0) + wave * 32 * RB;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -402,7 +412,12 @@ template <int D, bool F32>
 hipError_t launch(PromptParams P, hipStream_t s) {
   P.by_hkv.set((uint32_t)P.hkv);
   P.tiles = (int)(((int64_t)P.n_tokens << P.g_shift) / kPromptRows) + P.batch;
-  hipLaunchKernelGGL((prompt_attn_kernel<D, F32>), dim3((unsigned)((int64_t)P.tiles * P.hkv * P.splits)), dim3(256), 0, s, P);
+  const dim3 grid((unsigned)((int64_t)P.tiles * P.hkv * P.splits));
+  constexpr int few = keys_of(D, F32, false), many = keys_of(D, F32, true);
+  if (few == many || grid.x <= kManyGroups)
+    hipLaunchKernelGGL((prompt_attn_kernel<D, F32, few>), grid, dim3(256), 0, s, P);
+  else
+    hipLaunchKernelGGL((prompt_attn_kernel<D, F32, many>), grid, dim3(256), 0, s, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || P.splits == 1) return e;
   const int64_t rows = (int64_t)P.n_tokens * P.hq;

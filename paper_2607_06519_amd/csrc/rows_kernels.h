@@ -11,7 +11,6 @@ namespace fdkv {
 
 // causal attention of packed prompts (prompt.hip)
 constexpr int kPromptRows = 128;    // query rows (token, head of the group) of a workgroup
-constexpr int kPromptKeys = 64;     // keys of a tile (fp32: 32)
 struct PromptParams {
   DivU by_hkv;
   const void* q;               // [n_tokens][hq][d], q_stride bytes a token

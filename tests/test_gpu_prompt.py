@@ -117,6 +117,38 @@ def test_one_long_prompt(torch_dev):
     _run(torch_dev, "bf16", 128, 1, 2, [(1500, 1500)], "packed")
 
 
+@pytest.mark.parametrize("dtype,d,kv,G,seqs", [
+    ("bf16", 128, 16, 8, [(1100, 1100)]),                          # many workgroups: shorter tiles
+    ("bf16", 128, 64, 1, [(700, 700), (1, 1), (1300, 1333), (33, 31)]),
+    ("bf16", 64, 32, 4, [(900, 1000), (200, 200)]),
+    ("f32", 64, 16, 4, [(2100, 2100)]),
+])
+def test_many_workgroups(torch_dev, dtype, d, kv, G, seqs):
+    """A sample of the heads of a call that fills the card several times over."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    dims = B.dims(2, kv, kv * G, d, 0, dtype)
+    g = torch.Generator().manual_seed(kv + G)
+    n, keys = sum(s[0] for s in seqs), [s[1] for s in seqs]
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q = torch.randn(n, kv * G, d, generator=g).to(dt).cuda()
+    total = sum(keys)
+    k, v = (random_rows(torch, g, dtype, 1, kv, total, d).cuda() for _ in range(2))
+    starts, firsts = np.cumsum([0] + [s[0] for s in seqs]), np.cumsum([0] + keys)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32).cuda()
+    out = torch.full_like(q, math.nan)
+    B.prompt_attn(dims, q, k, v, i32(starts), i32(keys), out, 0.1, None, k_starts=i32(firsts[:-1]))
+    torch.cuda.synchronize()
+    assert out.isfinite().all()
+    got = out.double().cpu().numpy()
+    for s, (N, m) in enumerate(seqs):
+        a, f = starts[s], firsts[s]
+        for h in (0, kv * G // 2 + 1, kv * G - 1):
+            want, bound = attend(q[a:a + N, h].double().cpu().numpy(), k[0, h // G, f:f + m].double().cpu().numpy(),
+                                 v[0, h // G, f:f + m].double().cpu().numpy(), 0.1, dtype == "f32", np.clip(m - N + np.arange(N) + 1, 0, m))
+            check(got[a:a + N, h], want, bound, (s, h))
+
+
 def test_no_keys_at_all(torch_dev):
     torch = torch_dev
     from paper_2607_06519_amd import binding as B
