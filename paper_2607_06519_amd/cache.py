@@ -425,9 +425,9 @@ class PagedCache:
         r.counts, r.n, r.total, r.earlier = counts, int(starts[-1]), int(firsts[-1]), sum(past)
         r.starts, r.k_lens, r.k_starts = put(starts), put(k_lens), put(firsts[:-1])
         r.seqs, r.rows = put(np.repeat(part, new)), put(spans(past, new))
-        if r.earlier:                                       # where earlier and new rows lie among all of the call's keys
-            r.old_seqs, r.old_rows = put(np.repeat(part, past)), put(spans([0] * len(past), past))
-            r.old_at, r.new_at = (torch.from_numpy(x.astype(np.int64)).to(dev) for x in (spans(firsts[:-1], past), spans(firsts[:-1] + past, new)))
+        if r.earlier:                                       # every row of the sequences, and where the new ones lie among them
+            r.all_seqs, r.all_rows = put(np.repeat(part, k_lens)), put(spans([0] * len(part), k_lens))
+            r.new_at = torch.from_numpy(spans(firsts[:-1] + past, new).astype(np.int64)).to(dev)
         n = B.prompt_attn_workspace(self.dims, r.n, len(part), r.total) if r.n else 0
         r.ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=dev)
         self._open = r
@@ -445,13 +445,13 @@ class PagedCache:
         B.page_write(self.dims, pages, k, v, rows.seqs, rows.rows)
         keys = k.transpose(0, 1)[None], v.transpose(0, 1)[None]
         if rows.earlier:
-            shape = (rows.earlier, self.dims.n_kv_heads, self.dims.head_dim)
-            old = [torch.empty(shape, dtype=k.dtype, device=k.device) for _ in range(2)]
-            B.page_read(self.dims, pages, *old, rows.old_seqs, rows.old_rows)
-            keys = [torch.empty((rows.total, *shape[1:]), dtype=k.dtype, device=k.device) for _ in range(2)]
-            for both, a, b in zip(keys, old, (k, v)):
-                both[rows.old_at], both[rows.new_at] = a, b
-            keys = [x.transpose(0, 1)[None] for x in keys]
+            shape = (self.dims.n_kv_heads, rows.total, self.dims.head_dim)
+            keys = [torch.empty(shape, dtype=k.dtype, device=k.device) for _ in range(2)]
+            B.page_read(self.dims, pages, *(x.transpose(0, 1) for x in keys), rows.all_seqs, rows.all_rows)
+            if self.dims.dtype == B.BF16_E4M3:
+                for both, given in zip(keys, (k, v)):
+                    both[:, rows.new_at] = given.transpose(0, 1)
+            keys = [x[None] for x in keys]
         B.prompt_attn(self.dims, q, *keys, rows.starts, rows.k_lens, out, scale, rows.ws, k_starts=rows.k_starts)
         return out
 

@@ -1265,11 +1265,12 @@ int64_t prompt_tiles(const fdkv_dims* d, int64_t n, int batch) {
 // less than they save: 1024, in fp32, whose tiles of 32 keys take longer than bf16's of 64, 64.  (us, 32 + 16 heads of
 // 128, by the least number of keys, 256, 512, 1024, 2048: a prompt of 300 tokens 17.5, 13.0, 14.3, 11.8, of 1000 31.1, 31.4,
 // 26.1, 25.9, 64 tokens on 8000 keys 28.9, 26.7, 30.6, 45.0, one on 32000 33.6, 33.5, 33.8, 47.6; fp32, 64, 128, 256, 512: a
-// prompt of 128 tokens 20.4, 23.4, 23.6, 23.3, of 300 31.0, 30.3, 34.9, 46.9, 16 tokens on 4000 keys 33.2, 29.8, 43.0, 74.4.)
+// prompt of 128 tokens 20.4, 23.4, 23.6, 23.3, of 300 31.0, 30.3, 34.9, 46.9, 16 tokens on 4000 keys 33.2, 29.8, 43.0, 74.4.
+// fp32 fills the card twice, as its longest workgroups take longest: 1500 tokens 187, filled once 251.)
 int prompt_splits(const fdkv_dims* d, int n, int batch, int rows) {
   const int64_t groups = prompt_tiles(d, n, batch) * d->n_kv_heads;
   const int64_t least = d->dtype == FDKV_F32 ? 64 : 1024;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kFillGroups / groups, (rows + least - 1) / least));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((d->dtype == FDKV_F32 ? 2 : 1) * kFillGroups / groups, (rows + least - 1) / least));
 }
 uint64_t prompt_ws_bytes(const fdkv_dims* d, int n, int splits) {
   return splits == 1 ? 0 : (uint64_t)splits * n * d->n_q_heads * (d->head_dim + 4) * 4;
