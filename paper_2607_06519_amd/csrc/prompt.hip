@@ -5,7 +5,7 @@
 //
 // A workgroup takes 128 query rows (token, head of the group) of one sequence
 // and KV head, so that a group's heads share every key tile; its four waves
-// take 32 rows each and walk tiles of 64 keys (32 in fp32) that they stage
+// take 32 rows each and walk tiles of 64 or 32 keys that they stage
 // together in LDS, the next tile's loads in flight behind the current one:
 //   S^T = K Q^T    A: 32 keys x 16 channels from LDS, B: the queries, in registers;
 //   softmax        a row lives on lanes l and l + 32; running max (moved only by more
@@ -13,12 +13,21 @@
 //   O^T += V^T P^T the probabilities are the B operand where they lie (the keys of
 //                  a lane's S^T registers are the keys of its B slots), A: transposed
 //                  reads of the V tile.
-// Rows of workgroups with more keys come first.  The workgroups of a KV head are
-// hkv apart, which for eight heads keeps a head's keys in one XCD's L2.
-// Probabilities are rounded to bf16
-// (2^-9 each at most) for the product, their sum is not.
+// Workgroups with more keys come first.  Those of a KV head are hkv apart, which
+// for eight heads keeps a head's keys in one XCD's L2.
+// Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
 // Calls of few rows and many keys split the keys over workgroups, whose
 // (acc, m, l) records a second launch joins.
+//
+// What bounds it.  Long prompts: the card's power.  32768 tokens of 32 + 8 heads of 128
+// (bf16) take 7.7 ms, 1.14 PFLOP/s, where a large matrix product of the library's reaches 1.37, at some 1.65 GHz
+// with the matrix units busy 61% of the time; with inputs of zeros the same call takes 4.97 ms, 1.77 PFLOP/s, and the
+// library's product reaches 1.79.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
+// tokens, now 517); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
+// groups of waves that take turns at the matrix units wait for their operands (8.7), the next tile's logits ahead of
+// this one's softmax gain 1% where they have the registers.  Prompts of 2048 tokens (54 us, 630 TFLOP/s) wait for their
+// longest workgroups, a step of which takes 1.2 us without others beside it.  fp32: the matrix units (8192 tokens 140
+// TFLOP/s of 154).
 #include "parts.h"
 #include "rows_kernels.h"
 
@@ -156,6 +165,7 @@ __global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(
   const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
 
   float m = -INFINITY, l = 0.f;
+  float ref = 0.f, top = -INFINITY;  // m, or 0 where there is none; the product that moves it
   f32x16_t acc[CB];
 #pragma unroll
   for (int c = 0; c < CB; ++c)
@@ -236,18 +246,18 @@ __global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-    mx = scale * pair_max(mx);
-    if (__any(mx > m + kSlack)) {
-      const float mn = fmaxf(m, mx);
+    if (__any(mx > top)) {  // (of the lane's keys: the row's other lane looks at its own)
+      const float mn = fmaxf(m, scale * pair_max(mx));
       const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
+      ref = mn == -INFINITY ? 0.f : mn;
+      top = mn == -INFINITY ? -INFINITY : (mn + kSlack) / scale;
       l *= f;
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[c][i] *= f;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
