@@ -593,6 +593,8 @@ def pages(d: Dims, k, v, table, k_exp=None, v_exp=None) -> Pages:
     types = (torch.float8_e4m3fn, torch.uint8) if c8 else (_element(d.dtype),)
     if k.dim() != 4 or k.shape[1] != d.n_kv_heads or k.shape[3] != d.head_dim or v.shape != k.shape or table.dim() != 2:
         raise ValueError("pages: k and v are [n_pages][Hkv][page][d], table [batch][max_pages]")
+    if k.shape[2] not in (16, 32, 64, 128, 256):
+        raise ValueError(f"pages: a page holds 16, 32, 64, 128 or 256 rows, not {k.shape[2]}")
     if c8 != (k_exp is not None) or c8 != (v_exp is not None):
         raise ValueError("pages: E4M3 pages, and only they, have exponents")
     if c8 and not (k_exp.shape == v_exp.shape == k.shape[:3] and k_exp.dtype is v_exp.dtype is torch.uint8):
@@ -609,8 +611,11 @@ def pages(d: Dims, k, v, table, k_exp=None, v_exp=None) -> Pages:
 
 
 def _of_pages(what: str, d: Dims, p: Pages, at: int):
-    """Refuses pages that were made for other dims, or on another device than the current one."""
+    """Refuses pages that were made for other dims, or on another device than the current one.  (A descriptor of plain
+    addresses says nothing of what lies there.)"""
     c8 = d.dtype == BF16_E4M3
+    if getattr(p, "like", None) is None:
+        return
     if p.like != (c8, None if c8 else _element(d.dtype), d.n_kv_heads, d.head_dim) or p.device != at:
         raise ValueError(f"{what}: pages of other dims, or on another device than cuda:{at}")
 

@@ -61,15 +61,32 @@ struct Prompt {
   static __device__ __forceinline__ int v_flip(int row) { return F32 ? 0 : D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
 };
 
-// 16 bytes a lane from r + voff + soff to LDS, lane i's at `to` + 16 i.  The compiler does not see the load: its own
-// waits would hold up every LDS read until the loads in flight to the other half of the buffer have landed.
+// 16 bytes a lane from r + voff (+ i step) to LDS, lane l's at `to` (+ 4096 i) + 16 l.  The compiler does not see the
+// loads: its own waits would hold up every LDS read until the loads in flight to the other half of the buffer have
+// landed.  Nor does it see what has to lie between: five wait states from a vector instruction's write of a scalar
+// register to its use as an address, one from the write of m0 to a load to LDS.
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t soff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(soff))
-               : "memory");
-}
 __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory");
+  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory");
+}
+template <int NL>
+__device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t step, uint32_t to) {
+  static_assert(NL == 2 || NL == 4, "loads of a tile");
+  if constexpr (NL == 2)
+    asm volatile(
+        "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds" ::"s"(to),
+        "s"(to + 4096), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(step))
+        : "memory");
+  else
+    asm volatile(
+        "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds\n\t"
+        "s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %7 offen lds\n\t"
+        "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %8 offen lds" ::"s"(to),
+        "s"(to + 4096), "s"(to + 8192), "s"(to + 12288), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(step)),
+        "s"(__builtin_amdgcn_readfirstlane(2 * step)), "s"(__builtin_amdgcn_readfirstlane(3 * step))
+        : "memory");
 }
 // A buffer of rows from `base` on (the callers stay within their rows).
 __device__ __forceinline__ u32x4_t buffer_at(const uint8_t* base) {
@@ -187,16 +204,8 @@ __global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(
     const uint32_t to = to0 + b * 2 * S::TILE_BYTES;
     const auto kr = buffer_at(kbase + (int64_t)k * k_row), vr = buffer_at(vbase + (int64_t)k * v_row);
     if (n >= KEYS) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        if (i == 0) {
-          load_lds(kr, k_off, to);
-          load_lds(vr, v_off, to + S::TILE_BYTES);
-        } else {
-          load_lds(kr, k_off, 4 * RPI * i * k_row, to + 4096 * i);
-          load_lds(vr, v_off, 4 * RPI * i * v_row, to + S::TILE_BYTES + 4096 * i);
-        }
-      }
+      load_lds<NL>(kr, k_off, 4 * RPI * k_row, to);
+      load_lds<NL>(vr, v_off, 4 * RPI * v_row, to + S::TILE_BYTES);
     } else {  // the last row stands in for those behind it, whose probabilities are 0
 #pragma unroll
       for (int i = 0; i < NL; ++i) {

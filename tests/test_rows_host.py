@@ -187,7 +187,8 @@ def test_page_operands(cpu):
     for d, a in ((dims, (k, z(4, 2, 8, 128), i32(3, 2))), (dims, (k, k, i32(6))), (dims, (k, k, i32(3, 2), u8(4, 2, 16), u8(4, 2, 16))),
                  (dims8, (u8(4, 2, 16, 128), u8(4, 2, 16, 128), i32(3, 2))), (dims8, (u8(4, 2, 16, 128), u8(4, 2, 16, 128), i32(3, 2), u8(4, 2, 16), u8(4, 2, 8))),
                  (dims8, (k, k, i32(3, 2), u8(4, 2, 16), u8(4, 2, 16))), (dims, (u8(4, 2, 16, 128), k, i32(3, 2))), (dims, (k, k, torch.zeros(3, 2))),
-                 (dims, (z(4, 2, 128, 16).transpose(2, 3), k, i32(3, 2))), (dims, (k, k, i32(2, 3).T)), (dims, (z(4, 16, 2, 128), z(4, 16, 2, 128), i32(3, 2)))):
+                 (dims, (z(4, 2, 128, 16).transpose(2, 3), k, i32(3, 2))), (dims, (k, k, i32(2, 3).T)), (dims, (z(4, 16, 2, 128), z(4, 16, 2, 128), i32(3, 2))),
+                 (dims, (z(4, 2, 24, 128), z(4, 2, 24, 128), i32(3, 2))), (dims, (z(4, 2, 512, 128), z(4, 2, 512, 128), i32(3, 2)))):
         with pytest.raises(ValueError):
             B.pages(d, *a)
     rows = z(5, 2, 128)
