@@ -340,7 +340,8 @@ class PagedCache:
     replayed every step between ``begin_step`` and ``advance``, which change the
     positions, lengths and tables that the graph reads: captured calls are sized
     for ``max_len`` rows, others for the longest sequence.  All calls go to the
-    current stream.
+    current stream, and the calls and replays of one cache to one stream (they
+    share a workspace).
     """
 
     def __init__(self, dims: B.Dims, batch: int, max_len: int, n_pages: Optional[int] = None, page: int = 64, device="cuda"):

@@ -25,9 +25,11 @@
 // library's product reaches 1.79.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
 // tokens, now 517); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
 // groups of waves that take turns at the matrix units wait for their operands (8.7), the next tile's logits ahead of
-// this one's softmax gain 1% where they have the registers.  Prompts of 2048 tokens (54 us, 630 TFLOP/s) wait for their
+// this one's softmax gain 1% where they have the registers.  Prompts of 2048 tokens (51 us, 670 TFLOP/s) wait for their
 // longest workgroups, a step of which takes 1.2 us without others beside it.  fp32: the matrix units (8192 tokens 140
 // TFLOP/s of 154).
+#include <algorithm>
+
 #include "parts.h"
 #include "rows_kernels.h"
 
@@ -108,7 +110,7 @@ __device__ __forceinline__ float pair_sum(float x) {
 // 57.3, 8191 tokens 515 and 512, 24 prompts of up to 2000 tokens 360 and 341, 32768 tokens 7770 and 7600.)
 constexpr int keys_of(int D, bool F32, bool many) { return F32 || (many && D == 128) ? 32 : 64; }
 constexpr int per_cu(int D, bool F32, int keys) { return D == 64 ? 4 : F32 || keys == 64 ? 2 : 3; }
-constexpr int kManyGroups = 1024;
+constexpr int kManyGroups = 1024, kCus = 256;
 
 template <int D, bool F32, int KEYS>
 __global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(PromptParams P) {
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(256, per_cu(D, F32, KEYS)) void prompt_attn_kernel(
   const uint32_t y = P.by_hkv.div(blockIdx.x);
   const int head = (int)(blockIdx.x - y * P.hkv);
   const int split = P.splits > 1 ? (int)(y % (uint32_t)P.splits) : 0;
-  const int tile = P.tiles - 1 - (int)(P.splits > 1 ? y / (uint32_t)P.splits : y);
+  const int turn = (int)(P.splits > 1 ? y / (uint32_t)P.splits : y);
+  const int tile = turn < P.cut ? P.tiles - 1 - turn : turn - P.cut;
   // (lane i: the i-th of 64 sequences, everything about it in one trip to memory)
   int seq = -1, t0 = 0, t1 = 0, k0 = 0, K = 0;
   for (int s0 = 0; s0 < P.batch; s0 += 64) {
@@ -432,6 +435,11 @@ hipError_t launch(PromptParams P, hipStream_t s) {
   P.by_hkv.set((uint32_t)P.hkv);
   P.tiles = (int)(((int64_t)P.n_tokens << P.g_shift) / kPromptRows) + P.batch;
   const dim3 grid((unsigned)((int64_t)P.tiles * P.hkv * P.splits));
+  // Workgroups w and w + 256 share a CU where all of a call's run at once: the first 256 go from the longest on down, the
+  // others from the shortest on up (us, 2048 tokens 52 and 50.5, in fp32 369 and 281, two prompts of 1000 tokens 34.5 and 29;
+  // with more workgroups, which take the place of those that end, the longest go first: 2600 tokens 69 and 73).
+  const bool at_once = ((int64_t)P.n_tokens << P.g_shift) / kPromptRows * P.hkv <= 2 * kCus;
+  P.cut = P.splits == 1 && at_once ? std::max(kCus / P.hkv, 1) : P.tiles;
   constexpr int few = keys_of(D, F32, false), many = keys_of(D, F32, true);
   if (few == many || grid.x <= kManyGroups)
     hipLaunchKernelGGL((prompt_attn_kernel<D, F32, few>), grid, dim3(256), 0, s, P);

@@ -24,6 +24,7 @@ struct PromptParams {
   float* ws;                   // records [splits][n_tokens][hq][d + 4]
   float scale_log2;
   int n_tokens, batch, hq, hkv, g_shift, rows, d, splits, tiles;
+  int cut;                     // tiles of query rows that are taken from the last on, the others from the first on
   bool bf16;
 };
 
