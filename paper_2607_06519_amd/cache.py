@@ -438,6 +438,8 @@ class PagedCache:
         """Stores the new rows ``k`` / ``v [n][Hkv][d]`` of ``layer`` and returns the attention of ``q [n][Hq][d]`` over them
         and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held.)"""
         torch = _torch()
+        if rows is not self._open:
+            raise RuntimeError("not the rows that have begun")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if rows.n == 0:
@@ -476,8 +478,15 @@ class PagedCache:
         self.pos.copy_(now[0])
         self.lens.copy_(now[1])
 
+    def _in_step(self):
+        """Positions and lengths on the device are those of the last step until the next one begins.  (A graph may be
+        captured at any time.)"""
+        if self._open is not True and not _torch().cuda.is_current_stream_capturing():
+            raise RuntimeError("no step has begun")
+
     def append(self, layer: int, k_new, v_new):
         """This step's K / V rows ``[batch][Hkv][d]`` of ``layer`` (those of sequences that are not active are passed over)."""
+        self._in_step()
         B.page_write(self.dims, self.pools[layer], k_new, v_new, None, self.pos)
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, prefix: Optional[CompressedCache] = None):
@@ -494,6 +503,8 @@ class PagedCache:
         if prefix is not None:
             if prefix.batch != self.batch or not _same_cache(prefix.dims, self.dims) or prefix.dims.n_q_heads != self.dims.n_q_heads:
                 raise ValueError("a prefix of another batch, other dimensions, or compressed another way")
+        self._in_step()
+        if prefix is not None:
             if prefix.max_seq_len:
                 B.decode_partial(prefix.dims, self.batch, prefix.seq_lens, prefix.max_seq_len, prefix.modes, prefix.offsets,
                                  prefix.buf, layer, q, scale, prefix.ws)
@@ -514,6 +525,7 @@ class PagedCache:
     def read(self, layer: int, seq: int):
         """K and V rows ``[Hkv][T][d]`` of a sequence, as held."""
         torch = _torch()
+        seq = range(self.batch)[seq]                        # (a token of sequence -1 is of none)
         T, dev = self.lens_host[seq], self.table.device
         k, v = (torch.empty((self.dims.n_kv_heads, T, self.dims.head_dim), dtype=_input_dtype(self.dims), device=dev) for _ in range(2))
         if T:

@@ -230,3 +230,33 @@ def test_behind_a_prefix_and_into_compression(torch_dev, dtype):
         torch.cuda.synchronize()
         bufs.append(c.host_bytes())
     assert np.array_equal(*bufs)
+
+
+def test_calls_out_of_turn(torch_dev):
+    """Rows and layers of a step that has ended, or of another cache, change nothing."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    from paper_2607_06519_amd.cache import PagedCache
+    dims = B.dims(2, 1, 1, 64, 0, "bf16")
+    cache, other = (PagedCache(dims, 2, 64, page=16) for _ in range(2))
+    x = torch.ones(3, 1, 64, dtype=torch.bfloat16, device="cuda")
+    rows, theirs = cache.begin([0, 3]), other.begin([3, 0])
+    with pytest.raises(RuntimeError, match="not the rows"):
+        cache.prompt(theirs, 0, x, x, x)
+    cache.prompt(rows, 0, x, x, x)
+    cache.end(rows)
+    late = [lambda: cache.prompt(rows, 0, x, -x, -x), lambda: cache.append(0, -x[:2], -x[:2]), lambda: cache.decode(0, x[:2])]
+    for bad in late:
+        with pytest.raises(RuntimeError):
+            bad()
+    cache.begin_step()
+    cache.append(0, 2 * x[:2], 2 * x[:2])
+    cache.advance()
+    for bad in late:
+        with pytest.raises(RuntimeError):
+            bad()
+    want = torch.tensor([1.0, 1.0, 1.0, 2.0]).view(1, 4, 1).expand(1, 4, 64).double().numpy()
+    for seq in (1, -1):                                          # (counted from the last one on, too)
+        assert all(np.array_equal(num(y), want) for y in cache.read(0, seq))
+    with pytest.raises(IndexError):
+        cache.read(0, 2)
