@@ -571,11 +571,13 @@ fdkv_status fdkv_prompt_attn_workspace(const fdkv_dims* dims, int32_t n_tokens, 
  *   k_lens     device int32 [batch], K_s
  *   out        device [n_tokens][Hq][d], apart from every input (q itself where q_stride is Hq * d: in place)
  *   ws         device workspace of fdkv_prompt_attn_workspace() bytes (FDKV_E_WORKSPACE if smaller; NULL if 0)
- * Strides are multiples of 16 bytes and at most 2^35 elements, rows' below 2^24 bytes (FDKV_E_UNSUPPORTED otherwise).  Numbers
+ * Strides are multiples of 16 bytes and at most 2^35 elements (FDKV_E_INVALID_ARG otherwise), rows' below 2^24 bytes
+ * (FDKV_E_UNSUPPORTED).  Numbers
  * of q_starts, k_starts and k_lens outside of their ranges are taken as the nearest in them.
  * Rows that no sequence names are not used, whatever they hold; a value row that is
  * not finite may reach up to 63 tokens before its own.  Probabilities of bf16 calls are rounded
- * to bf16 for their product with V, their sum is not.  The order of fp32 sums depends on n_tokens,
+ * to bf16 for their product with V, their sum is not.  Sums over values are held at up to 2^8 of their
+ * softmax's scale: values of more than 2^119 / K_s may leave fp32.  The order of fp32 sums depends on n_tokens,
  * batch, rows and the place of a token in its sequence; the same call gives the same bits.
  */
 fdkv_status fdkv_prompt_attn(const fdkv_dims* dims, int32_t n_tokens, const void* q, int64_t q_stride, int32_t batch,
@@ -607,7 +609,7 @@ typedef struct {
  * pages, and back (exactly what is held; an FP8 row's codes times 2^e).
  *   n_tokens   rows of the call per head, >= 0; ceil(n_tokens / 8) x Hkv <= 2^22 (FDKV_E_UNSUPPORTED otherwise)
  *   k, v       device; head h of token i is at strides[0] i + strides[1] h elements (host int64 [2] each, >= 0,
- *              at most 2^35, multiples of 16 bytes; rows that are written do not overlap)
+ *              at most 2^35, multiples of 16 bytes: FDKV_E_INVALID_ARG otherwise; rows that are written do not overlap)
  *   seqs       device int32 [n_tokens], the sequence of each token; NULL: token i is of sequence i
  *   rows       device int32 [n_tokens], the row of each token in its sequence
  * A token whose sequence is outside [0, batch), whose row is outside [0, max_pages * page)
@@ -639,7 +641,8 @@ fdkv_status fdkv_paged_attn_workspace(const fdkv_dims* dims, int32_t batch, int3
  *              FDKV_E_WORKSPACE otherwise)
  * At most 2^23 workgroups (batch x Hkv x the chunks of max_len) and 2^23 query rows (FDKV_E_UNSUPPORTED
  * otherwise).  Rows at or past T_s are not used, whatever they hold.  Probabilities are rounded to
- * the element type for their product with V, their sum is not.  The order of fp32 sums
+ * the element type for their product with V, their sum is not.  Sums over values are held at
+ * up to 2^8 of their softmax's scale: values of more than 2^119 / T_s may leave fp32.  The order of fp32 sums
  * depends on batch, max_len and n_more; the same call gives the same bits.
  */
 fdkv_status fdkv_paged_attn(const fdkv_dims* dims, const fdkv_pages* pages, const int32_t* lens, int32_t max_len,

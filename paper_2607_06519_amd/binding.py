@@ -574,9 +574,10 @@ def prompt_attn(d: Dims, q, k, v, q_starts, k_lens, out, sm_scale: float, ws, k_
         raise ValueError(f"prompt_attn: q, k, v and out are {e}, all on the current device (cuda:{at})")
     numbers = [(q_starts, batch + 1), (k_lens, batch)] + ([] if k_starts is None else [(k_starts, batch)])
     _operands("prompt_attn", e, (), numbers, ws)
-    ks, vs = (_Strides3(t.stride(0) if seqs > 1 else 0, t.stride(1), t.stride(2)) for t in (k, v))
+    # (the stride of an axis of one can be anything: it is not used)
+    ks, vs = (_Strides3(t.stride(0) if seqs > 1 else 0, t.stride(1) if hkv > 1 else 0, t.stride(2) if rows > 1 else 0) for t in (k, v))
     st = (_lib or load()).fdkv_prompt_attn(
-        ctypes.byref(d), n, q.data_ptr(), q.stride(0), batch, q_starts.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, rows,
+        ctypes.byref(d), n, q.data_ptr(), q.stride(0) if n > 1 else 0, batch, q_starts.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, rows,
         _dev(k_starts), k_lens.data_ptr(), out.data_ptr(), sm_scale, _dev(ws),
         0 if ws is None else ws.numel() * ws.element_size(),
         torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
@@ -635,6 +636,10 @@ def _page_rows(what: str, d: Dims, p: Pages, k, v, seqs, rows, stream, written: 
         raise ValueError(f"{what}: k and v are {e}, all on the current device (cuda:{at})")
     if written and ((n > 1 and (k0 < hd or v0 < hd)) or (d.n_kv_heads > 1 and (k1 < hd or v1 < hd))):
         raise ValueError(f"{what}: rows that overlap")
+    if n == 1:                                              # (the stride of an axis of one can be anything)
+        k0 = v0 = 0
+    if d.n_kv_heads == 1:
+        k1 = v1 = 0
     if rows.dtype is not i32 or not rows.is_contiguous() or \
             (seqs is not None and (seqs.dtype is not i32 or seqs.shape != (n,) or not seqs.is_contiguous() or seqs.get_device() != at)):
         raise ValueError(f"{what}: seqs and rows are contiguous int32 [n] on cuda:{at}")

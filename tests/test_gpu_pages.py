@@ -115,3 +115,22 @@ def test_values_that_are_not_finite(torch_dev):
         t = t.cpu()
         assert t[0, 0, 3].isnan() and t[1, 0, 5].isnan()
         assert (t[0, 0, [i for i in range(64) if i != 3]] == 1).all()
+
+
+def test_strides_of_one(torch_dev):
+    """One token, one head, one row: whatever the stride of that axis is."""
+    torch = torch_dev
+    from paper_2607_06519_amd import binding as B
+    d, odd = 64, 2 ** 36 + 3
+    dims = B.dims(2, 1, 4, d, 0, "bf16")
+    pool = Pool(torch, dims, "bf16", 16, [1])
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    x, y, back = (torch.full((d,), f, dtype=torch.bfloat16, device="cuda") for f in (2.0, 3.0, 0.0))
+    one = lambda t, *strides: t.as_strided((1,) * len(strides) + (d,), strides + (1,))
+    B.page_write(dims, pool.desc, one(x, odd, odd), one(y, odd, d), i32(0), i32(0))
+    B.page_read(dims, pool.desc, one(back, odd, odd), torch.empty(1, 1, d, dtype=torch.bfloat16, device="cuda"), i32(0), i32(0))
+    q = torch.randn(4 * d, device="cuda").to(torch.bfloat16).as_strided((1, 4, d), (odd, d, 1))
+    out = torch.empty(1, 4, d, dtype=torch.bfloat16, device="cuda")
+    B.prompt_attn(dims, q, one(x, odd, odd, odd), one(y, odd, odd, odd), i32(0, 1), i32(1), out, 0.125,
+                  torch.empty(max(1, B.prompt_attn_workspace(dims, 1, 1, 1)), dtype=torch.uint8, device="cuda"))
+    assert (back == 2).all() and (out == 3).all()
