@@ -25,7 +25,8 @@
 // library's product reaches 1.79.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
 // tokens, now 517); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
 // groups of waves that take turns at the matrix units wait for their operands (8.7), the next tile's logits ahead of
-// this one's softmax gain 1% where they have the registers.  Prompts of 2048 tokens (51 us, 670 TFLOP/s) wait for their
+// this one's softmax gain 1% where they have the registers, and three or four tiles in LDS instead of two gain nothing
+// (32768 tokens 7.78 to 8.23 for 7.81, 2048 tokens 57 to 66 us for 51).  Prompts of 2048 tokens (51 us, 670 TFLOP/s) wait for their
 // longest workgroups, a step of which takes 1.2 us without others beside it.  fp32: the matrix units (8192 tokens 140
 // TFLOP/s of 154).
 #include <algorithm>
