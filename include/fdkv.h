@@ -589,8 +589,9 @@ fdkv_status fdkv_prompt_attn(const fdkv_dims* dims, int32_t n_tokens, const void
  * Pages: row r of sequence s is slot r % page of page table[s][r / page] of a
  * layer's pool.  A table entry outside [0, n_pages) names no page.  Rows have the
  * type of the dims; FDKV_BF16_E4M3: a row x is held as E4M3 codes of x 2^-e with the
- * least e for which max |x_i| <= 448 2^e (at least -126), and the byte e + 127.
- * A value that is not finite is held as NaN; one of at least 2^128 - 2^123 as 2^128, which reads as infinite.
+ * least e for which the largest finite |x_i| <= 448 2^e (at least -126), and the byte e + 127.
+ * A value that is not finite is held as NaN, and the row's others as if it were not there; one of at least
+ * 2^128 - 2^123 is held as 2^128, which reads as infinite.
  */
 typedef struct {
   int32_t n_pages;         /* pages of the pool, >= 1 */

@@ -3,7 +3,7 @@
 //
 // Row r of sequence s is slot r % page of page table[s][r / page], K and V
 // [n_pages][hkv][page][d].  An FP8 row x is held as E4M3 codes c and one exponent:
-//   e = the least with max |x_i| <= 448 2^e,   c_i = e4m3(x_i 2^-e),
+//   e = the least with max |x_i| <= 448 2^e over the finite x_i,   c_i = e4m3(x_i 2^-e),
 // so that a row's values keep four significant bits (a power of two costs an
 // E4M3 value nothing but range: the smallest values lose at most one of its 18
 // binades) and the way back, c_i 2^e, is exact in bf16.  With 448 = 7/8 2^9 and
@@ -79,16 +79,16 @@ __global__ __launch_bounds__(kThreads) void page_rows_kernel(PageRowsParams P) {
     uint8_t* exps = is_v ? P.pg.v_exp : P.pg.k_exp;
     if constexpr (WRITE) {
       const uint32_t x[8] = {w.x, w.y, w.z, w.w, w2.x, w2.y, w2.z, w2.w};
-      // bf16 magnitudes compare as their bits; what is not a number is left out (and stored as such)
+      // bf16 magnitudes compare as their bits; what is not finite is left out (and held as NaN)
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t lo = x[i] & 0x7FFFu, hi = (x[i] >> 16) & 0x7FFFu;
-        top = max(top, max(lo > 0x7F80u ? 0u : lo, hi > 0x7F80u ? 0u : hi));
+        top = max(top, max(lo >= 0x7F80u ? 0u : lo, hi >= 0x7F80u ? 0u : hi));
       }
       top = group_max<LPR>(top);
       // top = m 2^k, k + 127 its exponent bits; m > 7/4: fraction bits above 1100000
-      const int b = max((int)(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0), 1);  // 1 .. 248
+      const int b = max((int)(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0), 1);  // 1 .. 247
       const float f = as_f32((uint32_t)(254 - b) << 23);                            // 2^-(b - 127)
       uint32_t c[4];
 #pragma unroll
