@@ -440,6 +440,10 @@ class PagedCache:
         torch = _torch()
         if rows is not self._open:
             raise RuntimeError("not the rows that have begun")
+        d = self.dims
+        if q.shape != (rows.n, d.n_q_heads, d.head_dim) or (out is not None and out.shape != q.shape) or \
+                not k.shape == v.shape == (rows.n, d.n_kv_heads, d.head_dim):
+            raise ValueError(f"q and out are [{rows.n}][Hq][d], k and v [{rows.n}][Hkv][d]: the rows that have begun")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if rows.n == 0:

@@ -1,0 +1,54 @@
+"""PagedCache on the host: which calls it refuses and what they leave.  The library's device calls are replaced by stubs;
+everything else is the class's own code on CPU tensors."""
+import os
+
+import pytest
+
+from paper_2607_06519_amd import binding as B
+from paper_2607_06519_amd import cache as C
+
+DIMS = B.dims(2, 2, 8, 128, 0, "bf16")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    import torch
+    if not os.path.exists(B._LIB_PATH):
+        pytest.skip("libfdkv.so not built")
+    seen = []
+    monkeypatch.setattr(C, "_torch", lambda: torch)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    for name in ("page_write", "page_read", "prompt_attn", "paged_attn", "decode_partial"):
+        monkeypatch.setattr(C.B, name, lambda *a, _name=name, **k: seen.append((_name, a)))
+    return seen
+
+
+def _cache(batch=2, max_len=100, dims=DIMS, **o):
+    return C.PagedCache(dims, batch, max_len, page=16, device="cpu", **o)
+
+
+def _rows(n, heads, dtype=None):
+    import torch
+    return torch.zeros(n, heads, 128, dtype=dtype or torch.bfloat16)
+
+
+def test_a_prompt_of_other_rows_is_refused(calls):
+    """Queries, keys, values and outputs are those of the rows that have begun; a call that is refused stores nothing."""
+    import torch
+    c = _cache()
+    rows = c.begin([5, 2])
+    good = dict(q=_rows(7, 8), k=_rows(7, 2), v=_rows(7, 2))
+    for bad in (dict(q=_rows(6, 8)), dict(q=_rows(8, 8)), dict(q=_rows(0, 8)), dict(q=_rows(7, 4)), dict(q=_rows(7, 8)[..., :64]), dict(k=_rows(6, 2)),
+                dict(k=_rows(7, 8)), dict(v=_rows(8, 2)), dict(v=_rows(7, 1)), dict(q=_rows(7, 8).flatten(1)), dict(out=_rows(6, 8)), dict(out=_rows(8, 8))):
+        with pytest.raises(ValueError):
+            c.prompt(rows, 0, **{**good, **bad})
+    assert not calls
+    c.prompt(rows, 0, **good)
+    c.prompt(rows, 1, **good, out=torch.empty_like(good["q"]))
+    assert [x[0] for x in calls] == ["page_write", "prompt_attn"] * 2
+    c.end(rows)
+    none = c.begin([0, 0])
+    for bad in (dict(q=_rows(1, 8)), dict(k=_rows(1, 2)), dict(out=_rows(1, 8))):
+        with pytest.raises(ValueError):
+            c.prompt(none, 0, **{**dict(q=_rows(0, 8), k=_rows(0, 2), v=_rows(0, 2)), **bad})
+    assert c.prompt(none, 0, _rows(0, 8), _rows(0, 2), _rows(0, 2)).shape == (0, 8, 128)
