@@ -369,9 +369,8 @@ class PagedCache:
         self._ws = torch.empty(B.paged_attn_workspace(dims, self.batch, self.max_len) // 4 + 64, dtype=torch.float32,
                                device=device)
 
-    def _take(self, counts):
-        """Pages for ``counts[s]`` more rows of each sequence; none are taken where not all fit."""
-        torch = _torch()
+    def _room(self, counts):
+        """The pages that each sequence needs for ``counts[s]`` more rows, once it is sure that they can be had."""
         if self._open is not None:
             raise RuntimeError("end the rows, or advance the step, that have begun")
         if len(counts) != self.batch or min(counts) < 0:
@@ -381,12 +380,30 @@ class PagedCache:
             raise RuntimeError(f"a sequence holds {self.max_len} rows at most")
         if sum(max(0, w - len(h)) for w, h in zip(want, self.held)) > len(self.free):
             raise RuntimeError("the pool has no pages left: release sequences, or compress them")
-        for s, w in enumerate(want):
-            first = len(self.held[s])
-            if w > first:
-                new = [self.free.pop() for _ in range(w - first)]
-                self.held[s] += new
-                self.table[s, first:w] = torch.tensor(new, dtype=torch.int32).to(self.table.device)
+        return want
+
+    def _take(self, want):
+        """``want[s]`` pages for every sequence s, or none where that fails."""
+        torch = _torch()
+        try:
+            for s, w in enumerate(want):
+                first = len(self.held[s])
+                if w > first:
+                    new = [self.free.pop() for _ in range(w - first)]
+                    self.held[s] += new
+                    self.table[s, first:w] = torch.tensor(new, dtype=torch.int32).to(self.table.device)
+        except BaseException:
+            self._give_back()
+            raise
+
+    def _give_back(self):
+        """Pages behind the rows that their sequences hold are free."""
+        for s in reversed(range(self.batch)):               # (the order that they were taken in, backwards)
+            keep = -(-self.lens_host[s] // self.page)
+            if len(self.held[s]) > keep:
+                self.free += reversed(self.held[s][keep:])
+                del self.held[s][keep:]
+                self.table[s, keep:].fill_(-1)
 
     def release(self, seq: int):
         """Sequence ``seq`` ends: its pages are free, it holds no rows."""
@@ -406,7 +423,7 @@ class PagedCache:
         that follow) and returns what ``prompt`` needs to know of them."""
         torch = _torch()
         counts = [int(c) for c in counts]
-        self._take(counts)
+        want = self._room(counts)
 
         class Rows:
             pass
@@ -431,6 +448,7 @@ class PagedCache:
             r.new_at = torch.from_numpy(spans(firsts[:-1] + past, new).astype(np.int64)).to(dev)
         n = B.prompt_attn_workspace(self.dims, r.n, len(part), r.total) if r.n else 0
         r.ws = torch.empty(n // 4 + 64, dtype=torch.float32, device=dev)
+        self._take(want)
         self._open = r
         return r
 
@@ -475,10 +493,11 @@ class PagedCache:
         """A step of the ``active`` sequences (default: those that hold rows) begins: each takes a row."""
         torch = _torch()
         active = [n > 0 for n in self.lens_host] if active is None else [bool(a) for a in active]
-        self._take([int(a) for a in active])
-        self._open, self.active = True, active
+        want = self._room([int(a) for a in active])
         now = torch.tensor([[n if a else -1 for n, a in zip(self.lens_host, active)],
                             [n + 1 if a else 0 for n, a in zip(self.lens_host, active)]], dtype=torch.int32).to(self.pos.device)
+        self._take(want)
+        self._open, self.active = True, active
         self.pos.copy_(now[0])
         self.lens.copy_(now[1])
 

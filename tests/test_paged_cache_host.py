@@ -52,3 +52,37 @@ def test_a_prompt_of_other_rows_is_refused(calls):
         with pytest.raises(ValueError):
             c.prompt(none, 0, **{**dict(q=_rows(0, 8), k=_rows(0, 2), v=_rows(0, 2)), **bad})
     assert c.prompt(none, 0, _rows(0, 8), _rows(0, 2), _rows(0, 2)).shape == (0, 8, 128)
+
+
+def test_rows_that_cannot_begin_take_no_pages(calls, monkeypatch):
+    """A begin that is refused, or fails on its way, leaves the pages where they were."""
+    import torch
+    c = _cache(2, 1000)
+    rows = c.begin([40, 3])
+    c.end(rows)
+    free, table = list(c.free), c.table.clone()
+
+    def unchanged():
+        assert c.free == free and [len(h) for h in c.held] == [3, 1] and torch.equal(c.table, table) and c.lens_host == [40, 3]
+
+    def refuse(*a):
+        raise B.FdkvError(-2, "fdkv_prompt_attn_workspace")
+    with monkeypatch.context() as m:
+        m.setattr(C.B, "prompt_attn_workspace", refuse)
+        with pytest.raises(B.FdkvError):
+            c.begin([500, 0])
+    unchanged()
+    make, made = torch.tensor, []
+
+    def second(*a, **k):                                     # the second sequence's pages cannot be put into the table
+        made.append(a)
+        if len(made) == 2:
+            raise MemoryError
+        return make(*a, **k)
+    with monkeypatch.context() as m:
+        m.setattr(torch, "tensor", second)
+        with pytest.raises(MemoryError):
+            c.begin([30, 30])
+    unchanged()
+    c.end(c.begin([500, 60]))
+    assert sorted(c.free + c.held[0] + c.held[1]) == list(range(c.n_pages)) and c.lens_host == [540, 63]
