@@ -36,6 +36,7 @@ RES_CHANNELS, RES_TOKENS = 0, 1  # residual kinds (fdkv_residual)
 PART_OWN, PART_BLOCKS, PART_SHARED = 0, 1, 2  # parts of a decode step (fdkv_part_kind)
 BLOCK_TOKENS = 64                # tokens of a block of sparse decode (FDKV_BLOCK_TOKENS)
 DECODE_CHUNK = 512               # tokens of a record of fdkv_decode_partial
+MAX_PAGE_GROUPS = 1 << 22        # of fdkv_page_write and fdkv_page_read: ceil(n_tokens / 8) x Hkv
 MAX_SELECTED, MAX_SELECT_UNITS = 1 << 24, 65535  # of fdkv_block_select: n_sel, and batch x Hkv
 
 

@@ -417,6 +417,16 @@ class PagedCache:
         self.pos[seq].fill_(-1)
         self.lens[seq].fill_(0)
 
+    def _pass(self, call, layer: int, k, v, seqs, rows):
+        """``call``, page_write or page_read, over as many rows at a time as it takes."""
+        most = max(1, B.MAX_PAGE_GROUPS // self.dims.n_kv_heads) * 8
+        if len(rows) <= most:
+            call(self.dims, self.pools[layer], k, v, seqs, rows)
+            return
+        for a in range(0, len(rows), most):
+            at = slice(a, a + most)
+            call(self.dims, self.pools[layer], k[at], v[at], seqs[at], rows[at])
+
     # ------------------------------------------------------------ prompts
     def begin(self, counts: Sequence[int]):
         """Takes pages for ``counts[s]`` new tokens of every sequence (packed in the order of the sequences in the calls
@@ -466,13 +476,13 @@ class PagedCache:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if rows.n == 0:
             return out
-        pages, scale = self.pools[layer], 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
-        B.page_write(self.dims, pages, k, v, rows.seqs, rows.rows)
+        scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale
+        self._pass(B.page_write, layer, k, v, rows.seqs, rows.rows)
         keys = k.transpose(0, 1)[None], v.transpose(0, 1)[None]
         if rows.earlier:
             shape = (self.dims.n_kv_heads, rows.total, self.dims.head_dim)
             keys = [torch.empty(shape, dtype=k.dtype, device=k.device) for _ in range(2)]
-            B.page_read(self.dims, pages, *(x.transpose(0, 1) for x in keys), rows.all_seqs, rows.all_rows)
+            self._pass(B.page_read, layer, *(x.transpose(0, 1) for x in keys), rows.all_seqs, rows.all_rows)
             if self.dims.dtype == B.BF16_E4M3:
                 for both, given in zip(keys, (k, v)):
                     both[:, rows.new_at] = given.transpose(0, 1)
@@ -553,5 +563,5 @@ class PagedCache:
         k, v = (torch.empty((self.dims.n_kv_heads, T, self.dims.head_dim), dtype=_input_dtype(self.dims), device=dev) for _ in range(2))
         if T:
             rows = torch.arange(T, dtype=torch.int32, device=dev)
-            B.page_read(self.dims, self.pools[layer], k.transpose(0, 1), v.transpose(0, 1), torch.full_like(rows, seq), rows)
+            self._pass(B.page_read, layer, k.transpose(0, 1), v.transpose(0, 1), torch.full_like(rows, seq), rows)
         return k, v

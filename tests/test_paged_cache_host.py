@@ -86,3 +86,38 @@ def test_rows_that_cannot_begin_take_no_pages(calls, monkeypatch):
     unchanged()
     c.end(c.begin([500, 60]))
     assert sorted(c.free + c.held[0] + c.held[1]) == list(range(c.n_pages)) and c.lens_host == [540, 63]
+
+
+def test_more_rows_than_a_call_takes(calls, monkeypatch):
+    """A prompt's rows are stored, and earlier ones gathered, in calls of as many rows as one takes."""
+    monkeypatch.setattr(C.B, "MAX_PAGE_GROUPS", 4, raising=False)   # 16 rows of two heads
+    c = _cache(2, 1000)
+    for counts in ([33, 0], [7, 10]):
+        rows = c.begin(counts)
+        n = sum(counts)
+        calls.clear()
+        c.prompt(rows, 1, _rows(n, 8), _rows(n, 2), _rows(n, 2))
+        for name, total, heads_first in (("page_write", n, False), ("page_read", 50, True)):
+            mine = [a for x, a in calls if x == name]
+            if name == "page_read" and counts[0] == 33:
+                assert not mine
+                continue
+            assert [len(a[5]) for a in mine] == [16] * (total // 16) + [total % 16]
+            assert all(a[2].shape == a[3].shape == (len(a[5]), 2, 128) and len(a[4]) == len(a[5]) and a[1] is c.pools[1] for a in mine)
+            if heads_first:
+                assert [int(r) for a in mine for r in a[5]] == [*range(40), *range(10)]
+                base = mine[0][2].data_ptr()
+                assert [a[2].data_ptr() - base for a in mine] == [2 * 128 * 16 * i for i in range(len(mine))]
+        c.end(rows)
+    calls.clear()
+    k, v = c.read(0, 0)
+    assert k.shape == v.shape == (2, 40, 128) and [len(a[5]) for _, a in calls] == [16, 16, 8]
+    dims = B.dims(2, 8, 8, 128, 0, "bf16")                    # the limit is the library's
+    import ctypes
+    two = (ctypes.c_int64 * 2)(1024, 128)
+    pages = B.Pages(1, 16, 1, 1, 1 << 20, 1 << 20, 1 << 20, None, None)
+    monkeypatch.undo()
+    most = B.MAX_PAGE_GROUPS // 8 * 8
+    lib = B.load()
+    for n, status in ((most + 1, -2), (most, -1)):            # (no rows' addresses: refused for that alone)
+        assert lib.fdkv_page_read(ctypes.byref(dims), ctypes.byref(pages), n, None, two, None, two, None, None, None) == status
