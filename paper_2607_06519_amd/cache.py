@@ -331,7 +331,8 @@ class PagedCache:
     rows too), and ``end(rows)`` makes them part of the sequences.  A decode step:
     ``begin_step()`` takes a row for each active sequence, ``append(layer, k, v)``
     and ``decode(layer, q)`` store and attend layer by layer, ``advance()`` ends
-    it.  ``read`` gives a sequence's rows back as ``probe`` and
+    it.  ``cancel()`` gives up what has begun, a prompt's rows or a step, whatever
+    calls of it were made or failed, and leaves the sequences as they were.  ``read`` gives a sequence's rows back as ``probe`` and
     ``CompressedCache.compress`` take them, and ``release`` its pages to others.
     ``decode(..., prefix=cache)`` also attends over a compressed prefix that the
     paged rows continue.
@@ -372,7 +373,7 @@ class PagedCache:
     def _room(self, counts):
         """The pages that each sequence needs for ``counts[s]`` more rows, once it is sure that they can be had."""
         if self._open is not None:
-            raise RuntimeError("end the rows, or advance the step, that have begun")
+            raise RuntimeError("end the rows, or advance the step, that have begun (or cancel)")
         if len(counts) != self.batch or min(counts) < 0:
             raise ValueError("a number of new rows for each sequence")
         want = [-(-(n + c) // self.page) for n, c in zip(self.lens_host, counts)]
@@ -408,7 +409,7 @@ class PagedCache:
     def release(self, seq: int):
         """Sequence ``seq`` ends: its pages are free, it holds no rows."""
         if self._open is not None:
-            raise RuntimeError("end the rows, or advance the step, that have begun")
+            raise RuntimeError("end the rows, or advance the step, that have begun (or cancel)")
         self.free += reversed(self.held[seq])
         self.held[seq] = []
         self.lens_host[seq] = 0
@@ -553,6 +554,17 @@ class PagedCache:
         for s, a in enumerate(self.active):
             self.lens_host[s] += int(a)
         self.active = [False] * self.batch
+
+    def cancel(self):
+        """What has begun, a prompt's rows or a step, is given up: the sequences hold what they held before it."""
+        if self._open is None:
+            raise RuntimeError("nothing has begun")
+        if self._open is True:                              # (a step that is replayed now writes no row)
+            self.pos.fill_(-1)
+            self.lens.fill_(0)
+        self._open = None
+        self.active = [False] * self.batch
+        self._give_back()
 
     # ------------------------------------------------------------ rows back
     def read(self, layer: int, seq: int):

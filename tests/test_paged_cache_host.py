@@ -121,3 +121,37 @@ def test_more_rows_than_a_call_takes(calls, monkeypatch):
     lib = B.load()
     for n, status in ((most + 1, -2), (most, -1)):            # (no rows' addresses: refused for that alone)
         assert lib.fdkv_page_read(ctypes.byref(dims), ctypes.byref(pages), n, None, two, None, two, None, None, None) == status
+
+
+def test_cancelled_rows_and_steps(calls):
+    """What has begun can be given up, and leaves the sequences, the pages and the table as they were."""
+    import torch
+    c = _cache(3, 100, n_pages=13)
+    with pytest.raises(RuntimeError):
+        c.cancel()
+    c.end(c.begin([40, 16, 0]))
+    free, table = list(c.free), c.table.clone()
+
+    def unchanged():
+        assert c.free == free and [len(h) for h in c.held] == [3, 1, 0] and c.lens_host == [40, 16, 0] and torch.equal(c.table, table)
+        assert c._open is None and c.active == [False] * 3
+    rows = c.begin([30, 20, 50])
+    calls.clear()
+    c.prompt(rows, 0, _rows(100, 8), _rows(100, 2), _rows(100, 2))
+    c.cancel()
+    unchanged()
+    for late in (lambda: c.prompt(rows, 1, _rows(100, 8), _rows(100, 2), _rows(100, 2)), lambda: c.end(rows), c.cancel):
+        with pytest.raises(RuntimeError):
+            late()
+    c.begin_step([True, True, True])
+    assert c.pos.tolist() == [40, 16, 0] and len(c.held[1]) == 2
+    c.append(0, _rows(3, 2), _rows(3, 2))
+    c.cancel()
+    unchanged()
+    assert c.pos.tolist() == [-1] * 3 and c.lens.tolist() == [0] * 3
+    for late in (c.advance, lambda: c.append(1, _rows(3, 2), _rows(3, 2)), lambda: c.decode(1, _rows(3, 8))):
+        with pytest.raises(RuntimeError):
+            late()
+    c.release(0)
+    c.end(c.begin([1, 80, 90]))
+    assert sorted(c.free + sum(c.held, [])) == list(range(13)) and c.lens_host == [1, 96, 90]
