@@ -335,7 +335,8 @@ class PagedCache:
     calls of it were made or failed, and leaves the sequences as they were.  ``read`` gives a sequence's rows back as ``probe`` and
     ``CompressedCache.compress`` take them, and ``release`` its pages to others.
     ``decode(..., prefix=cache)`` also attends over a compressed prefix that the
-    paged rows continue.
+    paged rows continue; ``begin_step(prefix=cache)`` then takes a row for the
+    sequences that hold tokens of it alone, too.
 
     ``append`` and ``decode`` of one step can be captured in a graph once and
     replayed every step between ``begin_step`` and ``advance``, which change the
@@ -364,6 +365,8 @@ class PagedCache:
         self.held = [[] for _ in range(self.batch)]         # pages of each sequence
         self.lens_host = [0] * self.batch                   # rows held before the current step
         self.active = [False] * self.batch
+        self._by_default = False                            # ... that hold rows, as none were named
+        self._captured = None                               # the prefix of a captured step
         self._open = None                                   # rows of begin (or True: a step) that have not ended
         self.pos = torch.full((self.batch,), -1, dtype=torch.int32, device=device)  # row that a step writes
         self.lens = torch.zeros(self.batch, dtype=torch.int32, device=device)       # rows that a step attends
@@ -465,7 +468,7 @@ class PagedCache:
 
     def prompt(self, rows, layer: int, q, k, v, out=None, sm_scale: Optional[float] = None):
         """Stores the new rows ``k`` / ``v [n][Hkv][d]`` of ``layer`` and returns the attention of ``q [n][Hq][d]`` over them
-        and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held.)"""
+        and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held; a compressed prefix takes no part.)"""
         torch = _torch()
         if rows is not self._open:
             raise RuntimeError("not the rows that have begun")
@@ -500,15 +503,36 @@ class PagedCache:
             self.lens_host[s] += c
 
     # ------------------------------------------------------------ steps
-    def begin_step(self, active: Optional[Sequence[bool]] = None):
-        """A step of the ``active`` sequences (default: those that hold rows) begins: each takes a row."""
+    def _check_prefix(self, prefix: CompressedCache):
+        if prefix.batch != self.batch or not _same_cache(prefix.dims, self.dims) or prefix.dims.n_q_heads != self.dims.n_q_heads:
+            raise ValueError("a prefix of another batch, other dimensions, or compressed another way")
+
+    def _check_active(self, prefix: CompressedCache, active):
+        """A sequence that holds tokens of the prefix alone may be at its first step, or at its end: it is not passed over
+        unless the caller says so."""
+        alone = [s for s, (t, a) in enumerate(zip(prefix.seq_lens_host, active)) if t and not a]
+        if alone:
+            raise RuntimeError(f"sequences {alone} hold tokens of the prefix alone: begin the step with it, or name the active ones")
+
+    def begin_step(self, active: Optional[Sequence[bool]] = None, prefix: Optional[CompressedCache] = None):
+        """A step of the ``active`` sequences begins: each takes a row.  Default: those that hold rows, or tokens of
+        ``prefix``, the compressed cache that the step's ``decode`` is called with."""
         torch = _torch()
-        active = [n > 0 for n in self.lens_host] if active is None else [bool(a) for a in active]
+        by_default = active is None
+        if prefix is not None:
+            self._check_prefix(prefix)
+        if by_default:
+            active = [n > 0 for n in self.lens_host]
+            if prefix is not None:
+                active = [a or t > 0 for a, t in zip(active, prefix.seq_lens_host)]
+            elif self._captured is not None:
+                self._check_active(self._captured, active)
+        active = [bool(a) for a in active]
         want = self._room([int(a) for a in active])
         now = torch.tensor([[n if a else -1 for n, a in zip(self.lens_host, active)],
                             [n + 1 if a else 0 for n, a in zip(self.lens_host, active)]], dtype=torch.int32).to(self.pos.device)
         self._take(want)
-        self._open, self.active = True, active
+        self._open, self.active, self._by_default = True, active, by_default
         self.pos.copy_(now[0])
         self.lens.copy_(now[1])
 
@@ -525,7 +549,7 @@ class PagedCache:
 
     def decode(self, layer: int, q, out=None, sm_scale: Optional[float] = None, prefix: Optional[CompressedCache] = None):
         """The step's attention ``[batch][Hq][d]`` of ``layer``: over every active sequence's paged rows, and the tokens of
-        ``prefix``, a compressed cache of the same batch (of sequences that are not active: over the prefix alone)."""
+        ``prefix``, a compressed cache of the same batch (of sequences that were not named active: over the prefix alone)."""
         torch = _torch()
         if out is None:
             out = torch.empty_like(q)
@@ -535,10 +559,13 @@ class PagedCache:
             most = min(most, -(-max(n + a for n, a in zip(self.lens_host, self.active)) // 256) * 256)
         more, n_more = None, 0
         if prefix is not None:
-            if prefix.batch != self.batch or not _same_cache(prefix.dims, self.dims) or prefix.dims.n_q_heads != self.dims.n_q_heads:
-                raise ValueError("a prefix of another batch, other dimensions, or compressed another way")
+            self._check_prefix(prefix)
         self._in_step()
         if prefix is not None:
+            if self._open is True and self._by_default:
+                self._check_active(prefix, self.active)
+            if torch.cuda.is_current_stream_capturing():
+                self._captured = prefix
             if prefix.max_seq_len:
                 B.decode_partial(prefix.dims, self.batch, prefix.seq_lens, prefix.max_seq_len, prefix.modes, prefix.offsets,
                                  prefix.buf, layer, q, scale, prefix.ws)

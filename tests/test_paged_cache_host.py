@@ -155,3 +155,49 @@ def test_cancelled_rows_and_steps(calls):
     c.release(0)
     c.end(c.begin([1, 80, 90]))
     assert sorted(c.free + sum(c.held, [])) == list(range(13)) and c.lens_host == [1, 96, 90]
+
+
+def _prefix(lens, dims=DIMS):
+    import numpy as np
+    return C.CompressedCache(dims, lens, np.zeros((len(lens), len(B.blocks(dims)[0]), dims.n_kv_heads), np.uint8), device="cpu")
+
+
+def test_the_first_step_behind_a_prefix(calls, monkeypatch):
+    """A sequence that holds tokens of the prefix and no rows is not passed over unless the caller says so."""
+    import torch
+    c, prefix = _cache(3, 100), _prefix([300, 0, 20])
+    q, kv = _rows(3, 8), _rows(3, 2)
+    c.begin_step()                                           # (no sequence holds a row)
+    with pytest.raises(RuntimeError, match="prefix"):
+        c.decode(0, q, prefix=prefix)
+    assert not calls
+    c.decode(0, q)                                           # without it there is nothing to pass over
+    c.cancel()
+    c.begin_step(prefix=prefix)
+    assert c.active == [True, False, True] and c.pos.tolist() == [0, -1, 0] and c.lens.tolist() == [1, 0, 1]
+    c.append(0, kv, kv)
+    c.decode(0, q, prefix=prefix)
+    c.advance()
+    c.begin_step()                                           # both hold a row now
+    c.decode(0, q, prefix=prefix)
+    c.advance()
+    c.release(2)
+    c.begin_step([True, False, False])                       # sequence 2 has ended: the caller says so
+    c.decode(0, q, prefix=prefix)
+    c.advance()
+    c.begin_step([True, False, False], prefix=prefix)
+    assert c.active == [True, False, False]
+    c.decode(0, q, prefix=prefix)
+    c.advance()
+    with pytest.raises(ValueError):
+        c.begin_step(prefix=_prefix([1, 2]))
+    assert c._open is None and c.lens_host == [4, 0, 0]
+    # a captured step reads its prefix at every replay
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    c.decode(0, q, prefix=prefix)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    with pytest.raises(RuntimeError, match="prefix"):
+        c.begin_step()
+    assert c._open is None and c.lens_host == [4, 0, 0]
+    c.begin_step(prefix=prefix)
+    assert c.active == [True, False, True]
