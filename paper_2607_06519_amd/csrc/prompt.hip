@@ -70,7 +70,7 @@ struct Prompt {
 // register to its use as an address, one from the write of m0 to a load to LDS.
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t to) {
-  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory");
+  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory", "m0");
 }
 template <int NL>
 __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t step, uint32_t to) {
@@ -80,7 +80,7 @@ __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t step
         "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds" ::"s"(to),
         "s"(to + 4096), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(step))
-        : "memory");
+        : "memory", "m0");
   else
     asm volatile(
         "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds\n\t"
@@ -89,7 +89,7 @@ __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t step
         "s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %8 offen lds" ::"s"(to),
         "s"(to + 4096), "s"(to + 8192), "s"(to + 12288), "v"(voff), "s"(r), "s"(__builtin_amdgcn_readfirstlane(step)),
         "s"(__builtin_amdgcn_readfirstlane(2 * step)), "s"(__builtin_amdgcn_readfirstlane(3 * step))
-        : "memory");
+        : "memory", "m0");
 }
 // A buffer of rows from `base` on (the callers stay within their rows).
 __device__ __forceinline__ u32x4_t buffer_at(const uint8_t* base) {
