@@ -574,8 +574,8 @@ fdkv_status fdkv_prompt_attn_workspace(const fdkv_dims* dims, int32_t n_tokens, 
  * Strides are multiples of 16 bytes and at most 2^35 elements (FDKV_E_INVALID_ARG otherwise), rows' below 2^24 bytes
  * (FDKV_E_UNSUPPORTED).  Numbers
  * of q_starts, k_starts and k_lens outside of their ranges are taken as the nearest in them.
- * Rows that no sequence names are not used, whatever they hold; a value row that is
- * not finite may reach up to 63 tokens before its own.  Probabilities of bf16 calls are rounded
+ * Rows that no sequence names are not used, nor are a token's rows by those before it, whatever they hold.
+ * Probabilities of bf16 calls are rounded
  * to bf16 for their product with V, their sum is not.  Sums over values are held at up to 2^8 of their
  * softmax's scale: values of more than 2^119 / K_s may leave fp32.  The order of fp32 sums depends on n_tokens,
  * batch, rows and the place of a token in its sequence; the same call gives the same bits.
