@@ -622,6 +622,14 @@ def _of_pages(what: str, d: Dims, p: Pages, at: int):
         raise ValueError(f"{what}: pages of other dims, or on another device than cuda:{at}")
 
 
+def _overlap(n: int, by_n: int, m: int, by_m: int, width: int) -> bool:
+    """Whether rows of ``width`` at the strides of two axes share values: the wider stride has to leave the other axis
+    behind."""
+    if n > 1 and m > 1:
+        return min(by_n, by_m) < width or (by_n < (m - 1) * by_m + width and by_m < (n - 1) * by_n + width)
+    return (n > 1 and by_n < width) or (m > 1 and by_m < width)
+
+
 def _page_rows(what: str, d: Dims, p: Pages, k, v, seqs, rows, stream, written: bool):
     # (checks without loops and calls of their own, as a call takes some 7 us)
     import torch
@@ -635,7 +643,7 @@ def _page_rows(what: str, d: Dims, p: Pages, k, v, seqs, rows, stream, written: 
         raise ValueError(f"{what}: k and v are [n][Hkv][d], channels contiguous")
     if not (e is k.dtype is v.dtype) or not (at == k.get_device() == v.get_device() == rows.get_device()):
         raise ValueError(f"{what}: k and v are {e}, all on the current device (cuda:{at})")
-    if written and ((n > 1 and (k0 < hd or v0 < hd)) or (d.n_kv_heads > 1 and (k1 < hd or v1 < hd))):
+    if written and (_overlap(n, k0, d.n_kv_heads, k1, hd) or _overlap(n, v0, d.n_kv_heads, v1, hd)):
         raise ValueError(f"{what}: rows that overlap")
     if n == 1:                                              # (the stride of an axis of one can be anything)
         k0 = v0 = 0
