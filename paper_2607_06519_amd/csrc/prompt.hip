@@ -69,6 +69,9 @@ struct Prompt {
 // landed.  Nor does it see what has to lie between: five wait states from a vector instruction's write of a scalar
 // register to its use as an address, one from the write of m0 to a load to LDS.
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+// (m0 is the compiler's own register: it warns that what it holds is lost, which is what the clobber is to tell it)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t to) {
   asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(r) : "memory", "m0");
 }
@@ -91,6 +94,7 @@ __device__ __forceinline__ void load_lds(u32x4_t r, uint32_t voff, uint32_t step
         "s"(__builtin_amdgcn_readfirstlane(2 * step)), "s"(__builtin_amdgcn_readfirstlane(3 * step))
         : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // A buffer of rows from `base` on (the callers stay within their rows).
 __device__ __forceinline__ u32x4_t buffer_at(const uint8_t* base) {
   const uint64_t a = (uint64_t)(uintptr_t)base;
