@@ -551,6 +551,8 @@ class PagedCache:
         """The step's attention ``[batch][Hq][d]`` of ``layer``: over every active sequence's paged rows, and the tokens of
         ``prefix``, a compressed cache of the same batch (of sequences that were not named active: over the prefix alone)."""
         torch = _torch()
+        if q.numel() != self.batch * self.dims.n_q_heads * self.dims.head_dim or (out is not None and out.numel() != q.numel()):
+            raise ValueError("decode: q and out are [batch][Hq][d]")
         if out is None:
             out = torch.empty_like(q)
         scale = 1.0 / math.sqrt(self.dims.head_dim) if sm_scale is None else sm_scale

@@ -201,3 +201,15 @@ def test_the_first_step_behind_a_prefix(calls, monkeypatch):
     assert c._open is None and c.lens_host == [4, 0, 0]
     c.begin_step(prefix=prefix)
     assert c.active == [True, False, True]
+
+
+def test_a_step_of_another_batch_is_refused(calls):
+    """Queries and outputs of more sequences than the cache's would keep rows that nothing writes."""
+    c = _cache(3, 100)
+    c.begin_step([True] * 3)
+    for bad in (dict(q=_rows(4, 8)), dict(q=_rows(2, 8)), dict(q=_rows(3, 4)), dict(q=_rows(3, 8), out=_rows(4, 8)), dict(q=_rows(3, 8), out=_rows(2, 8))):
+        with pytest.raises(ValueError):
+            c.decode(0, **bad)
+    assert not calls
+    assert c.decode(0, _rows(3, 8)).shape == (3, 8, 128) and [x[0] for x in calls] == ["paged_attn"]
+    assert c.decode(0, _rows(3, 8).flatten(1)).shape == (3, 1024)
