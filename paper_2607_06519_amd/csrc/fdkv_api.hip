@@ -1267,6 +1267,9 @@ int64_t prompt_tiles(const fdkv_dims* d, int64_t n, int batch) {
 // 26.1, 25.9, 64 tokens on 8000 keys 28.9, 26.7, 30.6, 45.0, one on 32000 33.6, 33.5, 33.8, 47.6; fp32, 64, 128, 256, 512: a
 // prompt of 128 tokens 20.4, 23.4, 23.6, 23.3, of 300 31.0, 30.3, 34.9, 46.9, 16 tokens on 4000 keys 33.2, 29.8, 43.0, 74.4.
 // fp32 fills the card twice, as its longest workgroups take longest: 1500 tokens 187, filled once 251.)
+// `rows` bounds one sequence's keys in a cache; of packed rows it is all sequences' together, and many short prompts are
+// split although most of their splits hold no keys (us, packed and in a cache of [batch][Hkv][cap][d]: 8 prompts of 50
+// tokens in fp32 34.6 and 16.4, 8 prompts of 300 on two KV heads in bf16 23.8 and 13.5).
 int prompt_splits(const fdkv_dims* d, int n, int batch, int rows) {
   const int64_t groups = prompt_tiles(d, n, batch) * d->n_kv_heads;
   const int64_t least = d->dtype == FDKV_F32 ? 64 : 1024;

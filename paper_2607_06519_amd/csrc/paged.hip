@@ -21,10 +21,11 @@
 // (2^-8 each at most) for the product, their sum is not.
 //
 // What bounds it: HBM, behind a start of some 4 us (three trips to memory that need each other: what the launch says;
-// length, pages and queries; rows).  131072 tokens of 8 heads of 128 (bf16, 537 MB): 98 us, 5.5 TB/s, and 4.7 for the
-// join; 64 sequences of 100 to 8000 tokens 224 us for 1.21 GB, 5.4 TB/s; 32768 tokens in E4M3 (68 MB) 15.7 us, 4.3 TB/s,
-// and 4.7.  Two and three tiles in flight a wave instead of one took 5% and 9% longer (8000 tokens in E4M3), as fewer
-// waves share a CU.
+// length, pages and queries; rows).  131072 tokens of 8 heads of 128 (bf16, 537 MB): 93 us, 5.8 TB/s, and 4.6 for the
+// join; 64 sequences of 100 to 8000 tokens 223 us for 1.21 GB, 5.4 TB/s; 32768 tokens in E4M3 (68 MB) 15.5 us, 4.4 TB/s,
+// and 4.7.  Two and three tiles in flight a wave instead of one gain nothing, whether one workgroup runs on a CU or
+// several (E4M3, us of a pass: 32768 tokens, where a wave walks eight tiles, 314, 315 and 323; 8000 tokens, two tiles a
+// wave, 88.8, 93.9 and 95.8; 16 sequences of 1000 to 16000 tokens 485, 501 and 510).
 #include "parts.h"
 #include "rows_kernels.h"
 

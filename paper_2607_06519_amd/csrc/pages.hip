@@ -12,7 +12,7 @@
 // HBM bound: every row is read once and written once, in pieces of 16 bytes a
 // lane (32 of a row on its way into E4M3); a workgroup takes some 16 consecutive tokens of one
 // head, which of a prompt lie side by side in their page.  8191 tokens of 8 heads of 128
-// in E4M3: 11.7 us written (4.3 TB/s, read plus written), 10.8 us read (4.7 TB/s).  A head's tokens before the next head's took
+// in E4M3: 11.6 us written (4.4 TB/s, read plus written), 11.1 us read (4.6 TB/s).  A head's tokens before the next head's took
 // 15.4 us written; two, four and eight rows a lane, all requested before the first is used, as long as one in E4M3
 // (93, 93 and 96 us for 32768 tokens written and read, one row 92) and longer in bf16.
 #include <type_traits>

@@ -13,17 +13,18 @@
 //   O^T += V^T P^T the probabilities are the B operand where they lie (the keys of
 //                  a lane's S^T registers are the keys of its B slots), A: transposed
 //                  reads of the V tile.
-// Workgroups with more keys come first.  Those of a KV head are hkv apart, which
-// for eight heads keeps a head's keys in one XCD's L2.
+// Tiles of query rows are taken from the call's last on down (of one prompt: those
+// with more keys first), but for calls whose workgroups all run at once (`launch`).
+// Workgroups of a KV head are hkv apart, which for eight heads keeps a head's keys in one XCD's L2.
 // Probabilities are rounded to bf16 (2^-8 each at most) for the product, their sum is not.
 // Calls of few rows and many keys split the keys over workgroups, whose
 // (acc, m, l) records a second launch joins.
 //
 // What bounds it.  Long prompts: the card's power.  32768 tokens of 32 + 8 heads of 128
-// (bf16) take 7.7 ms, 1.14 PFLOP/s, where a large matrix product of the library's reaches 1.37, at some 1.65 GHz
-// with the matrix units busy 61% of the time; with inputs of zeros the same call takes 4.97 ms, 1.77 PFLOP/s, and the
-// library's product reaches 1.79.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
-// tokens, now 517); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
+// (bf16) take 7.5 ms, 1.17 PFLOP/s, where a large matrix product of the library's reaches 1.43, at some 1.7 GHz
+// with the matrix units busy 60% of the time; with inputs of zeros the same call takes 4.99 ms, 1.76 PFLOP/s, and the
+// library's product reaches 1.81.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
+// tokens, now 496); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
 // groups of waves that take turns at the matrix units wait for their operands (8.7), the next tile's logits ahead of
 // this one's softmax gain 1% where they have the registers, and three or four tiles in LDS instead of two gain nothing
 // (32768 tokens 7.78 to 8.23 for 7.81, 2048 tokens 57 to 66 us for 51).  Prompts of 2048 tokens (51 us, 670 TFLOP/s) wait for their
@@ -124,7 +125,10 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t x) {
 
 // KEYS of a tile, workgroups to a CU.  (bf16 of 128 channels: tiles of 64 keys for calls of few workgroups, 32 for those of
 // many, of which a CU then holds three.  us, tiles of 64 and 32: a prompt of 1000 tokens 26.7 and 28.9, 2048 tokens 53.5 and
-// 57.3, 8191 tokens 515 and 512, 24 prompts of up to 2000 tokens 360 and 341, 32768 tokens 7770 and 7600.)
+// 57.3, 8191 tokens 515 and 512, 24 prompts of up to 2000 tokens 360 and 341, 32768 tokens 7770 and 7600, 250 tokens on 33018
+// keys 288 and 295.)  64 channels: four workgroups, although bf16 then spills some registers outside of the loops (us, four
+// and three, bf16: 2048 tokens 37.2 and 36.5, 8192 tokens 311 and 318, 32768 tokens 4651 and 4744, 24 prompts of up to 2000
+// tokens 218 and 221; fp32: 1000 tokens 63.1 and 63.4, 8192 tokens 2006 and 2064, the 24 prompts 1275 and 1264).
 constexpr int keys_of(int D, bool F32, bool many) { return F32 || (many && D == 128) ? 32 : 64; }
 constexpr int per_cu(int D, bool F32, int keys) { return D == 64 ? 4 : F32 || keys == 64 ? 2 : 3; }
 constexpr int kManyGroups = 1024, kCus = 256;
