@@ -332,7 +332,8 @@ class PagedCache:
     ``begin_step()`` takes a row for each active sequence, ``append(layer, k, v)``
     and ``decode(layer, q)`` store and attend layer by layer, ``advance()`` ends
     it.  ``cancel()`` gives up what has begun, a prompt's rows or a step, whatever
-    calls of it were made or failed, and leaves the sequences as they were.  ``read`` gives a sequence's rows back as ``probe`` and
+    calls of it were made or failed, and leaves the sequences as they were.
+    ``read`` gives a sequence's rows back as ``probe`` and
     ``CompressedCache.compress`` take them, and ``release`` its pages to others.
     ``decode(..., prefix=cache)`` also attends over a compressed prefix that the
     paged rows continue; ``begin_step(prefix=cache)`` then takes a row for the
@@ -365,7 +366,7 @@ class PagedCache:
         self.held = [[] for _ in range(self.batch)]         # pages of each sequence
         self.lens_host = [0] * self.batch                   # rows held before the current step
         self.active = [False] * self.batch
-        self._by_default = False                            # ... that hold rows, as none were named
+        self._by_default = False                            # the active sequences of the step were not named
         self._captured = None                               # the prefix of a captured step
         self._open = None                                   # rows of begin (or True: a step) that have not ended
         self.pos = torch.full((self.batch,), -1, dtype=torch.int32, device=device)  # row that a step writes
@@ -468,7 +469,8 @@ class PagedCache:
 
     def prompt(self, rows, layer: int, q, k, v, out=None, sm_scale: Optional[float] = None):
         """Stores the new rows ``k`` / ``v [n][Hkv][d]`` of ``layer`` and returns the attention of ``q [n][Hq][d]`` over them
-        and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held; a compressed prefix takes no part.)"""
+        and the earlier rows of their sequences.  (The new rows take part as they are given, earlier ones as held;
+        a compressed prefix takes no part.)"""
         torch = _torch()
         if rows is not self._open:
             raise RuntimeError("not the rows that have begun")

@@ -59,7 +59,6 @@ struct Paged {
   }
 };
 
-// Writes row g of the output, or its record, from acc (unnormalised), m and l.
 template <int D, int TY>
 __global__ __launch_bounds__(256) void paged_attn_kernel(PagedParams P) {
   using S = Paged<D, TY>;

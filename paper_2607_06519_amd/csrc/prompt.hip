@@ -21,7 +21,7 @@
 // (acc, m, l) records a second launch joins.
 //
 // What bounds it.  Long prompts: the card's power.  32768 tokens of 32 + 8 heads of 128
-// (bf16) take 7.5 ms, 1.17 PFLOP/s, where a large matrix product of the library's reaches 1.43, at some 1.7 GHz
+// (bf16) take 7.5 ms, 1.18 PFLOP/s, where a large matrix product of the library's reaches 1.43, at some 1.7 GHz
 // with the matrix units busy 60% of the time; with inputs of zeros the same call takes 4.99 ms, 1.76 PFLOP/s, and the
 // library's product reaches 1.81.  Key tiles that pass through registers on their way to LDS spill (2028 us for 8191
 // tokens, now 496); 64 rows a wave, which halve what is read from LDS, leave one wave a SIMD (32768 tokens 8.8 ms), two
